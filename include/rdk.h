@@ -1,7 +1,8 @@
 /*
  * rdk.h -- C ABI of the MI355X (gfx950) library for Redistributing Drafter Kernels (RDK).
  *
- * The library covers the data-parallel hot path of the method: for a batch of B positions it
+ * The library covers the data-parallel hot path of the method, and beside it what its drafter is trained on and what decodes the same
+ * rows without drawing: the teacher's top logits, distillation from them, beam search.  For a batch of B positions it
  * redistributes a vocabulary-pruned drafter's distribution q (n kept ids) onto the target
  * vocabulary (N ids) through a row-stochastic token-affinity kernel M (Alg. 1 of the paper), and
  * runs the accept / residual / sample step of speculative decoding against the target
@@ -318,6 +319,107 @@ rdk_status_t rdk_verify_multi(const rdk_multi_desc_t *desc, const void *p, rdk_i
 rdk_status_t rdk_tree_walk(int32_t S, int32_t nodes, int32_t C, const int32_t *child_node, const int32_t *accepted,
                            const int32_t *token, int32_t *n_accepted, int32_t *out_tokens, void *stream);
 
+/*
+ * The k largest entries of every row and the logarithm of its normaliser: what is kept of a teacher's rows (rdk_distill_*), or of
+ * redistributed rows.  Per row b of x [B, ldx] over N ids:
+ *   ids[b, :]    = the ids of the k largest unmasked entries, descending, equal entries by ascending id; a logit of -inf and a weight of 0
+ *                  are masked; -1 where fewer than k are left.  A NaN counts as larger than any number.
+ *   values[b, :] = the entries themselves (logits are not divided by the temperature), widened to fp32; -inf (logits) or 0 (weights) beside -1.
+ *   lse[b]       = log sum_j exp(x_bj / temperature) for logits, log sum_j x_bj for weights (temperature 1); -inf for a row that is
+ *                  masked altogether; NaN for a row with a NaN or a logit of +inf.  May be NULL.
+ * ids and values are [B, k] without gaps.  1 <= k <= min(N, 128), temperature > 0 and finite.  The ids and values are exact, whatever the
+ * input; sums run in fp32.  Rows that crowd out the fast way (thousands of entries that tie with the k-th) take a slower one.
+ * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, N, k, ldx, temperature), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x or the workspace),
+ * RDK_ERR_UNSUPPORTED (k above 128; weights with a temperature other than 1), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ */
+typedef struct {
+    int32_t B, N, k;            /* rows, ids, entries kept per row */
+    float temperature;          /* of lse */
+} rdk_topk_desc_t;
+rdk_status_t rdk_topk_workspace_bytes(const rdk_topk_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes);
+rdk_status_t rdk_topk(const rdk_topk_desc_t *desc, const void *x, rdk_input_kind_t x_kind, int64_t ldx, int32_t *ids, float *values,
+                      float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Distillation of a drafter from its teacher's top logits.  Per position b the drafter has logits z [B, ldz] over its n kept slots (fp32
+ * or bf16) and the teacher K entries: top_ids [B, K] target ids and top_logits [B, K] fp32 (rdk_topk writes both).  `kernel` (any
+ * format) says which slot a target id has; with NULL the ids are slots themselves.  An entry counts if its id lies in the drafter's vocabulary
+ * and its logit is above -inf; others (id -1, pruned ids) are passed over.  The ids of a row that count are distinct.  With T = temperature,
+ * s = softmax(z_b / T), A = the slots of the entries that count and w = weight[b] (NULL: 1):
+ *   teacher_lse == NULL: the teacher is renormalised over A (Eq. 1 of the paper on its own rows),  t_k = exp(v_k / T) / sum_A exp(v / T):
+ *     loss[b] = w sum_A t (log t - log s),   dz[b, j] = w / T (s_j - t_j);      both 0 if A is empty.
+ *   teacher_lse [B] = log sum exp(v / T) over the teacher's whole row (rdk_topk's lse at this temperature):  t_k = exp(v_k / T - lse), and what
+ *     remains, r = max(0, 1 - sum_A t), is held against the drafter's remainder rho = sum_{j not in A} s_j:
+ *     loss[b] = w (sum_A t (log t - log s) + r (log r - log rho)),
+ *     dz[b, j] = w / T (s_j - t_j) on A,  w / T s_j (1 - r / rho) elsewhere;    without a slot outside A as if teacher_lse were NULL.
+ * A row of weight 0 has loss 0 and gradient 0 whatever its logits hold (they are not read).  Masked logits (-inf) have s = 0: the loss is +inf
+ * where the teacher has mass on them.  A drafter row that is masked altogether has s = 0 everywhere.  NaN in a row that counts shows in its loss.
+ *   rdk_distill_loss       forward: loss [B] and stats [B, 4] fp32, which the backward call reads (contents not part of the interface).
+ *   rdk_distill_grad       backward: dz [B, ldd] of z's type from stats; weight is what comes from above (d / d loss[b], times whatever
+ *                          weight the forward call had).  Same z, top_ids, top_logits and temperature as in the forward call.  No workspace.
+ *   rdk_distill_loss_grad  both at once, for weights known beforehand; z is read once where a row fits the registers.  stats may be NULL.
+ * dz may be z itself (same stride), else they must not overlap.  Sums and statistics are held in fp32; a bf16 gradient is rounded once.
+ * 1 <= K <= 128; top_ids and top_logits without gaps.
+ * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, n, K, strides, temperature, n other than the kernel's), RDK_ERR_DTYPE, RDK_ERR_ALIGN (z, dz, workspace),
+ * RDK_ERR_UNSUPPORTED (K above 128; rows of probabilities), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ */
+typedef struct {
+    int32_t B, n, K;            /* positions, drafter slots, teacher entries per position */
+    float temperature;
+} rdk_distill_desc_t;
+rdk_status_t rdk_distill_workspace_bytes(const rdk_distill_desc_t *desc, rdk_input_kind_t z_kind, size_t *bytes);
+rdk_status_t rdk_distill_loss(const rdk_distill_desc_t *desc, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t z_kind, int64_t ldz,
+                              const int32_t *top_ids, const float *top_logits, const float *teacher_lse, const float *weight, float *loss,
+                              float *stats, void *workspace, size_t workspace_bytes, void *stream);
+rdk_status_t rdk_distill_grad(const rdk_distill_desc_t *desc, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t z_kind, int64_t ldz,
+                              const int32_t *top_ids, const float *top_logits, const float *stats, const float *weight, void *dz, int64_t ldd,
+                              void *stream);
+rdk_status_t rdk_distill_loss_grad(const rdk_distill_desc_t *desc, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t z_kind,
+                                   int64_t ldz, const int32_t *top_ids, const float *top_logits, const float *teacher_lse, const float *weight,
+                                   float *loss, float *stats, void *dz, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Beam search's selection over beams and vocabulary.  G requests of W beams; x [G W, ldx] the next-token rows of the beams (logits, or weights
+ * such as redistributed rows), scores [G, W] their scores (summed log-probabilities).  Candidates of a request:
+ *   a live beam w: every unmasked id j, with  scores[w] + log softmax(x_w)_j  (weights: log(x_wj / sum x_w)), formed in fp32 as
+ *     scores[w] + ((x_wj - max x_w) - log sum exp(x_w - max x_w));
+ *   a beam with finished[w] != 0: the id eos alone, with scores[w];   a beam of score -inf: none.  Rows of such beams are not read.
+ * The K best by descending score, equal scores by ascending beam, then id (of a beam only its K largest entries are candidates, equal entries by
+ * ascending id): scores_out, parent (beam 0 .. W-1), token, finished_out (the beam was finished, or token == eos), all [G, K]; score -inf,
+ * parent -1, token -1, finished 0 where there are fewer.  NaN and +inf in a live row make its scores NaN, which rank first.
+ * finished and finished_out may be NULL; eos = -1: no id ends a beam (finished must be NULL then).  Outputs must not overlap the inputs.
+ * 1 <= W <= 64, 1 <= K <= 128, W N < 2^31.
+ * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (G, W, N, K, ldx, eos, an output that overlaps its input), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x, workspace),
+ * RDK_ERR_UNSUPPORTED (limits), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ */
+typedef struct {
+    int32_t G, W, N, K;         /* requests, beams per request, ids, candidates kept per request */
+    int32_t eos;                /* id that ends a beam, or -1 */
+} rdk_beam_desc_t;
+rdk_status_t rdk_beam_select_workspace_bytes(const rdk_beam_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes);
+rdk_status_t rdk_beam_select(const rdk_beam_desc_t *desc, const void *x, rdk_input_kind_t x_kind, int64_t ldx, const float *scores,
+                             const uint8_t *finished, float *scores_out, int32_t *parent, int32_t *token, uint8_t *finished_out,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The states of the beams after a selection: row i of request g in dst becomes row parent[g, i] of request g in src, for `count` states at once
+ * (`states` is a HOST array of device buffers: key-value caches, token histories, recurrent states).  parent [G, K] (device) holds beams
+ * 0 .. W-1; a row whose parent is -1 (or not a beam) is left as it is.  src has G W rows, dst G K rows.  A row is `segments` pieces of segment_bytes, *_pitch
+ * bytes apart (the filled part of a cache with room for more), rows are *_stride bytes apart; any alignment (fastest where everything is a
+ * multiple of 16).  dst == src with the same strides reorders in place (K must be W), rows that keep their beam are then not touched; otherwise
+ * src and dst must not overlap.  Segments of a state must not overlap one another, nor states.  Copies are exact.
+ * 1 <= W, K <= 64; no workspace.
+ * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (sizes, strides, overlap, K other than W in place), RDK_ERR_UNSUPPORTED (W or K above 64), RDK_ERR_HIP.
+ */
+typedef struct {
+    const void *src;            /* device */
+    void *dst;                  /* device */
+    int64_t src_stride, dst_stride;   /* bytes from one beam's row to the next */
+    int64_t segments, segment_bytes;  /* pieces of a row, and their size */
+    int64_t src_pitch, dst_pitch;     /* bytes from one piece to the next (ignored for one piece) */
+} rdk_state_t;
+rdk_status_t rdk_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *parent, const rdk_state_t *states, int32_t count, void *stream);
+
 /* The four Philox words of `count` consecutive positions, [count, 4] uint32 on the device (for
  * checking the random stream against an independent implementation). */
 rdk_status_t rdk_philox_words(uint64_t seed, uint64_t offset, int32_t count, uint32_t *words,
@@ -335,7 +437,8 @@ rdk_status_t rdk_philox_words(uint64_t seed, uint64_t offset, int32_t count, uin
  * sequence_scan_kernel, taylor_stats_kernel, taylor_write_kernel, taylor_row_kernel, taylor_whole_kernel, tli_scatter_kernel,
  * tree_walk_kernel, verify_multi_kernel, verify_multi_round_kernel,
  * q_transpose_kernel, sparse_product_kernel, prep_a_split_kernel, exact_f32_split_kernel,
- * exact_reduce_kernel, prep_a_bf16_kernel, exact_bf16_kernel.
+ * exact_reduce_kernel, prep_a_bf16_kernel, exact_bf16_kernel, topk_part_kernel, topk_merge_kernel, beam_merge_kernel, beam_reorder_kernel,
+ * distill_row_kernel, distill_part_kernel, distill_finish_kernel, distill_grad_kernel.
  */
 rdk_status_t rdk_timing_select(const char *kernel_name);
 rdk_status_t rdk_timing_read(const char *kernel_name, int64_t *launches, double *total_ms);

@@ -636,6 +636,206 @@ rdk_status_t rdk_redistribute_verify(const rdk_kernel_t *kernel, rdk_linear_mode
     return launch_sparse_fused(h, c, workspace, (hipStream_t)stream);
 }
 
+static bool temperature_ok(float t) { return t > 0.f && t < INFINITY; }
+
+static rdk_status_t check_topk(const rdk_topk_desc_t *d, rdk_input_kind_t kind)
+{
+    if (!d) return RDK_ERR_NULL;
+    if (!kind_ok(kind)) return RDK_ERR_DTYPE;
+    if (d->B < 1 || d->N < 1 || d->k < 1 || d->k > d->N || !temperature_ok(d->temperature)) return RDK_ERR_SHAPE;
+    if (d->k > select_max_entries() || (kind == RDK_PROB_F32 && d->temperature != 1.f)) return RDK_ERR_UNSUPPORTED;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_topk_workspace_bytes(const rdk_topk_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes)
+{
+    if (!bytes) return RDK_ERR_NULL;
+    rdk_status_t rc = check_topk(desc, x_kind);
+    if (rc != RDK_OK) return rc;
+    *bytes = topk_workspace_bytes(*desc, x_kind) + 256;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_topk(const rdk_topk_desc_t *desc, const void *x, rdk_input_kind_t x_kind, int64_t ldx, int32_t *ids, float *values,
+                      float *lse, void *workspace, size_t workspace_bytes, void *stream)
+{
+    size_t need = 0;
+    rdk_status_t rc = rdk_topk_workspace_bytes(desc, x_kind, &need);
+    if (rc != RDK_OK) return rc;
+    rc = check_rows(x, x_kind, ldx, desc->N);
+    if (rc != RDK_OK) return rc;
+    if (!ids || !values || !workspace) return RDK_ERR_NULL;
+    if (!aligned16(workspace)) return RDK_ERR_ALIGN;
+    if (workspace_bytes < need) return RDK_ERR_WORKSPACE;
+    return launch_topk(*desc, RowInput{x, x_kind, ldx}, ids, values, lse, workspace, (hipStream_t)stream);
+}
+
+static rdk_status_t check_distill(const rdk_distill_desc_t *d, rdk_input_kind_t kind)
+{
+    if (!d) return RDK_ERR_NULL;
+    if (!kind_ok(kind)) return RDK_ERR_DTYPE;
+    if (d->B < 1 || d->n < 1 || d->K < 1 || !temperature_ok(d->temperature)) return RDK_ERR_SHAPE;
+    if (d->K > distill_max_entries() || kind == RDK_PROB_F32) return RDK_ERR_UNSUPPORTED;
+    return RDK_OK;
+}
+
+static rdk_status_t check_distill_call(const rdk_distill_desc_t *d, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t kind, int64_t ldz,
+                                       const int32_t *top_ids, const float *top_logits)
+{
+    rdk_status_t rc = check_distill(d, kind);
+    if (rc != RDK_OK) return rc;
+    rc = check_rows(z, kind, ldz, d->n);
+    if (rc != RDK_OK) return rc;
+    if (!top_ids || !top_logits) return RDK_ERR_NULL;
+    return kernel && kernel->h.n != d->n ? RDK_ERR_SHAPE : RDK_OK;
+}
+
+// dz is z itself or lies apart from it
+static rdk_status_t check_gradient(const rdk_distill_desc_t *d, rdk_input_kind_t kind, const void *z, int64_t ldz, const void *dz, int64_t ldd)
+{
+    if (!dz) return RDK_ERR_NULL;
+    if (ldd < d->n) return RDK_ERR_SHAPE;
+    if (!aligned16(dz)) return RDK_ERR_ALIGN;
+    if (dz == z) return ldd == ldz ? RDK_OK : RDK_ERR_SHAPE;
+    const int64_t size = kind == RDK_LOGIT_BF16 ? 2 : 4;
+    const uintptr_t a = (uintptr_t)z, b = (uintptr_t)dz;
+    const uintptr_t a_end = a + ((uint64_t)(d->B - 1) * ldz + d->n) * size, b_end = b + ((uint64_t)(d->B - 1) * ldd + d->n) * size;
+    return a < b_end && b < a_end ? RDK_ERR_SHAPE : RDK_OK;
+}
+
+rdk_status_t rdk_distill_workspace_bytes(const rdk_distill_desc_t *desc, rdk_input_kind_t z_kind, size_t *bytes)
+{
+    if (!bytes) return RDK_ERR_NULL;
+    rdk_status_t rc = check_distill(desc, z_kind);
+    if (rc != RDK_OK) return rc;
+    *bytes = distill_workspace_bytes(*desc, z_kind) + 256;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_distill_loss(const rdk_distill_desc_t *desc, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t z_kind, int64_t ldz,
+                              const int32_t *top_ids, const float *top_logits, const float *teacher_lse, const float *weight, float *loss,
+                              float *stats, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rdk_status_t rc = check_distill_call(desc, kernel, z, z_kind, ldz, top_ids, top_logits);
+    if (rc != RDK_OK) return rc;
+    if (!loss || !stats || !workspace) return RDK_ERR_NULL;
+    if (!aligned16(stats) || !aligned16(workspace)) return RDK_ERR_ALIGN;
+    if (workspace_bytes < distill_workspace_bytes(*desc, z_kind)) return RDK_ERR_WORKSPACE;
+    return launch_distill_loss(*desc, kernel ? &kernel->h : nullptr, RowInput{z, z_kind, ldz}, top_ids, top_logits, teacher_lse, weight, loss,
+                               stats, nullptr, 0, workspace, (hipStream_t)stream);
+}
+
+rdk_status_t rdk_distill_grad(const rdk_distill_desc_t *desc, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t z_kind, int64_t ldz,
+                              const int32_t *top_ids, const float *top_logits, const float *stats, const float *weight, void *dz, int64_t ldd,
+                              void *stream)
+{
+    rdk_status_t rc = check_distill_call(desc, kernel, z, z_kind, ldz, top_ids, top_logits);
+    if (rc != RDK_OK) return rc;
+    if (!stats) return RDK_ERR_NULL;
+    if (!aligned16(stats)) return RDK_ERR_ALIGN;
+    rc = check_gradient(desc, z_kind, z, ldz, dz, ldd);
+    if (rc != RDK_OK) return rc;
+    return launch_distill_grad(*desc, kernel ? &kernel->h : nullptr, RowInput{z, z_kind, ldz}, top_ids, top_logits, stats, weight, dz, ldd,
+                               (hipStream_t)stream);
+}
+
+rdk_status_t rdk_distill_loss_grad(const rdk_distill_desc_t *desc, const rdk_kernel_t *kernel, const void *z, rdk_input_kind_t z_kind,
+                                   int64_t ldz, const int32_t *top_ids, const float *top_logits, const float *teacher_lse, const float *weight,
+                                   float *loss, float *stats, void *dz, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rdk_status_t rc = check_distill_call(desc, kernel, z, z_kind, ldz, top_ids, top_logits);
+    if (rc != RDK_OK) return rc;
+    if (!loss || !workspace) return RDK_ERR_NULL;
+    if (!aligned16(workspace) || (stats && !aligned16(stats))) return RDK_ERR_ALIGN;
+    rc = check_gradient(desc, z_kind, z, ldz, dz, ldd);
+    if (rc != RDK_OK) return rc;
+    if (workspace_bytes < distill_workspace_bytes(*desc, z_kind)) return RDK_ERR_WORKSPACE;
+    return launch_distill_loss(*desc, kernel ? &kernel->h : nullptr, RowInput{z, z_kind, ldz}, top_ids, top_logits, teacher_lse, weight, loss,
+                               stats, dz, ldd, workspace, (hipStream_t)stream);
+}
+
+static rdk_status_t check_beam(const rdk_beam_desc_t *d, rdk_input_kind_t kind)
+{
+    if (!d) return RDK_ERR_NULL;
+    if (!kind_ok(kind)) return RDK_ERR_DTYPE;
+    if (d->G < 1 || d->W < 1 || d->N < 1 || d->K < 1 || d->eos < -1 || d->eos >= d->N) return RDK_ERR_SHAPE;
+    if (d->W > reorder_max_beams() || d->K > select_max_entries()) return RDK_ERR_UNSUPPORTED;
+    if ((int64_t)d->W * d->N > INT32_MAX || (int64_t)d->G * d->W > INT32_MAX) return RDK_ERR_UNSUPPORTED;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_beam_select_workspace_bytes(const rdk_beam_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes)
+{
+    if (!bytes) return RDK_ERR_NULL;
+    rdk_status_t rc = check_beam(desc, x_kind);
+    if (rc != RDK_OK) return rc;
+    *bytes = beam_select_workspace_bytes(*desc, x_kind) + 256;
+    return RDK_OK;
+}
+
+static bool overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes)
+{
+    return a && b && (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
+rdk_status_t rdk_beam_select(const rdk_beam_desc_t *desc, const void *x, rdk_input_kind_t x_kind, int64_t ldx, const float *scores,
+                             const uint8_t *finished, float *scores_out, int32_t *parent, int32_t *token, uint8_t *finished_out,
+                             void *workspace, size_t workspace_bytes, void *stream)
+{
+    size_t need = 0;
+    rdk_status_t rc = rdk_beam_select_workspace_bytes(desc, x_kind, &need);
+    if (rc != RDK_OK) return rc;
+    rc = check_rows(x, x_kind, ldx, desc->N);
+    if (rc != RDK_OK) return rc;
+    if (!scores || !scores_out || !parent || !token || !workspace) return RDK_ERR_NULL;
+    if (finished && desc->eos < 0) return RDK_ERR_SHAPE;
+    const size_t in = (size_t)desc->G * desc->W, out = (size_t)desc->G * desc->K;
+    if (overlap(scores, in * 4, scores_out, out * 4) || overlap(finished, in, finished_out, out)) return RDK_ERR_SHAPE;
+    if (!aligned16(workspace)) return RDK_ERR_ALIGN;
+    if (workspace_bytes < need) return RDK_ERR_WORKSPACE;
+    return launch_beam_select(*desc, RowInput{x, x_kind, ldx}, scores, finished, scores_out, parent, token, finished_out, workspace,
+                              (hipStream_t)stream);
+}
+
+// One state: sizes, strides that keep rows and pieces apart, and either in place or apart.
+static rdk_status_t check_state(const rdk_state_t &s, int64_t G, int32_t W, int32_t K)
+{
+    constexpr int64_t kMost = (int64_t)1 << 46;   // bytes: products below stay inside 64 bits
+    if (s.segments < 0 || s.segment_bytes < 0 || s.segments > kMost || s.segment_bytes > kMost) return RDK_ERR_SHAPE;
+    if (s.segments == 0 || s.segment_bytes == 0) return RDK_OK;   // nothing to do
+    if (!s.src || !s.dst) return RDK_ERR_NULL;
+    int64_t span[2];
+    for (int i = 0; i < 2; ++i) {
+        const int64_t stride = i ? s.dst_stride : s.src_stride, rows = G * (i ? K : W);
+        int64_t row = s.segment_bytes;
+        if (s.segments > 1) {
+            const int64_t pitch = i ? s.dst_pitch : s.src_pitch;
+            if (pitch < s.segment_bytes || pitch > kMost / s.segments) return RDK_ERR_SHAPE;
+            row += (s.segments - 1) * pitch;
+        }
+        if (stride < 0 || (rows > 1 && (stride < s.segment_bytes || stride > kMost / rows))) return RDK_ERR_SHAPE;
+        // pieces side by side along the rows (a state stored piece by piece) or rows one behind the other; anything between may overlap
+        const int64_t pitch = i ? s.dst_pitch : s.src_pitch;
+        if (rows > 1 && stride < row && !(s.segments > 1 && pitch >= (rows - 1) * stride + s.segment_bytes)) return RDK_ERR_SHAPE;
+        span[i] = (rows > 1 ? (rows - 1) * stride : 0) + row;
+    }
+    if (s.src == s.dst)
+        return K == W && s.src_stride == s.dst_stride && (s.segments == 1 || s.src_pitch == s.dst_pitch) ? RDK_OK : RDK_ERR_SHAPE;
+    return overlap(s.src, (size_t)span[0], s.dst, (size_t)span[1]) ? RDK_ERR_SHAPE : RDK_OK;
+}
+
+rdk_status_t rdk_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *parent, const rdk_state_t *states, int32_t count, void *stream)
+{
+    if (G < 1 || W < 1 || K < 1 || count < 0) return RDK_ERR_SHAPE;
+    if (W > reorder_max_beams() || K > reorder_max_beams()) return RDK_ERR_UNSUPPORTED;
+    if (!parent || (count > 0 && !states)) return RDK_ERR_NULL;
+    for (int32_t i = 0; i < count; ++i) {
+        const rdk_status_t rc = check_state(states[i], G, W, K);
+        if (rc != RDK_OK) return rc;
+    }
+    return launch_beam_reorder(G, W, K, parent, states, count, (hipStream_t)stream);
+}
+
 rdk_status_t rdk_timing_select(const char *kernel_name)
 {
     std::lock_guard<std::mutex> lock(g_timing_mutex);

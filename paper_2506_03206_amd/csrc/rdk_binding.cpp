@@ -12,6 +12,8 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <vector>
+
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -93,7 +95,7 @@ struct Rows {   // a [B, len] input
 
 struct Names {
     PyObject *h, *ws, *draft_ws, *fused_ws, *out_ws, *draft_ids, *accept, *alpha, *resid_mass, *resid_ids, *n_accepted, *out_tokens,
-        *cand_ids, *accepted, *token, *B, *N, *gamma;
+        *cand_ids, *accepted, *token, *B, *N, *gamma, *ids, *values, *lse, *loss, *stats, *grad, *scores, *parent, *finished;
 } g;
 
 struct Ref {   // an owned reference
@@ -407,10 +409,207 @@ PyObject *tree_walk(PyObject *const *a)
     return t;
 }
 
+float real(PyObject *o)
+{
+    const double v = PyFloat_AsDouble(o);
+    if (v == -1.0 && PyErr_Occurred()) throw PyFail{};
+    return (float)v;
+}
+
+// data pointer of a device tensor of `count` values without gaps
+template <class T>
+T *plain(PyObject *o, at::ScalarType type, int64_t count, const char *what)
+{
+    const at::Tensor &t = tensor(o, what);
+    need(t.scalar_type() == type && t.numel() == count && t.is_contiguous() && t.is_cuda(), what);
+    return (T *)ptr(t);
+}
+
+template <class T>
+T *plain_or_none(PyObject *o, at::ScalarType type, int64_t count, const char *what)
+{
+    return o == Py_None ? nullptr : plain<T>(o, type, count, what);
+}
+
+template <class T>
+T *plain_attr(PyObject *obj, PyObject *name, at::ScalarType type, int64_t count, const char *what)
+{
+    Ref a(PyObject_GetAttr(obj, name));
+    return plain<T>(a.o, type, count, what);
+}
+
+int32_t extent(const at::Tensor &t, int64_t dim, const char *what)
+{
+    need(t.dim() == 2 && t.size(dim) <= INT32_MAX, what);
+    return (int32_t)t.size(dim);
+}
+
+// x, k, x_kind, temperature, outputs
+PyObject *topk(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[0], "x is not a tensor");
+    PyObject *o = a[4];
+    rdk_topk_desc_t d;
+    d.B = extent(x, 0, "x is a [B, N] tensor");
+    d.N = extent(x, 1, "x is a [B, N] tensor");
+    d.k = int32_of(a[1]);
+    d.temperature = real(a[3]);
+    const Rows xi(x, a[2]);
+    size_t bytes = 0;
+    const rdk_status_t rc = rdk_topk_workspace_bytes(&d, xi.kind, &bytes);
+    if (rc != RDK_OK) return status(rc);
+    const int64_t count = (int64_t)d.B * d.k;
+    const char *what = "the outputs were made for another batch shape";
+    int32_t *ids = plain_attr<int32_t>(o, g.ids, at::kInt, count, what);
+    float *values = plain_attr<float>(o, g.values, at::kFloat, count, what), *lse = plain_attr<float>(o, g.lse, at::kFloat, d.B, what);
+    const Scratch w = workspace(o, g.out_ws, bytes, x);
+    void *st = stream();
+    return status(unlocked([&] { return rdk_topk(&d, xi.p, xi.kind, xi.ld, ids, values, lse, w.p, w.bytes, st); }));
+}
+
+// kernel or None, z, top_ids, top_logits, teacher_lse or None, temperature, weight or None, outputs, part (0: loss, 1: loss and gradient, 2: gradient)
+PyObject *distill(PyObject *const *a)
+{
+    const rdk_kernel_t *k = a[0] == Py_None ? nullptr : handle(a[0]);
+    const at::Tensor &z = tensor(a[1], "z is not a tensor"), &top = tensor(a[2], "top_ids is not a tensor");
+    PyObject *o = a[7];
+    const int32_t part = int32_of(a[8]);
+    rdk_distill_desc_t d;
+    d.B = extent(z, 0, "z is a [B, n] tensor");
+    d.n = extent(z, 1, "z is a [B, n] tensor");
+    d.K = extent(top, 1, "top_ids is a [B, K] tensor");
+    d.temperature = real(a[5]);
+    need(z.scalar_type() == at::kFloat || z.scalar_type() == at::kBFloat16, "logits are float32 or bfloat16");
+    const rdk_input_kind_t kind = z.scalar_type() == at::kBFloat16 ? RDK_LOGIT_BF16 : RDK_LOGIT_F32;
+    const int64_t ldz = rows(z), count = (int64_t)d.B * d.K;
+    need(top.size(0) == d.B, "top_ids holds one row per row of z");
+    const int32_t *ids = plain<int32_t>(a[2], at::kInt, count, "top_ids: int32 [B, K] on the device, without gaps");
+    const float *logits = plain<float>(a[3], at::kFloat, count, "top_logits: float32 [B, K] on the device, without gaps");
+    const float *lse = plain_or_none<float>(a[4], at::kFloat, d.B, "teacher_lse: float32 [B] on the device");
+    const float *weight = plain_or_none<float>(a[6], at::kFloat, d.B, "weight: float32 [B] on the device");
+    const char *what = "the outputs were made for another batch shape";
+    float *loss = plain_attr<float>(o, g.loss, at::kFloat, d.B, what), *stats = plain_attr<float>(o, g.stats, at::kFloat, 4 * (int64_t)d.B, what);
+    void *zp = ptr(z), *st = stream(), *dz = nullptr;
+    int64_t ldd = 0;
+    if (part) {
+        Ref r(PyObject_GetAttr(o, g.grad));
+        const at::Tensor &t = tensor(r.o, "the outputs hold no gradient");
+        need(t.scalar_type() == z.scalar_type() && t.dim() == 2 && t.size(0) == d.B && t.size(1) == d.n, "the gradient has z's shape and type");
+        ldd = rows(t);
+        dz = ptr(t);
+    }
+    if (part == 2)
+        return status(unlocked([&] { return rdk_distill_grad(&d, k, zp, kind, ldz, ids, logits, stats, weight, dz, ldd, st); }));
+    size_t bytes = 0;
+    const rdk_status_t rc = rdk_distill_workspace_bytes(&d, kind, &bytes);
+    if (rc != RDK_OK) return status(rc);
+    const Scratch w = workspace(o, g.out_ws, bytes, z);
+    if (part == 1)
+        return status(unlocked([&] {
+            return rdk_distill_loss_grad(&d, k, zp, kind, ldz, ids, logits, lse, weight, loss, stats, dz, ldd, w.p, w.bytes, st);
+        }));
+    return status(unlocked([&] { return rdk_distill_loss(&d, k, zp, kind, ldz, ids, logits, lse, weight, loss, stats, w.p, w.bytes, st); }));
+}
+
+// x, scores, K, x_kind, finished or None, eos, outputs
+PyObject *beam_select(PyObject *const *a)
+{
+    const at::Tensor &x = tensor(a[0], "x is not a tensor"), &scores = tensor(a[1], "scores is not a tensor");
+    PyObject *o = a[6];
+    rdk_beam_desc_t d;
+    d.G = extent(scores, 0, "scores is a [G, W] tensor");
+    d.W = extent(scores, 1, "scores is a [G, W] tensor");
+    d.N = extent(x, 1, "x is a [G W, N] tensor");
+    d.K = int32_of(a[2]);
+    d.eos = int32_of(a[5]);
+    const int64_t in = (int64_t)d.G * d.W, out = (int64_t)d.G * d.K;
+    need(x.size(0) == in, "x holds one row per beam");
+    const Rows xi(x, a[3]);
+    const float *si = plain<float>(a[1], at::kFloat, in, "scores: float32 [G, W] on the device, without gaps");
+    const uint8_t *fi = plain_or_none<uint8_t>(a[4], at::kByte, in, "finished: uint8 [G, W] on the device, without gaps");
+    size_t bytes = 0;
+    const rdk_status_t rc = rdk_beam_select_workspace_bytes(&d, xi.kind, &bytes);
+    if (rc != RDK_OK) return status(rc);
+    const char *what = "the outputs were made for another batch shape";
+    float *so = plain_attr<float>(o, g.scores, at::kFloat, out, what);
+    int32_t *parent = plain_attr<int32_t>(o, g.parent, at::kInt, out, what), *token = plain_attr<int32_t>(o, g.token, at::kInt, out, what);
+    uint8_t *fo = plain_attr<uint8_t>(o, g.finished, at::kByte, out, what);
+    const Scratch w = workspace(o, g.out_ws, bytes, x);
+    void *st = stream();
+    return status(unlocked([&] { return rdk_beam_select(&d, xi.p, xi.kind, xi.ld, si, fi, so, parent, token, fo, w.p, w.bytes, st); }));
+}
+
+// One state of beams for rdk_beam_reorder: its rows as pieces with at most one gap between them.
+rdk_state_t state_of(const at::Tensor &src, const at::Tensor &dst)
+{
+    need(src.is_cuda() && dst.is_cuda() && src.scalar_type() == dst.scalar_type() && src.dim() >= 1 && dst.dim() == src.dim(),
+         "a state and its destination are device tensors of one type");
+    const int64_t size = (int64_t)src.element_size();
+    rdk_state_t s{};
+    s.src = ptr(src);
+    s.dst = ptr(dst);
+    s.src_stride = src.stride(0) * size;
+    s.dst_stride = dst.stride(0) * size;
+    s.segments = 1;
+    int64_t piece = 1;   // elements
+    bool whole = true;   // no gap met so far
+    for (int64_t i = src.dim() - 1; i >= 1; --i) {
+        const int64_t n = src.size(i);
+        need(dst.size(i) == n, "a state and its destination have rows of one shape");
+        if (n == 1) continue;
+        if (n == 0) {
+            piece = 0;
+            break;
+        }
+        if (whole && src.stride(i) == piece && dst.stride(i) == piece) {
+            piece *= n;
+            continue;
+        }
+        if (whole) {
+            whole = false;
+            s.src_pitch = src.stride(i) * size;
+            s.dst_pitch = dst.stride(i) * size;
+            s.segments = n;
+            continue;
+        }
+        need(src.stride(i) * size == s.src_pitch * s.segments && dst.stride(i) * size == s.dst_pitch * s.segments,
+             "the rows of a state have more than one gap");
+        s.segments *= n;
+    }
+    s.segment_bytes = piece * size;
+    return s;
+}
+
+// states, parent, W, out or None
+PyObject *beam_reorder(PyObject *const *a)
+{
+    const at::Tensor &parent = tensor(a[1], "parent is not a tensor");
+    const int32_t G = extent(parent, 0, "parent is a [G, K] tensor"), K = extent(parent, 1, "parent is a [G, K] tensor"), W = int32_of(a[2]);
+    const int32_t *pi = plain<int32_t>(a[1], at::kInt, (int64_t)G * K, "parent: int32 [G, K] on the device, without gaps");
+    Ref in(PySequence_Fast(a[0], "states is a list of tensors"));
+    const bool apart = a[3] != Py_None;
+    Ref out(PySequence_Fast(apart ? a[3] : a[0], "out is a list of tensors"));
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(in.o);
+    need(PySequence_Fast_GET_SIZE(out.o) == count && count <= INT32_MAX, "one destination per state");
+    std::vector<rdk_state_t> states;
+    std::vector<at::Tensor> held;   // another thread may change the lists during the call
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        held.push_back(tensor(PySequence_Fast_GET_ITEM(in.o, i), "a state is not a tensor"));
+        held.push_back(tensor(PySequence_Fast_GET_ITEM(out.o, i), "a destination is not a tensor"));
+        const at::Tensor &src = held[2 * i], &dst = held[2 * i + 1];
+        need(src.dim() >= 1 && dst.dim() >= 1 && src.size(0) == (int64_t)G * W && dst.size(0) == (int64_t)G * K,
+             "states have G W rows, their destinations G K");
+        states.push_back(state_of(src, dst));
+    }
+    void *st = stream();
+    return status(unlocked([&] { return rdk_beam_reorder(G, W, K, pi, states.data(), (int32_t)count, st); }));
+}
+
 #define RDK_METHOD(NAME, COUNT) {#NAME, (PyCFunction)(void (*)(void))(&guarded<NAME, COUNT>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RDK_METHOD(redistribute_verify, 12), RDK_METHOD(verify_sample, 9),  RDK_METHOD(redistribute_exact, 4),
                          RDK_METHOD(redistribute_linear, 7),  RDK_METHOD(sample_draft, 8),   RDK_METHOD(verify_multi, 8),
-                         RDK_METHOD(tree_walk, 3),            {nullptr, nullptr, 0, nullptr}};
+                         RDK_METHOD(tree_walk, 3),            RDK_METHOD(topk, 5),           RDK_METHOD(distill, 9),
+                         RDK_METHOD(beam_select, 7),          RDK_METHOD(beam_reorder, 4),   {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rdk_binding", "Per-step calls of the RDK library on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
@@ -420,9 +619,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rdk_binding", "Per-step calls of 
 PyMODINIT_FUNC PyInit__rdk_binding(void)
 {
     PyObject **slot[] = {&g.h, &g.ws, &g.draft_ws, &g.fused_ws, &g.out_ws, &g.draft_ids, &g.accept, &g.alpha, &g.resid_mass,
-                         &g.resid_ids, &g.n_accepted, &g.out_tokens, &g.cand_ids, &g.accepted, &g.token, &g.B, &g.N, &g.gamma};
+                         &g.resid_ids, &g.n_accepted, &g.out_tokens, &g.cand_ids, &g.accepted, &g.token, &g.B, &g.N, &g.gamma,
+                         &g.ids, &g.values, &g.lse, &g.loss, &g.stats, &g.grad, &g.scores, &g.parent, &g.finished};
     const char *name[] = {"_h", "_ws", "_draft_ws", "fused_ws", "ws", "draft_ids", "accept", "alpha", "resid_mass",
-                          "resid_ids", "n_accepted", "out_tokens", "cand_ids", "accepted", "token", "B", "N", "gamma"};
+                          "resid_ids", "n_accepted", "out_tokens", "cand_ids", "accepted", "token", "B", "N", "gamma",
+                          "ids", "values", "lse", "loss", "stats", "grad", "scores", "parent", "finished"};
     for (size_t i = 0; i < sizeof(slot) / sizeof(slot[0]); ++i) {
         *slot[i] = PyUnicode_InternFromString(name[i]);
         if (!*slot[i]) return nullptr;

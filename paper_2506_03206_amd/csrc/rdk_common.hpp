@@ -205,6 +205,27 @@ rdk_status_t launch_verify_multi(const rdk_multi_desc_t &d, RowInput p, const fl
 rdk_status_t launch_tree_walk(int32_t S, int32_t nodes, int32_t C, const int32_t *child_node, const int32_t *accepted,
                               const int32_t *token, int32_t *n_accepted, int32_t *out_tokens, hipStream_t st);
 
+// rdk_topk.hip
+int select_max_entries();
+size_t topk_workspace_bytes(const rdk_topk_desc_t &d, rdk_input_kind_t kind);
+rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, float *values, float *lse, void *ws, hipStream_t st);
+size_t beam_select_workspace_bytes(const rdk_beam_desc_t &d, rdk_input_kind_t kind);
+rdk_status_t launch_beam_select(const rdk_beam_desc_t &d, RowInput x, const float *scores, const uint8_t *finished, float *scores_out,
+                                int32_t *parent, int32_t *token, uint8_t *finished_out, void *ws, hipStream_t st);
+
+// rdk_reorder.hip
+int reorder_max_beams();
+rdk_status_t launch_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *parent, const rdk_state_t *states, int32_t count, hipStream_t st);
+
+// rdk_distill.hip  (h: the drafter's vocabulary, or NULL; dz: NULL for the loss alone; stats may be NULL with dz)
+int distill_max_entries();
+size_t distill_workspace_bytes(const rdk_distill_desc_t &d, rdk_input_kind_t kind);
+rdk_status_t launch_distill_loss(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
+                                 const float *teacher_lse, const float *weight, float *loss, float *stats, void *dz, int64_t ldd, void *ws,
+                                 hipStream_t st);
+rdk_status_t launch_distill_grad(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
+                                 const float *stats, const float *weight, void *dz, int64_t ldd, hipStream_t st);
+
 // rdk_verify.hip
 // What a call cannot do without, and what it asks for: with room for the records of the per-sequence scan the scan runs inside
 // the finish, with less it is a launch of its own.

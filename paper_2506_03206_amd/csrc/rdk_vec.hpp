@@ -1,0 +1,100 @@
+// Sixteen bytes of a row at a time: eight bf16 or four fp32 values, at any multiple of the element's size.
+#pragma once
+#include "rdk_device.hpp"
+
+namespace rdk {
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+
+template <int KIND>
+struct Vec {
+    static constexpr int kSize = KIND == RDK_LOGIT_BF16 ? 2 : 4;
+    static constexpr int kLen = 16 / kSize;   // elements
+    // what stands for "no element": -inf for logits, 0 for weights
+    static constexpr unsigned kFill = KIND == RDK_LOGIT_BF16 ? 0xFF80u : KIND == RDK_LOGIT_F32 ? 0xFF800000u : 0u;
+    static constexpr unsigned kFillWord = KIND == RDK_LOGIT_BF16 ? 0xFF80FF80u : kFill;
+
+    static __device__ __forceinline__ u32x4 fill() { return u32x4{kFillWord, kFillWord, kFillWord, kFillWord}; }
+
+    static __device__ __forceinline__ void to(const u32x4 r, float (&v)[kLen])
+    {
+        if constexpr (KIND == RDK_LOGIT_BF16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(r[i] << 16);
+                v[2 * i + 1] = __uint_as_float(r[i] & 0xFFFF0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+        }
+    }
+
+    static __device__ __forceinline__ unsigned one(const void *row, int64_t i)
+    {
+        if constexpr (KIND == RDK_LOGIT_BF16) return ((const uint16_t *)row)[i];
+        return ((const unsigned *)row)[i];
+    }
+
+    // elements i .. i + kLen - 1 of a row that ends at `end`: those behind it are fill
+    static __device__ __forceinline__ u32x4 load(const void *row, int64_t i, int64_t end)
+    {
+        if (i + kLen <= end) return *(const u32x4_any *)((const char *)row + i * kSize);
+        u32x4 r = fill();
+#pragma unroll
+        for (int e = 0; e < kLen - 1; ++e)   // the vector is not whole
+            if (i + e < end) set(r, e, one(row, i + e));
+        return r;
+    }
+
+    // element e (a constant after unrolling) of a vector
+    static __device__ __forceinline__ void set(u32x4 &r, int e, unsigned bits)
+    {
+        if constexpr (KIND == RDK_LOGIT_BF16)
+            r[e / 2] = e % 2 ? (r[e / 2] & 0xFFFFu) | (bits << 16) : (r[e / 2] & 0xFFFF0000u) | bits;
+        else
+            r[e] = bits;
+    }
+
+    // results in the row's own type, to the nearest, ties to even
+    static __device__ __forceinline__ u32x4 from(const float (&v)[kLen])
+    {
+        u32x4 r;
+        if constexpr (KIND == RDK_LOGIT_BF16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = (unsigned)round_bf16(v[2 * i]) | ((unsigned)round_bf16(v[2 * i + 1]) << 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(v[i]);
+        }
+        return r;
+    }
+
+    static __device__ __forceinline__ uint16_t round_bf16(float x)
+    {
+        return __builtin_bit_cast(uint16_t, (__bf16)x);   // one conversion instruction on gfx950
+    }
+
+    static __device__ __forceinline__ void store(void *row, int64_t i, int64_t end, const u32x4 r)
+    {
+        if (i + kLen <= end) {
+            *(u32x4_any *)((char *)row + i * kSize) = r;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < kLen - 1; ++e)
+            if (i + e < end) {
+                if constexpr (KIND == RDK_LOGIT_BF16) ((uint16_t *)row)[i + e] = (uint16_t)(r[e / 2] >> (e % 2 * 16));
+                else ((unsigned *)row)[i + e] = r[e];
+            }
+    }
+
+    static __device__ __forceinline__ void store1(void *row, int64_t i, float x)
+    {
+        if constexpr (KIND == RDK_LOGIT_BF16) ((uint16_t *)row)[i] = round_bf16(x);
+        else ((float *)row)[i] = x;
+    }
+};
+
+}  // namespace rdk

@@ -27,6 +27,8 @@ EXPORTS = [
     "rdk_timing_select", "rdk_timing_read", "rdk_redistribute_verify_workspace_bytes", "rdk_redistribute_verify",
     "rdk_sample_draft_workspace_bytes", "rdk_sample_draft", "rdk_features_from_scores",
     "rdk_verify_multi_workspace_bytes", "rdk_verify_multi", "rdk_tree_walk", "rdk_verify_sample_static",
+    "rdk_topk_workspace_bytes", "rdk_topk", "rdk_distill_workspace_bytes", "rdk_distill_loss", "rdk_distill_grad",
+    "rdk_distill_loss_grad", "rdk_beam_select_workspace_bytes", "rdk_beam_select", "rdk_beam_reorder",
 ]
 
 
@@ -45,6 +47,24 @@ class VerifyDesc(ctypes.Structure):
 class MultiDesc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("C", ctypes.c_int32), ("seed", ctypes.c_uint64),
                 ("offset", ctypes.c_uint64), ("sample_candidates", ctypes.c_int)]
+
+
+class TopkDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+class DistillDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("n", ctypes.c_int32), ("K", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+class BeamDesc(ctypes.Structure):
+    _fields_ = [("G", ctypes.c_int32), ("W", ctypes.c_int32), ("N", ctypes.c_int32), ("K", ctypes.c_int32), ("eos", ctypes.c_int32)]
+
+
+class State(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("src_stride", ctypes.c_int64), ("dst_stride", ctypes.c_int64),
+                ("segments", ctypes.c_int64), ("segment_bytes", ctypes.c_int64), ("src_pitch", ctypes.c_int64),
+                ("dst_pitch", ctypes.c_int64)]
 
 
 class RdkError(RuntimeError):
@@ -109,6 +129,16 @@ def lib():
         L.rdk_verify_multi_workspace_bytes.argtypes = [ctypes.POINTER(MultiDesc), ctypes.c_int, psz]
         L.rdk_verify_multi.argtypes = [ctypes.POINTER(MultiDesc), vp, ctypes.c_int, i64, vp, i64, vp, vp, vp, vp, vp, sz, vp]
         L.rdk_tree_walk.argtypes = [i32, i32, i32, vp, vp, vp, vp, vp, vp]
+        kind = ctypes.c_int
+        L.rdk_topk_workspace_bytes.argtypes = [ctypes.POINTER(TopkDesc), kind, psz]
+        L.rdk_topk.argtypes = [ctypes.POINTER(TopkDesc), vp, kind, i64, vp, vp, vp, vp, sz, vp]
+        L.rdk_distill_workspace_bytes.argtypes = [ctypes.POINTER(DistillDesc), kind, psz]
+        L.rdk_distill_loss.argtypes = [ctypes.POINTER(DistillDesc), vp, vp, kind, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.rdk_distill_grad.argtypes = [ctypes.POINTER(DistillDesc), vp, vp, kind, i64, vp, vp, vp, vp, vp, i64, vp]
+        L.rdk_distill_loss_grad.argtypes = [ctypes.POINTER(DistillDesc), vp, vp, kind, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.rdk_beam_select_workspace_bytes.argtypes = [ctypes.POINTER(BeamDesc), kind, psz]
+        L.rdk_beam_select.argtypes = [ctypes.POINTER(BeamDesc), vp, kind, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.rdk_beam_reorder.argtypes = [i32, i32, i32, vp, ctypes.POINTER(State), i32, vp]
         L.rdk_timing_select.argtypes = [ctypes.c_char_p]
         L.rdk_timing_read.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]
         for name in EXPORTS:
@@ -336,6 +366,108 @@ def rdk_tree_walk(child_node, accepted, token):
     status, n_acc, out = (_native or native()).tree_walk(child_node, accepted, token)
     _check(status, "rdk_tree_walk")
     return n_acc, out
+
+
+class TopkOutputs:
+    """Outputs (and scratch) of rdk_topk for a fixed batch shape: ids [B,k] int32, values [B,k] fp32, lse [B] fp32."""
+
+    def __init__(self, B, N, k, device):
+        self.B, self.N, self.k = B, N, k
+        self.ids = torch.empty((B, k), dtype=torch.int32, device=device)
+        self.values = torch.empty((B, k), dtype=torch.float32, device=device)
+        self.lse = torch.empty(B, dtype=torch.float32, device=device)
+        self.ws = None
+
+
+def rdk_topk(x, k, x_kind="logit", temperature=1.0, outputs=None):
+    """The k largest entries of every row of x [B,N], descending (equal ones by id; -1 where fewer are unmasked), and the
+    logarithm of the row's normaliser at a temperature."""
+    o = outputs or TopkOutputs(x.shape[0], x.shape[1], k, x.device)
+    _check((_native or native()).topk(x, k, x_kind, temperature, o), "rdk_topk")
+    return o
+
+
+class DistillOutputs:
+    """Outputs (and scratch) of the rdk_distill calls for a fixed batch shape: loss [B] fp32, stats [B,4] fp32 (what the backward
+    call reads), grad [B,n] of z's type (grad=False: the loss alone; a tensor: the gradient goes there, z itself included)."""
+
+    def __init__(self, B, n, dtype, device, grad=True):
+        self.loss = torch.empty(B, dtype=torch.float32, device=device)
+        self.stats = torch.empty((B, 4), dtype=torch.float32, device=device)
+        self.grad = grad if isinstance(grad, torch.Tensor) else torch.empty((B, n), dtype=dtype, device=device) if grad else None
+        self.ws = None
+
+
+def rdk_distill_loss(kernel, z, top_ids, top_logits, teacher_lse=None, temperature=1.0, weight=None, outputs=None):
+    """Loss of the drafter's logits z [B,n] against the teacher's top logits.  kernel: the drafter's vocabulary (None: top_ids are
+    slots).  teacher_lse None: the teacher renormalised over the entries that the drafter holds; else its remainder counts too."""
+    o = outputs or DistillOutputs(z.shape[0], z.shape[1], z.dtype, z.device, grad=False)
+    _check((_native or native()).distill(kernel, z, top_ids, top_logits, teacher_lse, temperature, weight, o, 0), "rdk_distill_loss")
+    return o
+
+
+def rdk_distill_grad(kernel, z, top_ids, top_logits, outputs, temperature=1.0, weight=None):
+    """Gradient of weight[b] * loss into outputs.grad, from the statistics that rdk_distill_loss left in outputs."""
+    _check((_native or native()).distill(kernel, z, top_ids, top_logits, None, temperature, weight, outputs, 2), "rdk_distill_grad")
+    return outputs
+
+
+def rdk_distill_loss_grad(kernel, z, top_ids, top_logits, teacher_lse=None, temperature=1.0, weight=None, outputs=None):
+    """rdk_distill_loss and rdk_distill_grad in one call, for weights known beforehand."""
+    o = outputs or DistillOutputs(z.shape[0], z.shape[1], z.dtype, z.device)
+    _check((_native or native()).distill(kernel, z, top_ids, top_logits, teacher_lse, temperature, weight, o, 1), "rdk_distill_loss_grad")
+    return o
+
+
+class _Distill(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, z, kernel, top_ids, top_logits, teacher_lse, temperature):
+        o = rdk_distill_loss(kernel, z, top_ids, top_logits, teacher_lse, temperature)
+        ctx.save_for_backward(z, top_ids, top_logits, o.stats)
+        ctx.kernel, ctx.temperature = kernel, temperature
+        return o.loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, above):
+        z, top_ids, top_logits, stats = ctx.saved_tensors
+        o = DistillOutputs(z.shape[0], z.shape[1], z.dtype, z.device)
+        o.stats = stats
+        rdk_distill_grad(ctx.kernel, z, top_ids, top_logits, o, ctx.temperature, above.contiguous())
+        return o.grad, None, None, None, None, None
+
+
+def rdk_distill(kernel, z, top_ids, top_logits, teacher_lse=None, temperature=1.0):
+    """rdk_distill_loss under torch's automatic differentiation: the losses [B], whose gradient reaches z."""
+    return _Distill.apply(z, kernel, top_ids, top_logits, teacher_lse, temperature)
+
+
+class BeamOutputs:
+    """Outputs (and scratch) of rdk_beam_select: scores [G,K] fp32, parent, token [G,K] int32, finished [G,K] uint8."""
+
+    def __init__(self, G, W, N, K, device):
+        self.scores = torch.empty((G, K), dtype=torch.float32, device=device)
+        self.parent = torch.empty((G, K), dtype=torch.int32, device=device)
+        self.token = torch.empty((G, K), dtype=torch.int32, device=device)
+        self.finished = torch.empty((G, K), dtype=torch.uint8, device=device)
+        self.ws = None
+
+
+def rdk_beam_select(x, scores, K=None, x_kind="logit", finished=None, eos=-1, outputs=None):
+    """The K (default W) best continuations of every request over its W beams and the vocabulary: x [G*W,N] next-token rows,
+    scores [G,W] summed log-probabilities, finished [G,W] uint8."""
+    G, W = scores.shape
+    K = W if K is None else K
+    o = outputs or BeamOutputs(G, W, x.shape[1], K, x.device)
+    _check((_native or native()).beam_select(x, scores, K, x_kind, finished, eos, o), "rdk_beam_select")
+    return o
+
+
+def rdk_beam_reorder(states, parent, W=None, out=None):
+    """Row i of request g of every state becomes row parent[g, i]: in place, or into `out` ([G*K, ...] each).  states: tensors
+    [G*W, ...] whose rows have at most one gap (a cache of which a part is filled).  Returns the reordered states."""
+    _check((_native or native()).beam_reorder(states, parent, parent.shape[1] if W is None else W, out), "rdk_beam_reorder")
+    return list(states) if out is None else list(out)
 
 
 def rdk_philox_words(seed, offset, count, device="cuda"):
