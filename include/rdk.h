@@ -330,7 +330,7 @@ rdk_status_t rdk_tree_walk(int32_t S, int32_t nodes, int32_t C, const int32_t *c
  * ids and values are [B, k] without gaps.  1 <= k <= min(N, 128), temperature > 0 and finite.  The ids and values are exact, whatever the
  * input; sums run in fp32.  Rows that crowd out the fast way (thousands of entries that tie with the k-th) take a slower one.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, N, k, ldx, temperature), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x or the workspace),
- * RDK_ERR_UNSUPPORTED (k above 128; weights with a temperature other than 1), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ * RDK_ERR_UNSUPPORTED (k above 128, N above 2^30; weights with a temperature other than 1), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */
 typedef struct {
     int32_t B, N, k;            /* rows, ids, entries kept per row */
@@ -388,7 +388,7 @@ rdk_status_t rdk_distill_loss_grad(const rdk_distill_desc_t *desc, const rdk_ker
  * ascending id): scores_out, parent (beam 0 .. W-1), token, finished_out (the beam was finished, or token == eos), all [G, K]; score -inf,
  * parent -1, token -1, finished 0 where there are fewer.  NaN and +inf in a live row make its scores NaN, which rank first.
  * finished and finished_out may be NULL; eos = -1: no id ends a beam (finished must be NULL then).  Outputs must not overlap the inputs.
- * 1 <= W <= 64, 1 <= K <= 128, W N < 2^31.
+ * 1 <= W <= 64, 1 <= K <= 128, N <= 2^30, W N < 2^31, G W < 2^31.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (G, W, N, K, ldx, eos, an output that overlaps its input), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x, workspace),
  * RDK_ERR_UNSUPPORTED (limits), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */

@@ -643,7 +643,7 @@ static rdk_status_t check_topk(const rdk_topk_desc_t *d, rdk_input_kind_t kind)
     if (!d) return RDK_ERR_NULL;
     if (!kind_ok(kind)) return RDK_ERR_DTYPE;
     if (d->B < 1 || d->N < 1 || d->k < 1 || d->k > d->N || !temperature_ok(d->temperature)) return RDK_ERR_SHAPE;
-    if (d->k > select_max_entries() || (kind == RDK_PROB_F32 && d->temperature != 1.f)) return RDK_ERR_UNSUPPORTED;
+    if (d->k > select_max_entries() || d->N > select_max_ids() || (kind == RDK_PROB_F32 && d->temperature != 1.f)) return RDK_ERR_UNSUPPORTED;
     return RDK_OK;
 }
 
@@ -759,7 +759,7 @@ static rdk_status_t check_beam(const rdk_beam_desc_t *d, rdk_input_kind_t kind)
     if (!d) return RDK_ERR_NULL;
     if (!kind_ok(kind)) return RDK_ERR_DTYPE;
     if (d->G < 1 || d->W < 1 || d->N < 1 || d->K < 1 || d->eos < -1 || d->eos >= d->N) return RDK_ERR_SHAPE;
-    if (d->W > reorder_max_beams() || d->K > select_max_entries()) return RDK_ERR_UNSUPPORTED;
+    if (d->W > reorder_max_beams() || d->K > select_max_entries() || d->N > select_max_ids()) return RDK_ERR_UNSUPPORTED;
     if ((int64_t)d->W * d->N > INT32_MAX || (int64_t)d->G * d->W > INT32_MAX) return RDK_ERR_UNSUPPORTED;
     return RDK_OK;
 }

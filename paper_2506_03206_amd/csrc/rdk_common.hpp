@@ -207,6 +207,7 @@ rdk_status_t launch_tree_walk(int32_t S, int32_t nodes, int32_t C, const int32_t
 
 // rdk_topk.hip
 int select_max_entries();
+int select_max_ids();
 size_t topk_workspace_bytes(const rdk_topk_desc_t &d, rdk_input_kind_t kind);
 rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, float *values, float *lse, void *ws, hipStream_t st);
 size_t beam_select_workspace_bytes(const rdk_beam_desc_t &d, rdk_input_kind_t kind);
