@@ -26,43 +26,66 @@ struct StateArgs {
     const int32_t *parent;
 };
 
-template <class T>
-__device__ void reorder_unit(const StateArgs &a, const StateArg &s, int64_t g, int64_t u, const int *from)
+// The units of the rows I .. MOST - 1: all are read on the way down, and written on the way back up.  (One variable a row: an array of them is
+// made one wide register tuple, copied at every branch.)
+template <class T, int I, int MOST>
+struct Rows {
+    static __device__ __forceinline__ void move(const char *src, char *dst, int64_t src_stride, int64_t dst_stride, const int *parent, int W, int K,
+                                                bool in_place)
+    {
+        const int p = I < K ? parent[I] : -1;
+        const bool moves = (unsigned)p < (unsigned)W && !(in_place && p == I);   // the same for the workgroup
+        T v{};
+        if (moves) v = __builtin_nontemporal_load((const T *)(src + p * src_stride));
+        Rows<T, I + 1, MOST>::move(src, dst, src_stride, dst_stride, parent, W, K, in_place);
+        if (moves) __builtin_nontemporal_store(v, (T *)(dst + I * dst_stride));
+    }
+};
+template <class T, int MOST>
+struct Rows<T, MOST, MOST> {
+    static __device__ __forceinline__ void move(const char *, char *, int64_t, int64_t, const int *, int, int, bool) {}
+};
+
+// MOST: rows held in registers, K or more.
+template <class T, int MOST>
+__device__ __forceinline__ void reorder_unit(const StateArgs &a, const StateArg &s, int64_t g, int64_t u, const int *parent, bool in_place)
 {
-    const int64_t seg = u / s.per_segment, off = (u - seg * s.per_segment) * (int64_t)sizeof(T);
+    int64_t seg = 0;
+    if (s.units != s.per_segment) seg = (s.units >> 32) == 0 ? (uint32_t)u / (uint32_t)s.per_segment : u / s.per_segment;
+    const int64_t off = (u - seg * s.per_segment) * (int64_t)sizeof(T);
     const char *src = s.src + g * a.W * s.src_stride + seg * s.src_pitch + off;
     char *dst = s.dst + g * a.K * s.dst_stride + seg * s.dst_pitch + off;
-    T v[kMaxBeams];
-#pragma unroll
-    for (int i = 0; i < kMaxBeams; ++i)
-        if (i < a.K && from[i] >= 0) v[i] = *(const T *)(src + from[i] * s.src_stride);
-#pragma unroll
-    for (int i = 0; i < kMaxBeams; ++i)
-        if (i < a.K && from[i] >= 0) *(T *)(dst + i * s.dst_stride) = v[i];
+    Rows<T, 0, MOST>::move(src, dst, s.src_stride, s.dst_stride, parent, a.W, a.K, in_place);
 }
 
-__global__ __launch_bounds__(kReorderThreads) void beam_reorder_kernel(StateArgs a)
+template <int MOST>
+__global__ __launch_bounds__(kReorderThreads, MOST <= 8 ? 8 : MOST <= 16 ? 5 : MOST <= 32 ? 3 : 1) void beam_reorder_kernel(StateArgs a)
 {
-    __shared__ int from[kMaxBeams];
     int n = 0;
     while (n + 1 < a.count && blockIdx.x >= a.s[n + 1].first_block) ++n;
     const StateArg &s = a.s[n];
-    const unsigned b = blockIdx.x - s.first_block;
-    const int64_t g = b / s.blocks, u = (int64_t)(b % s.blocks) * kReorderThreads + threadIdx.x;
-    if ((int)threadIdx.x < a.K) {
-        const int p = a.parent[g * a.K + threadIdx.x];
-        const bool stays = (a.in_place >> n & 1) && p == (int)threadIdx.x;
-        from[threadIdx.x] = p < 0 || p >= a.W || stays ? -1 : p;
-    }
-    __syncthreads();
+    const unsigned b = blockIdx.x - s.first_block, g = b / s.blocks;
+    const int64_t u = (int64_t)(b - g * s.blocks) * kReorderThreads + threadIdx.x;
     if (u >= s.units) return;
+    const int *parent = a.parent + (int64_t)g * a.K;
+    const bool in_place = a.in_place >> n & 1;
     switch (s.unit) {
-        case 16: reorder_unit<u32x4>(a, s, g, u, from); break;
-        case 8: reorder_unit<uint64_t>(a, s, g, u, from); break;
-        case 4: reorder_unit<uint32_t>(a, s, g, u, from); break;
-        case 2: reorder_unit<uint16_t>(a, s, g, u, from); break;
-        default: reorder_unit<uint8_t>(a, s, g, u, from); break;
+        case 16: reorder_unit<u32x4, MOST>(a, s, g, u, parent, in_place); break;
+        case 8: reorder_unit<uint64_t, MOST>(a, s, g, u, parent, in_place); break;
+        case 4: reorder_unit<uint32_t, MOST>(a, s, g, u, parent, in_place); break;
+        case 2: reorder_unit<uint16_t, MOST>(a, s, g, u, parent, in_place); break;
+        default: reorder_unit<uint8_t, MOST>(a, s, g, u, parent, in_place); break;
     }
+}
+
+template <class F>
+void with_rows(int K, const F &f)
+{
+    if (K <= 4) f(std::integral_constant<int, 4>());
+    else if (K <= 8) f(std::integral_constant<int, 8>());
+    else if (K <= 16) f(std::integral_constant<int, 16>());
+    else if (K <= 32) f(std::integral_constant<int, 32>());
+    else f(std::integral_constant<int, 64>());
 }
 
 }  // namespace
@@ -101,7 +124,9 @@ rdk_status_t launch_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t 
             ++done;
         }
         if (!a.count) break;
-        RDK_TIMED_LAUNCH("beam_reorder_kernel", beam_reorder_kernel, dim3((unsigned)blocks), dim3(kReorderThreads), 0, st, a);
+        with_rows(K, [&](auto rows) {
+            RDK_TIMED_LAUNCH("beam_reorder_kernel", (beam_reorder_kernel<decltype(rows)::value>), dim3((unsigned)blocks), dim3(kReorderThreads), 0, st, a);
+        });
         RDK_LAUNCH_CHECK("beam_reorder_kernel");
     }
     return RDK_OK;
