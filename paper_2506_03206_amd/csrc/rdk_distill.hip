@@ -13,6 +13,7 @@ namespace {
 constexpr int kMaxEntries = 128;          // teacher entries of a position: two to a lane of one wavefront
 constexpr int kPerLane = kMaxEntries / kWave;
 constexpr int kDistillThreads = 256;
+constexpr int kGradVecs = 8;             // 16-byte vectors of a thread in the backward call
 constexpr int kPartSlots = 65536;         // at most, of a row in one workgroup: the bitmap of A
 constexpr float kLog2e = 1.44269504088896341f;
 
@@ -21,7 +22,7 @@ struct DistillArgs {
     int64_t ldz;
     const int32_t *slot_of;   // target id -> slot, or NULL: ids are slots
     int ids;                  // ids below this have an entry there
-    int n, K, parts, part_slots;
+    int n, K, parts, part_slots, grad_parts;
     float inv_t;
     const int32_t *top_ids;
     const float *top_logits, *teacher_lse, *weight;
@@ -126,63 +127,98 @@ __global__ __launch_bounds__(kDistillThreads) void distill_part_kernel(DistillAr
     }
 }
 
-// What the row's loss and gradient follow from, by one wavefront: `st` the statistics of the row (REST: of its slots outside A), zt its logits at
-// the entries (-inf for those that do not count).  Returns the row's loss without its weight; stats in every lane.
-template <bool REST>
-__device__ __forceinline__ float row_loss(const DistillArgs &a, int64_t row, const Entries &t, const float (&zt)[kPerLane], SoftStat st, float4 *stats)
-{
-    const float c = a.inv_t * kLog2e;
-    float m = st.m;
-    int held = 0;
-    float vmax = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < kPerLane; ++j) {
-        if (REST) m = fmaxf(m, zt[j]);
-        held += __popcll(__ballot(t.slot[j] >= 0));
-        if (t.slot[j] >= 0) vmax = fmaxf(vmax, t.v[j]);
-    }
-    if (REST) m = wave_max(m);
-    vmax = weight_reference(wave_max(vmax));
-    const float ref = weight_reference(m);
-    float rest = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c), sum_a = 0.f, sum_t = 0.f;
-#pragma unroll
-    for (int j = 0; j < kPerLane; ++j)
-        if (t.slot[j] >= 0) {
-            if (REST) sum_a += soft_term(zt[j], ref, c);
-            sum_t += expf((t.v[j] - vmax) * a.inv_t);
-        }
-    const float total = REST ? rest + wave_sum(sum_a) : rest;
-    sum_t = wave_sum(sum_t);
-    const bool remainder = REST && held < a.n;
-    const float log_total = logf(total);
-    // log t = v / T - constant
-    const float constant = remainder ? a.teacher_lse[row] : vmax * a.inv_t + logf(sum_t);
-    float loss = 0.f, mass = 0.f;
-#pragma unroll
-    for (int j = 0; j < kPerLane; ++j)
-        if (t.slot[j] >= 0) {
-            const float log_t = t.v[j] * a.inv_t - constant, p = expf(log_t);
-            const float log_s = total == 0.f ? -INFINITY : (zt[j] - ref) * a.inv_t - log_total;
-            mass += p;
-            if (p != 0.f) loss += p * (log_t - log_s);
-        }
-    loss = wave_sum(loss);
-    float outside = held ? 1.f : 0.f;
-    if (remainder) {
-        const float r = fmaxf(0.f, 1.f - wave_sum(mass));
-        if (r > 0.f) loss += r * (logf(r) - (rest == 0.f ? -INFINITY : logf(rest) - log_total));
-        outside = rest == 0.f ? 1.f : 1.f - r * total / rest;
-    }
-    *stats = make_float4(ref, total == 0.f ? 0.f : 1.f / total, outside, constant);
-    return loss;
-}
-
 // The row's logits at the entries.
 template <int KIND>
 __device__ __forceinline__ void entry_logits(const void *zr, const Entries &t, float (&zt)[kPerLane])
 {
 #pragma unroll
     for (int j = 0; j < kPerLane; ++j) zt[j] = t.slot[j] >= 0 ? load1<KIND>(zr, t.slot[j]) : -INFINITY;
+}
+
+// What the teacher's entries of a row amount to, by one wavefront.  The few sums and logarithms of a row that its loss is a small difference of are
+// held in 64 bits.
+struct Teacher {
+    double log_t[kPerLane];    // log t of the lane's entries
+    float p[kPerLane];         // t, 0 for entries that do not count
+    double constant;           // log t = v / T - constant
+    int held;
+    bool remainder;            // the mass outside A counts
+    double r;                  // the teacher's
+};
+template <bool REST>
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, int64_t row, const Entries &t)
+{
+    Teacher o;
+    o.held = 0;
+    float vmax = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) {
+        o.held += __popcll(__ballot(t.slot[j] >= 0));
+        if (t.slot[j] >= 0) vmax = fmaxf(vmax, t.v[j]);
+    }
+    o.remainder = REST && o.held < a.n;
+    if (o.remainder) {
+        o.constant = a.teacher_lse[row];
+    } else {
+        vmax = weight_reference(wave_max(vmax));
+        double sum = 0.;
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j)
+            if (t.slot[j] >= 0) sum += expf((t.v[j] - vmax) * a.inv_t);
+        o.constant = (double)vmax * a.inv_t + log(wave_sum(sum));
+    }
+    double mass = 0.;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) {
+        o.log_t[j] = (double)t.v[j] * a.inv_t - o.constant;
+        o.p[j] = t.slot[j] >= 0 ? expf((float)o.log_t[j]) : 0.f;
+        mass += o.p[j];
+    }
+    mass = wave_sum(mass);
+    o.r = o.remainder ? fmax(0., 1. - mass) : 0.;
+    if (mass != mass) o.r = mass;
+    return o;
+}
+
+// exp((z - reference) / T) summed over the entries, and their largest logit.
+__device__ __forceinline__ SoftStat entry_stat(const Entries &t, const float (&zt)[kPerLane], float c)
+{
+    SoftStat st;
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) m = fmaxf(m, zt[j]);
+    st.m = wave_max(m);
+    const float ref = weight_reference(st.m);
+    st.s = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j)
+        if (t.slot[j] >= 0) st.s += soft_term(zt[j], ref, c);
+    st.s = wave_sum(st.s);
+    return st;
+}
+
+// Factor of s outside A in the gradient.
+__device__ __forceinline__ float outside_of(bool remainder, float r, int held, float total, float rest)
+{
+    if (!remainder) return held ? 1.f : 0.f;
+    return rest == 0.f ? 1.f : 1.f - r * total / rest;
+}
+
+// The row's loss, by one wavefront: sums relative to ref, of the whole row and of its slots outside A.
+__device__ __forceinline__ double loss_of(const DistillArgs &a, const Entries &t, const float (&zt)[kPerLane], const Teacher &o, float ref, float total,
+                                          float rest)
+{
+    const double log_total = log((double)total);
+    double loss = 0.;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j)
+        if (o.p[j] != 0.f) {
+            const double log_s = total == 0.f ? -INFINITY : (double)(zt[j] - ref) * a.inv_t - log_total;
+            loss += o.p[j] * (o.log_t[j] - log_s);
+        }
+    loss = wave_sum(loss);
+    if (o.remainder && o.r != 0.) loss += rest == 0.f ? INFINITY : o.r * log(o.r * total / rest);
+    return loss;
 }
 
 template <int KIND, bool REST>
@@ -201,56 +237,208 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
     float zt[kPerLane];
     entry_logits<KIND>(row_ptr<KIND>(a.z, a.ldz, row), t, zt);
     const float c = a.inv_t * kLog2e;
+    const Teacher o = teacher_of<REST>(a, row, t);
     SoftStat st{-INFINITY, 0.f};
     for (int p = lane_id(); p < a.parts; p += kWave) st = merge_at(st, a.part[row * a.parts + p], c);
     st = wave_merge_at(st, c);
-    float4 stats;
-    const float loss = row_loss<REST>(a, row, t, zt, st, &stats);
+    const SoftStat at = REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f}, all = merge_at(st, at, c);
+    const float ref = weight_reference(all.m), rest = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
+    const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
     if (threadIdx.x == 0) {
-        a.loss[row] = w * loss;
-        a.stats[row] = stats;
+        a.loss[row] = (float)(w * loss);
+        a.stats[row] = make_float4(ref, all.s == 0.f ? 0.f : 1.f / all.s, outside_of(o.remainder, (float)o.r, o.held, all.s, rest), (float)o.constant);
     }
 }
 
-// dz of a part of a row.
+// A whole row in the registers of one workgroup: its logits are read once, for the loss and the gradient.  The first wavefront follows the
+// teacher's entries meanwhile (ids to slots to logits, a chain of three reads) and adds up the loss while the others write the gradient;
+// the entries' own gradient then goes over what stands at their slots.
+template <int KIND, int THREADS, int VECS, bool REST, bool GRAD>
+__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
+{
+    typedef Vec<KIND> V;
+    constexpr int kWaves = THREADS / kWave;
+    __shared__ __attribute__((aligned(16))) uint8_t marked[REST ? THREADS * VECS : 16];   // a bit per slot of A, by the thread that holds it
+    __shared__ SoftStat waves[kWaves], entries;
+    __shared__ float remaining;
+    __shared__ int held;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x;
+    const void *zr = row_ptr<KIND>(a.z, a.ldz, row);
+    void *dr = GRAD ? const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row)) : nullptr;
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        if (GRAD) {
+            const u32x4 zero{0, 0, 0, 0};
+            for (int i = tid * V::kLen; i < a.n; i += THREADS * V::kLen) V::store(dr, i, a.n, zero);
+        }
+        if (tid == 0) {
+            a.loss[row] = 0.f;
+            if (a.stats) a.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        return;
+    }
+    const float c = a.inv_t * kLog2e;
+    Entries t;
+    float zt[kPerLane];
+    Teacher o;
+    u32x4 raw[VECS];
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+        const int i = (j * THREADS + tid) * V::kLen;
+        raw[j] = i < a.n ? V::load(zr, i, a.n) : V::fill();
+    }
+    if (REST) {
+        for (int i = tid; i < THREADS * VECS / 4; i += THREADS) ((unsigned *)marked)[i] = 0;
+        __syncthreads();
+    }
+    if (tid < kWave) {
+        t = row_entries(a, row);
+        entry_logits<KIND>(zr, t, zt);
+        if (REST) {
+#pragma unroll
+            for (int j = 0; j < kPerLane; ++j)
+                if (t.slot[j] >= 0) {
+                    const int q = t.slot[j] / V::kLen, at = q % THREADS * VECS + q / THREADS;
+                    atomicOr((unsigned *)marked + at / 4, 1u << (at % 4 * 8 + t.slot[j] % V::kLen));
+                }
+        }
+        o = teacher_of<REST>(a, row, t);
+        const SoftStat at = REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f};
+        if (tid == 0) {
+            entries = at;
+            remaining = (float)o.r;
+            held = o.held;
+        }
+    }
+    if (REST) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            const unsigned bits = marked[tid * VECS + j];
+            if (bits) {
+#pragma unroll
+                for (int e = 0; e < V::kLen; ++e)
+                    if (bits >> e & 1u) V::set(raw[j], e, V::kFill);
+            }
+        }
+    }
+    float v[V::kLen];
+    SoftStat st{-INFINITY, 0.f};
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+        V::to(raw[j], v);
+#pragma unroll
+        for (int e = 0; e < V::kLen; ++e) st.m = fmaxf(st.m, v[e]);
+    }
+    {
+        const float ref = weight_reference(st.m);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            V::again(raw[j]);
+            V::to(raw[j], v);
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < V::kLen; ++e) part += soft_term(v[e], ref, c);
+            st.s += part;
+        }
+    }
+    st = wave_merge_at(st, c);
+    if (lane_id() == 0) waves[tid / kWave] = st;
+    __syncthreads();   // (the logits at the entries have been read too: dz may be z)
+    st = waves[0];
+    for (int k = 1; k < kWaves; ++k) st.m = fmaxf(st.m, waves[k].m);
+    SoftStat all{st.m, 0.f};
+    if (REST) all.m = fmaxf(all.m, entries.m);
+    const float ref = weight_reference(all.m);
+    float rest = 0.f;
+    for (int k = 0; k < kWaves; ++k) rest += waves[k].s == 0.f ? 0.f : waves[k].s * soft_term(weight_reference(waves[k].m), ref, c);
+    all.s = rest;
+    if (REST) all.s += entries.s == 0.f ? 0.f : entries.s * soft_term(weight_reference(entries.m), ref, c);
+    const float inv = all.s == 0.f ? 0.f : 1.f / all.s;
+    const float outside = outside_of(REST && held < a.n, remaining, held, all.s, rest), wt = w * a.inv_t;
+    if (tid < kWave) {
+        const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
+        if (tid == 0) {
+            a.loss[row] = (float)(w * loss);
+            if (a.stats) a.stats[row] = make_float4(ref, inv, outside, (float)o.constant);
+        }
+    }
+    if (!GRAD) return;
+    const float scale = wt * inv * outside;
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+        const int i = (j * THREADS + tid) * V::kLen;
+        if (i < a.n) {
+            V::again(raw[j]);
+            V::to(raw[j], v);
+#pragma unroll
+            for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], ref, c);
+            V::store(dr, i, a.n, V::from(v));
+        }
+    }
+    __syncthreads();
+    if (tid < kWave) {
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j)
+            if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - o.p[j]));
+    }
+}
+
+// dz of a part of a row, whose logits lie in the registers.
 template <int KIND>
 __global__ __launch_bounds__(kDistillThreads) void distill_grad_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
-    const int64_t row = blockIdx.x / a.parts;
-    const int part = blockIdx.x % a.parts, begin = part * a.part_slots, end = min(a.n, begin + a.part_slots);
+    constexpr int kSlots = kDistillThreads * kGradVecs * V::kLen;
+    const int64_t row = blockIdx.x / a.grad_parts;
+    const int begin = (int)(blockIdx.x % a.grad_parts) * kSlots, end = min(a.n, begin + kSlots), tid = threadIdx.x;
     const void *zr = row_ptr<KIND>(a.z, a.ldz, row);
     void *dr = const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row));
     const float w = a.weight ? a.weight[row] : 1.f;
     if (w == 0.f) {
         const u32x4 zero{0, 0, 0, 0};
-        for (int i = begin + (int)threadIdx.x * V::kLen; i < end; i += kDistillThreads * V::kLen) V::store(dr, i, end, zero);
+        for (int i = begin + tid * V::kLen; i < end; i += kDistillThreads * V::kLen) V::store(dr, i, end, zero);
         return;
+    }
+    u32x4 raw[kGradVecs];
+#pragma unroll
+    for (int j = 0; j < kGradVecs; ++j) {
+        const int i = begin + (j * kDistillThreads + tid) * V::kLen;
+        raw[j] = i < end ? V::load(zr, i, end) : V::fill();
     }
     const float4 stats = a.stats[row];
     const float c = a.inv_t * kLog2e, wt = w * a.inv_t, scale = stats.y * stats.z * wt;
     Entries t;
     float zt[kPerLane];
-    if (threadIdx.x < kWave) {
+    if (tid < kWave) {
         t = row_entries(a, row);
         entry_logits<KIND>(zr, t, zt);
     }
     __syncthreads();   // the logits at the entries have been read before anything is written: dz may be z
-    for (int i = begin + (int)threadIdx.x * V::kLen; i < end; i += kDistillThreads * V::kLen) {
-        float v[V::kLen];
-        V::to(V::load(zr, i, end), v);
 #pragma unroll
-        for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
-        V::store(dr, i, end, V::from(v));
+    for (int j = 0; j < kGradVecs; ++j) {
+        const int i = begin + (j * kDistillThreads + tid) * V::kLen;
+        if (i < end) {
+            float v[V::kLen];
+            V::to(raw[j], v);
+#pragma unroll
+            for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
+            V::store(dr, i, end, V::from(v));
+        }
     }
     __syncthreads();   // the entries' own gradient goes over what stands at their slots
-    if (threadIdx.x < kWave) {
+    if (tid < kWave) {
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
             if (t.slot[j] >= begin && t.slot[j] < end)
                 V::store1(dr, t.slot[j], wt * (soft_term(zt[j], stats.x, c) * stats.y - expf(t.v[j] * a.inv_t - stats.w)));
     }
 }
+
+// The longest row that a workgroup holds.
+template <int KIND>
+constexpr int kRowSlots = 1024 * 16 * Vec<KIND>::kLen;
 
 template <class F>
 void with_logits(rdk_input_kind_t kind, const F &f)
@@ -278,13 +466,44 @@ DistillArgs arguments(const rdk_distill_desc_t &d, const KernelHandle *h, RowInp
     return a;
 }
 
-rdk_status_t launch_grad(const DistillArgs &a, rdk_input_kind_t kind, int32_t B, hipStream_t st)
+template <int KIND>
+rdk_status_t launch_grad(DistillArgs a, int32_t B, hipStream_t st)
 {
-    with_logits(kind, [&](auto k) {
-        RDK_TIMED_LAUNCH("distill_grad_kernel", (distill_grad_kernel<decltype(k)::value>), dim3((unsigned)B * a.parts), dim3(kDistillThreads), 0, st, a);
-    });
+    constexpr int kSlots = kDistillThreads * kGradVecs * Vec<KIND>::kLen;
+    a.grad_parts = (a.n + kSlots - 1) / kSlots;
+    RDK_TIMED_LAUNCH("distill_grad_kernel", (distill_grad_kernel<KIND>), dim3((unsigned)B * a.grad_parts), dim3(kDistillThreads), 0, st, a);
     RDK_LAUNCH_CHECK("distill_grad_kernel");
     return RDK_OK;
+}
+
+template <int KIND, bool REST>
+rdk_status_t launch_split(const DistillArgs &a, int32_t B, hipStream_t st)
+{
+    RDK_TIMED_LAUNCH("distill_part_kernel", (distill_part_kernel<KIND, REST>), dim3((unsigned)B * a.parts), dim3(kDistillThreads), 0, st, a);
+    RDK_TIMED_LAUNCH("distill_finish_kernel", (distill_finish_kernel<KIND, REST>), dim3((unsigned)B), dim3(kWave), 0, st, a);
+    RDK_LAUNCH_CHECK("distill_finish_kernel");
+    return a.dz ? launch_grad<KIND>(a, B, st) : RDK_OK;
+}
+
+template <int KIND, int THREADS, int VECS, bool REST>
+rdk_status_t launch_row(const DistillArgs &a, int32_t B, hipStream_t st)
+{
+    if (a.dz) RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, true>), dim3((unsigned)B), dim3(THREADS), 0, st, a);
+    else RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, false>), dim3((unsigned)B), dim3(THREADS), 0, st, a);
+    RDK_LAUNCH_CHECK("distill_row_kernel");
+    return RDK_OK;
+}
+
+template <int KIND, bool REST>
+rdk_status_t launch_loss(const DistillArgs &a, int32_t B, hipStream_t st)
+{
+    constexpr int kLen = Vec<KIND>::kLen;
+    if (a.n <= 256 * 2 * kLen) return launch_row<KIND, 256, 2, REST>(a, B, st);
+    if (a.n <= 256 * 8 * kLen) return launch_row<KIND, 256, 8, REST>(a, B, st);
+    if (a.n <= 512 * 8 * kLen) return launch_row<KIND, 512, 8, REST>(a, B, st);
+    if (a.n <= 1024 * 8 * kLen) return launch_row<KIND, 1024, 8, REST>(a, B, st);
+    if (a.n <= kRowSlots<KIND>) return launch_row<KIND, 1024, 16, REST>(a, B, st);
+    return launch_split<KIND, REST>(a, B, st);
 }
 
 }  // namespace
@@ -308,18 +527,12 @@ rdk_status_t launch_distill_loss(const rdk_distill_desc_t &d, const KernelHandle
     a.part = (SoftStat *)ws;
     a.stats = stats ? (float4 *)stats : (float4 *)((char *)ws + align_up((size_t)d.B * a.parts * sizeof(SoftStat), 256));
     a.dz = dz; a.ldd = ldd;
+    rdk_status_t rc = RDK_OK;
     with_logits(z.kind, [&](auto k) {
         constexpr int KIND = decltype(k)::value;
-        if (teacher_lse) {
-            RDK_TIMED_LAUNCH("distill_part_kernel", (distill_part_kernel<KIND, true>), dim3((unsigned)d.B * a.parts), dim3(kDistillThreads), 0, st, a);
-            RDK_TIMED_LAUNCH("distill_finish_kernel", (distill_finish_kernel<KIND, true>), dim3((unsigned)d.B), dim3(kWave), 0, st, a);
-        } else {
-            RDK_TIMED_LAUNCH("distill_part_kernel", (distill_part_kernel<KIND, false>), dim3((unsigned)d.B * a.parts), dim3(kDistillThreads), 0, st, a);
-            RDK_TIMED_LAUNCH("distill_finish_kernel", (distill_finish_kernel<KIND, false>), dim3((unsigned)d.B), dim3(kWave), 0, st, a);
-        }
+        rc = teacher_lse ? launch_loss<KIND, true>(a, d.B, st) : launch_loss<KIND, false>(a, d.B, st);
     });
-    RDK_LAUNCH_CHECK("distill_finish_kernel");
-    return dz ? launch_grad(a, z.kind, d.B, st) : RDK_OK;
+    return rc;
 }
 
 rdk_status_t launch_distill_grad(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
@@ -328,7 +541,9 @@ rdk_status_t launch_distill_grad(const rdk_distill_desc_t &d, const KernelHandle
     DistillArgs a = arguments(d, h, z, top_ids, top_logits, weight);
     a.stats = (float4 *)const_cast<float *>(stats);
     a.dz = dz; a.ldd = ldd;
-    return launch_grad(a, z.kind, d.B, st);
+    rdk_status_t rc = RDK_OK;
+    with_logits(z.kind, [&](auto k) { rc = launch_grad<decltype(k)::value>(a, d.B, st); });
+    return rc;
 }
 
 }  // namespace rdk

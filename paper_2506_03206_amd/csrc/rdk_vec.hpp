@@ -31,6 +31,13 @@ struct Vec {
         }
     }
 
+    // What was made of a vector so far is made anew after this: values kept from one pass over a row in registers to the next would take
+    // twice the registers of the row itself.
+    static __device__ __forceinline__ void again(u32x4 &r)
+    {
+        if constexpr (KIND == RDK_LOGIT_BF16) asm volatile("" : "+v"(r));
+    }
+
     static __device__ __forceinline__ unsigned one(const void *row, int64_t i)
     {
         if constexpr (KIND == RDK_LOGIT_BF16) return ((const uint16_t *)row)[i];
