@@ -250,20 +250,50 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
     }
 }
 
+// The first wavefront's entries while its registers hold its share of the row.
+struct EntryShared {
+    double log_t[kMaxEntries], constant, r;
+    int slot[kMaxEntries], held, remainder;
+    float zt[kMaxEntries], p[kMaxEntries];
+
+    __device__ __forceinline__ void put(const Entries &t, const float (&z)[kPerLane], const Teacher &o)
+    {
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j) {
+            const int k = lane_id() + j * kWave;
+            log_t[k] = o.log_t[j]; slot[k] = t.slot[j]; zt[k] = z[j]; p[k] = o.p[j];
+        }
+        if (lane_id() == 0) {
+            constant = o.constant; r = o.r; held = o.held; remainder = o.remainder;
+        }
+    }
+    __device__ __forceinline__ void get(Entries &t, float (&z)[kPerLane], Teacher &o) const
+    {
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j) {
+            const int k = lane_id() + j * kWave;
+            o.log_t[j] = log_t[k]; t.slot[j] = slot[k]; z[j] = zt[k]; o.p[j] = p[k];
+        }
+        o.constant = constant; o.r = r; o.held = held; o.remainder = remainder;
+    }
+};
+
 // A whole row in the registers of one workgroup: its logits are read once, for the loss and the gradient.  The first wavefront follows the
-// teacher's entries meanwhile (ids to slots to logits, a chain of three reads) and adds up the loss while the others write the gradient;
-// the entries' own gradient then goes over what stands at their slots.
+// teacher's entries meanwhile (ids to slots to logits, a chain of three reads); their own gradient goes over what stands at their slots.
+// The exponentials, relative to the largest logit of their thread, stay in the registers for the gradient where 64 of them hold a thread's share
+// (the vector unit would be busy with them twice: 19 instructions a logit instead of 12, half as long as the row takes to stream), else
+// they are formed again.  The up to kLen - 1 logits behind the last whole vector of a row are one thread's each.
 template <int KIND, int THREADS, int VECS, bool REST, bool GRAD>
 __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
     constexpr int kWaves = THREADS / kWave;
-    __shared__ __attribute__((aligned(16))) uint8_t marked[REST ? THREADS * VECS : 16];   // a bit per slot of A, by the thread that holds it
+    constexpr bool KEEP = GRAD && VECS * V::kLen <= 64;
+    __shared__ __attribute__((aligned(16))) uint8_t marked[REST ? THREADS * VECS + 16 : 16];   // a bit per slot of A, by the thread that holds it
     __shared__ SoftStat waves[kWaves], entries;
-    __shared__ float remaining;
-    __shared__ int held;
+    __shared__ EntryShared kept;
     const int64_t row = blockIdx.x;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, whole = a.n / V::kLen, behind = a.n % V::kLen;   // whole vectors, logits behind them
     const void *zr = row_ptr<KIND>(a.z, a.ldz, row);
     void *dr = GRAD ? const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row)) : nullptr;
     const float w = a.weight ? a.weight[row] : 1.f;
@@ -279,37 +309,33 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
         return;
     }
     const float c = a.inv_t * kLog2e;
-    Entries t;
-    float zt[kPerLane];
-    Teacher o;
     u32x4 raw[VECS];
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
-        const int i = (j * THREADS + tid) * V::kLen;
-        raw[j] = i < a.n ? V::load(zr, i, a.n) : V::fill();
+        raw[j] = V::fill();
+        if (j * THREADS + tid < whole) raw[j] = *(const u32x4_any *)((const char *)zr + j * THREADS * 16 + (uint32_t)tid * 16);
     }
+    float last = tid < behind ? load1<KIND>(zr, whole * V::kLen + tid) : -INFINITY;
     if (REST) {
-        for (int i = tid; i < THREADS * VECS / 4; i += THREADS) ((unsigned *)marked)[i] = 0;
+        for (int i = tid; i < THREADS * VECS / 4 + 4; i += THREADS) ((unsigned *)marked)[i] = 0;
         __syncthreads();
     }
     if (tid < kWave) {
-        t = row_entries(a, row);
+        const Entries t = row_entries(a, row);
+        float zt[kPerLane];
         entry_logits<KIND>(zr, t, zt);
         if (REST) {
 #pragma unroll
             for (int j = 0; j < kPerLane; ++j)
                 if (t.slot[j] >= 0) {
-                    const int q = t.slot[j] / V::kLen, at = q % THREADS * VECS + q / THREADS;
+                    const int q = t.slot[j] / V::kLen, at = q == whole ? THREADS * VECS : q % THREADS * VECS + q / THREADS;
                     atomicOr((unsigned *)marked + at / 4, 1u << (at % 4 * 8 + t.slot[j] % V::kLen));
                 }
         }
-        o = teacher_of<REST>(a, row, t);
+        const Teacher o = teacher_of<REST>(a, row, t);
         const SoftStat at = REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f};
-        if (tid == 0) {
-            entries = at;
-            remaining = (float)o.r;
-            held = o.held;
-        }
+        if (tid == 0) entries = at;
+        kept.put(t, zt, o);
     }
     if (REST) {
         __syncthreads();
@@ -322,27 +348,32 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
                     if (bits >> e & 1u) V::set(raw[j], e, V::kFill);
             }
         }
+        if (tid < behind && (marked[THREADS * VECS] >> tid & 1)) last = -INFINITY;
     }
-    float v[V::kLen];
-    SoftStat st{-INFINITY, 0.f};
+    float v[V::kLen], e[KEEP ? VECS : 1][V::kLen];
+    SoftStat st{last, 0.f};
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
         V::to(raw[j], v);
 #pragma unroll
-        for (int e = 0; e < V::kLen; ++e) st.m = fmaxf(st.m, v[e]);
+        for (int k = 0; k < V::kLen; ++k) st.m = fmaxf(st.m, v[k]);
     }
-    {
-        const float ref = weight_reference(st.m);
+    const float own_ref = weight_reference(st.m), e_last = soft_term(last, own_ref, c);
+    st.s = e_last;
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) {
-            V::again(raw[j]);
-            V::to(raw[j], v);
-            float part = 0.f;
+    for (int j = 0; j < VECS; ++j) {
+        V::again(raw[j]);
+        V::to(raw[j], v);
+        float part = 0.f;
 #pragma unroll
-            for (int e = 0; e < V::kLen; ++e) part += soft_term(v[e], ref, c);
-            st.s += part;
+        for (int k = 0; k < V::kLen; ++k) {
+            const float x = soft_term(v[k], own_ref, c);
+            if (KEEP) e[j][k] = x;
+            part += x;
         }
+        st.s += part;
     }
+    const float own_s = st.s;
     st = wave_merge_at(st, c);
     if (lane_id() == 0) waves[tid / kWave] = st;
     __syncthreads();   // (the logits at the entries have been read too: dz may be z)
@@ -356,32 +387,39 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
     all.s = rest;
     if (REST) all.s += entries.s == 0.f ? 0.f : entries.s * soft_term(weight_reference(entries.m), ref, c);
     const float inv = all.s == 0.f ? 0.f : 1.f / all.s;
-    const float outside = outside_of(REST && held < a.n, remaining, held, all.s, rest), wt = w * a.inv_t;
-    if (tid < kWave) {
+    const float outside = outside_of(REST && kept.remainder, (float)kept.r, kept.held, all.s, rest), wt = w * a.inv_t;
+    if (GRAD) {
+        const float scale = wt * inv * outside;
+        const float own_scale = own_s == 0.f ? 0.f : scale * soft_term(own_ref, ref, c);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j)
+            if (j * THREADS + tid < whole) {
+                if (!KEEP) {
+                    V::again(raw[j]);
+                    V::to(raw[j], v);
+                }
+#pragma unroll
+                for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], ref, c);
+                V::store_at((char *)dr + j * THREADS * 16, tid * 16, V::kLen, V::from(v));
+            }
+        if (tid < behind) V::store1(dr, whole * V::kLen + tid, own_scale * e_last);
+        __syncthreads();
+    }
+    if (tid < kWave) {   // (the registers of the row are free by now)
+        Entries t;
+        float zt[kPerLane];
+        Teacher o;
+        kept.get(t, zt, o);
+        if (GRAD) {
+#pragma unroll
+            for (int j = 0; j < kPerLane; ++j)
+                if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - o.p[j]));
+        }
         const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
         if (tid == 0) {
             a.loss[row] = (float)(w * loss);
             if (a.stats) a.stats[row] = make_float4(ref, inv, outside, (float)o.constant);
         }
-    }
-    if (!GRAD) return;
-    const float scale = wt * inv * outside;
-#pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        const int i = (j * THREADS + tid) * V::kLen;
-        if (i < a.n) {
-            V::again(raw[j]);
-            V::to(raw[j], v);
-#pragma unroll
-            for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], ref, c);
-            V::store(dr, i, a.n, V::from(v));
-        }
-    }
-    __syncthreads();
-    if (tid < kWave) {
-#pragma unroll
-        for (int j = 0; j < kPerLane; ++j)
-            if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - o.p[j]));
     }
 }
 
@@ -404,8 +442,8 @@ __global__ __launch_bounds__(kDistillThreads) void distill_grad_kernel(DistillAr
     u32x4 raw[kGradVecs];
 #pragma unroll
     for (int j = 0; j < kGradVecs; ++j) {
-        const int i = begin + (j * kDistillThreads + tid) * V::kLen;
-        raw[j] = i < end ? V::load(zr, i, end) : V::fill();
+        const int left = end - begin - (j * kDistillThreads + tid) * V::kLen;
+        raw[j] = left > 0 ? V::load_at((const char *)zr + ((int64_t)begin * V::kSize + j * kDistillThreads * 16), tid * 16, left) : V::fill();
     }
     const float4 stats = a.stats[row];
     const float c = a.inv_t * kLog2e, wt = w * a.inv_t, scale = stats.y * stats.z * wt;
@@ -418,13 +456,13 @@ __global__ __launch_bounds__(kDistillThreads) void distill_grad_kernel(DistillAr
     __syncthreads();   // the logits at the entries have been read before anything is written: dz may be z
 #pragma unroll
     for (int j = 0; j < kGradVecs; ++j) {
-        const int i = begin + (j * kDistillThreads + tid) * V::kLen;
-        if (i < end) {
+        const int left = end - begin - (j * kDistillThreads + tid) * V::kLen;
+        if (left > 0) {
             float v[V::kLen];
             V::to(raw[j], v);
 #pragma unroll
             for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
-            V::store(dr, i, end, V::from(v));
+            V::store_at((char *)dr + ((int64_t)begin * V::kSize + j * kDistillThreads * 16), tid * 16, left, V::from(v));
         }
     }
     __syncthreads();   // the entries' own gradient goes over what stands at their slots

@@ -44,15 +44,23 @@ struct Vec {
         return ((const unsigned *)row)[i];
     }
 
-    // elements i .. i + kLen - 1 of a row that ends at `end`: those behind it are fill
-    static __device__ __forceinline__ u32x4 load(const void *row, int64_t i, int64_t end)
+    // The vector `off` bytes behind a place that all lanes share (a scalar base and 32 bits of a lane's own: two registers less per address),
+    // of which `left` elements belong to the row: the others are fill.
+    static __device__ __forceinline__ u32x4 load_at(const void *base, uint32_t off, int left)
     {
-        if (i + kLen <= end) return *(const u32x4_any *)((const char *)row + i * kSize);
+        const char *p = (const char *)base + off;
+        if (left >= kLen) return *(const u32x4_any *)p;
         u32x4 r = fill();
 #pragma unroll
         for (int e = 0; e < kLen - 1; ++e)   // the vector is not whole
-            if (i + e < end) set(r, e, one(row, i + e));
+            if (e < left) set(r, e, one(p, e));
         return r;
+    }
+
+    // elements i .. i + kLen - 1 of a row that ends at `end`
+    static __device__ __forceinline__ u32x4 load(const void *row, int64_t i, int64_t end)
+    {
+        return load_at((const char *)row + i * kSize, 0, end - i < kLen ? (int)(end - i) : kLen);
     }
 
     // element e (a constant after unrolling) of a vector
@@ -70,7 +78,11 @@ struct Vec {
         u32x4 r;
         if constexpr (KIND == RDK_LOGIT_BF16) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) r[i] = (unsigned)round_bf16(v[2 * i]) | ((unsigned)round_bf16(v[2 * i + 1]) << 16);
+            for (int i = 0; i < 4; ++i) {   // one conversion instruction for two
+                typedef float f2 __attribute__((ext_vector_type(2)));
+                typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+                r[i] = __builtin_bit_cast(unsigned, __builtin_convertvector(f2{v[2 * i], v[2 * i + 1]}, b2));
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) r[i] = __float_as_uint(v[i]);
@@ -80,21 +92,27 @@ struct Vec {
 
     static __device__ __forceinline__ uint16_t round_bf16(float x)
     {
-        return __builtin_bit_cast(uint16_t, (__bf16)x);   // one conversion instruction on gfx950
+        return __builtin_bit_cast(uint16_t, (__bf16)x);
     }
 
-    static __device__ __forceinline__ void store(void *row, int64_t i, int64_t end, const u32x4 r)
+    // non-temporal: results are larger than the caches, and what is read again should stay there
+    static __device__ __forceinline__ void store_at(void *base, uint32_t off, int left, const u32x4 r)
     {
-        if (i + kLen <= end) {
-            *(u32x4_any *)((char *)row + i * kSize) = r;
+        char *p = (char *)base + off;
+        if (left >= kLen) {
+            __builtin_nontemporal_store(r, (u32x4_any *)p);
             return;
         }
 #pragma unroll
         for (int e = 0; e < kLen - 1; ++e)
-            if (i + e < end) {
-                if constexpr (KIND == RDK_LOGIT_BF16) ((uint16_t *)row)[i + e] = (uint16_t)(r[e / 2] >> (e % 2 * 16));
-                else ((unsigned *)row)[i + e] = r[e];
+            if (e < left) {
+                if constexpr (KIND == RDK_LOGIT_BF16) ((uint16_t *)p)[e] = (uint16_t)(r[e / 2] >> (e % 2 * 16));
+                else ((unsigned *)p)[e] = r[e];
             }
+    }
+    static __device__ __forceinline__ void store(void *row, int64_t i, int64_t end, const u32x4 r)
+    {
+        store_at((char *)row + i * kSize, 0, end - i < kLen ? (int)(end - i) : kLen, r);
     }
 
     static __device__ __forceinline__ void store1(void *row, int64_t i, float x)
