@@ -55,6 +55,19 @@ __device__ __forceinline__ Entries row_entries(const DistillArgs &a, int64_t row
     return t;
 }
 
+// The same with the slots known.
+__device__ __forceinline__ Entries row_entries(const DistillArgs &a, int64_t row, const int *slots)
+{
+    Entries t;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j) {
+        const int k = lane_id() + j * kWave;
+        t.slot[j] = slots[k];
+        t.v[j] = k < a.K ? a.top_logits[row * a.K + k] : -INFINITY;
+    }
+    return t;
+}
+
 __device__ __forceinline__ float soft_term(float z, float ref, float c) { return __builtin_amdgcn_exp2f((z - ref) * c); }
 
 __device__ __forceinline__ SoftStat merge_at(SoftStat a, SoftStat b, float c)
@@ -250,18 +263,18 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
     }
 }
 
-// The first wavefront's entries while its registers hold its share of the row.
+// A row's entries between the steps of the wavefront that follows them.
 struct EntryShared {
     double log_t[kMaxEntries], constant, r;
     int slot[kMaxEntries], held, remainder;
     float zt[kMaxEntries], p[kMaxEntries];
 
-    __device__ __forceinline__ void put(const Entries &t, const float (&z)[kPerLane], const Teacher &o)
+    __device__ __forceinline__ void put(const float (&z)[kPerLane], const Teacher &o)
     {
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j) {
             const int k = lane_id() + j * kWave;
-            log_t[k] = o.log_t[j]; slot[k] = t.slot[j]; zt[k] = z[j]; p[k] = o.p[j];
+            log_t[k] = o.log_t[j]; zt[k] = z[j]; p[k] = o.p[j];
         }
         if (lane_id() == 0) {
             constant = o.constant; r = o.r; held = o.held; remainder = o.remainder;
@@ -278,29 +291,45 @@ struct EntryShared {
     }
 };
 
-// A whole row in the registers of one workgroup: its logits are read once, for the loss and the gradient.  The first wavefront follows the
-// teacher's entries meanwhile (ids to slots to logits, a chain of three reads); their own gradient goes over what stands at their slots.
-// The exponentials, relative to the largest logit of their thread, stay in the registers for the gradient where 64 of them hold a thread's share
+template <int KIND, bool REST>
+__device__ __forceinline__ void follow(const DistillArgs &a, int64_t row, const void *zr, float c, const Entries &t, EntryShared &kept, SoftStat *entries)
+{
+    float zt[kPerLane];
+    entry_logits<KIND>(zr, t, zt);
+    const Teacher o = teacher_of<REST>(a, row, t);
+    if (REST) {
+        const SoftStat st = entry_stat(t, zt, c);
+        if (lane_id() == 0) *entries = st;
+    }
+    kept.put(zt, o);
+}
+
+// A whole row in the registers of one workgroup: its logits are read once, for the loss and the gradient.  One wavefront beside the THREADS that
+// hold the row follows the teacher's entries (ids to slots to logits, a chain of three reads that would otherwise wait for the row: loads
+// return in order) and adds up the loss; the entries' own gradient goes over what stands at their slots.
+// The exponentials, relative to the largest logit of their thread, stay in the registers for the gradient where 72 of them hold a thread's share
 // (the vector unit would be busy with them twice: 19 instructions a logit instead of 12, half as long as the row takes to stream), else
 // they are formed again.  The up to kLen - 1 logits behind the last whole vector of a row are one thread's each.
 template <int KIND, int THREADS, int VECS, bool REST, bool GRAD>
-__global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
+__global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
     constexpr int kWaves = THREADS / kWave;
-    constexpr bool KEEP = GRAD && VECS * V::kLen <= 64;
-    __shared__ __attribute__((aligned(16))) uint8_t marked[REST ? THREADS * VECS + 16 : 16];   // a bit per slot of A, by the thread that holds it
+    constexpr bool KEEP = GRAD && VECS * V::kLen <= 72;
+    constexpr int kMarks = REST ? (int)((THREADS * VECS + 31) / 16 * 16) : 16;
+    __shared__ __attribute__((aligned(16))) uint8_t marked[kMarks];   // a bit per slot of A, by the thread that holds it
     __shared__ SoftStat waves[kWaves], entries;
     __shared__ EntryShared kept;
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, whole = a.n / V::kLen, behind = a.n % V::kLen;   // whole vectors, logits behind them
+    const bool follows = tid >= THREADS;                                          // the wavefront of the entries
     const void *zr = row_ptr<KIND>(a.z, a.ldz, row);
     void *dr = GRAD ? const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row)) : nullptr;
     const float w = a.weight ? a.weight[row] : 1.f;
     if (w == 0.f) {
         if (GRAD) {
             const u32x4 zero{0, 0, 0, 0};
-            for (int i = tid * V::kLen; i < a.n; i += THREADS * V::kLen) V::store(dr, i, a.n, zero);
+            for (int i = tid * V::kLen; i < a.n; i += (THREADS + kWave) * V::kLen) V::store(dr, i, a.n, zero);
         }
         if (tid == 0) {
             a.loss[row] = 0.f;
@@ -310,21 +339,11 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
     }
     const float c = a.inv_t * kLog2e;
     u32x4 raw[VECS];
-#pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        raw[j] = V::fill();
-        if (j * THREADS + tid < whole) raw[j] = *(const u32x4_any *)((const char *)zr + j * THREADS * 16 + (uint32_t)tid * 16);
-    }
-    float last = tid < behind ? load1<KIND>(zr, whole * V::kLen + tid) : -INFINITY;
-    if (REST) {
-        for (int i = tid; i < THREADS * VECS / 4 + 4; i += THREADS) ((unsigned *)marked)[i] = 0;
-        __syncthreads();
-    }
-    if (tid < kWave) {
+    float last = -INFINITY;
+    if (follows) {
         const Entries t = row_entries(a, row);
-        float zt[kPerLane];
-        entry_logits<KIND>(zr, t, zt);
         if (REST) {
+            for (int i = lane_id() * 16; i < kMarks; i += kWave * 16) *(u32x4 *)(marked + i) = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < kPerLane; ++j)
                 if (t.slot[j] >= 0) {
@@ -332,94 +351,107 @@ __global__ __launch_bounds__(THREADS) void distill_row_kernel(DistillArgs a)
                     atomicOr((unsigned *)marked + at / 4, 1u << (at % 4 * 8 + t.slot[j] % V::kLen));
                 }
         }
-        const Teacher o = teacher_of<REST>(a, row, t);
-        const SoftStat at = REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f};
-        if (tid == 0) entries = at;
-        kept.put(t, zt, o);
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j) kept.slot[lane_id() + j * kWave] = t.slot[j];
+        if (!REST) follow<KIND, REST>(a, row, zr, c, t, kept, &entries);
+    } else {
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            raw[j] = V::fill();
+            if (j * THREADS + tid < whole) raw[j] = *(const u32x4_any *)((const char *)zr + j * THREADS * 16 + (uint32_t)tid * 16);
+        }
+        if (tid < behind) last = load1<KIND>(zr, whole * V::kLen + tid);
     }
     if (REST) {
         __syncthreads();
+        if (follows) {
+            const Entries t = row_entries(a, row, kept.slot);
+            follow<KIND, REST>(a, row, zr, c, t, kept, &entries);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) {
+                const unsigned bits = marked[tid * VECS + j];
+                if (bits) {
+#pragma unroll
+                    for (int e = 0; e < V::kLen; ++e)
+                        if (bits >> e & 1u) V::set(raw[j], e, V::kFill);
+                }
+            }
+            if (tid < behind && (marked[THREADS * VECS] >> tid & 1)) last = -INFINITY;
+        }
+    }
+    float v[V::kLen], e[KEEP ? VECS : 1][V::kLen], own_ref = 0.f, own_s = 0.f, e_last = 0.f;
+    if (!follows) {
+        float m = last;
 #pragma unroll
         for (int j = 0; j < VECS; ++j) {
-            const unsigned bits = marked[tid * VECS + j];
-            if (bits) {
+            V::to(raw[j], v);
 #pragma unroll
-                for (int e = 0; e < V::kLen; ++e)
-                    if (bits >> e & 1u) V::set(raw[j], e, V::kFill);
+            for (int k = 0; k < V::kLen; ++k) m = fmaxf(m, v[k]);
+        }
+        own_ref = weight_reference(m);
+        own_s = e_last = soft_term(last, own_ref, c);
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            V::again(raw[j]);
+            V::to(raw[j], v);
+            float part = 0.f;
+#pragma unroll
+            for (int k = 0; k < V::kLen; ++k) {
+                const float x = soft_term(v[k], own_ref, c);
+                if (KEEP) e[j][k] = x;
+                part += x;
             }
+            own_s += part;
         }
-        if (tid < behind && (marked[THREADS * VECS] >> tid & 1)) last = -INFINITY;
+        const SoftStat st = wave_merge_at(SoftStat{m, own_s}, c);
+        if (lane_id() == 0) waves[tid / kWave] = st;
     }
-    float v[V::kLen], e[KEEP ? VECS : 1][V::kLen];
-    SoftStat st{last, 0.f};
-#pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        V::to(raw[j], v);
-#pragma unroll
-        for (int k = 0; k < V::kLen; ++k) st.m = fmaxf(st.m, v[k]);
-    }
-    const float own_ref = weight_reference(st.m), e_last = soft_term(last, own_ref, c);
-    st.s = e_last;
-#pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        V::again(raw[j]);
-        V::to(raw[j], v);
-        float part = 0.f;
-#pragma unroll
-        for (int k = 0; k < V::kLen; ++k) {
-            const float x = soft_term(v[k], own_ref, c);
-            if (KEEP) e[j][k] = x;
-            part += x;
-        }
-        st.s += part;
-    }
-    const float own_s = st.s;
-    st = wave_merge_at(st, c);
-    if (lane_id() == 0) waves[tid / kWave] = st;
     __syncthreads();   // (the logits at the entries have been read too: dz may be z)
-    st = waves[0];
-    for (int k = 1; k < kWaves; ++k) st.m = fmaxf(st.m, waves[k].m);
-    SoftStat all{st.m, 0.f};
-    if (REST) all.m = fmaxf(all.m, entries.m);
-    const float ref = weight_reference(all.m);
+    float top = REST ? entries.m : -INFINITY;
+    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, waves[k].m);
+    const float ref = weight_reference(top);
     float rest = 0.f;
     for (int k = 0; k < kWaves; ++k) rest += waves[k].s == 0.f ? 0.f : waves[k].s * soft_term(weight_reference(waves[k].m), ref, c);
-    all.s = rest;
-    if (REST) all.s += entries.s == 0.f ? 0.f : entries.s * soft_term(weight_reference(entries.m), ref, c);
-    const float inv = all.s == 0.f ? 0.f : 1.f / all.s;
-    const float outside = outside_of(REST && kept.remainder, (float)kept.r, kept.held, all.s, rest), wt = w * a.inv_t;
+    float total = rest;
+    if (REST) total += entries.s == 0.f ? 0.f : entries.s * soft_term(weight_reference(entries.m), ref, c);
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    const float outside = outside_of(REST && kept.remainder, (float)kept.r, kept.held, total, rest), wt = w * a.inv_t;
     if (GRAD) {
         const float scale = wt * inv * outside;
         const float own_scale = own_s == 0.f ? 0.f : scale * soft_term(own_ref, ref, c);
+        if (!follows) {
 #pragma unroll
-        for (int j = 0; j < VECS; ++j)
-            if (j * THREADS + tid < whole) {
-                if (!KEEP) {
-                    V::again(raw[j]);
-                    V::to(raw[j], v);
+            for (int j = 0; j < VECS; ++j)
+                if (j * THREADS + tid < whole) {
+                    if (!KEEP) {
+                        V::again(raw[j]);
+                        V::to(raw[j], v);
+                    }
+#pragma unroll
+                    for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], ref, c);
+                    V::store_at((char *)dr + j * THREADS * 16, tid * 16, V::kLen, V::from(v));
                 }
-#pragma unroll
-                for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], ref, c);
-                V::store_at((char *)dr + j * THREADS * 16, tid * 16, V::kLen, V::from(v));
-            }
-        if (tid < behind) V::store1(dr, whole * V::kLen + tid, own_scale * e_last);
-        __syncthreads();
-    }
-    if (tid < kWave) {   // (the registers of the row are free by now)
-        Entries t;
-        float zt[kPerLane];
-        Teacher o;
-        kept.get(t, zt, o);
-        if (GRAD) {
-#pragma unroll
-            for (int j = 0; j < kPerLane; ++j)
-                if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - o.p[j]));
+            if (tid < behind) V::store1(dr, whole * V::kLen + tid, own_scale * e_last);
         }
-        const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
-        if (tid == 0) {
+    }
+    Entries t;
+    float zt[kPerLane];
+    Teacher o;
+    if (follows) {
+        kept.get(t, zt, o);
+        const double loss = loss_of(a, t, zt, o, ref, total, rest);
+        if (lane_id() == 0) {
             a.loss[row] = (float)(w * loss);
             if (a.stats) a.stats[row] = make_float4(ref, inv, outside, (float)o.constant);
         }
+    }
+    if (!GRAD) return;
+    __syncthreads();
+    if (follows) {
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j)
+            if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - o.p[j]));
     }
 }
 
@@ -476,7 +508,7 @@ __global__ __launch_bounds__(kDistillThreads) void distill_grad_kernel(DistillAr
 
 // The longest row that a workgroup holds.
 template <int KIND>
-constexpr int kRowSlots = 1024 * 16 * Vec<KIND>::kLen;
+constexpr int kRowSlots = 960 * 17 * Vec<KIND>::kLen;
 
 template <class F>
 void with_logits(rdk_input_kind_t kind, const F &f)
@@ -526,8 +558,8 @@ rdk_status_t launch_split(const DistillArgs &a, int32_t B, hipStream_t st)
 template <int KIND, int THREADS, int VECS, bool REST>
 rdk_status_t launch_row(const DistillArgs &a, int32_t B, hipStream_t st)
 {
-    if (a.dz) RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, true>), dim3((unsigned)B), dim3(THREADS), 0, st, a);
-    else RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, false>), dim3((unsigned)B), dim3(THREADS), 0, st, a);
+    if (a.dz) RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, true>), dim3((unsigned)B), dim3(THREADS + kWave), 0, st, a);
+    else RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, false>), dim3((unsigned)B), dim3(THREADS + kWave), 0, st, a);
     RDK_LAUNCH_CHECK("distill_row_kernel");
     return RDK_OK;
 }
@@ -536,11 +568,12 @@ template <int KIND, bool REST>
 rdk_status_t launch_loss(const DistillArgs &a, int32_t B, hipStream_t st)
 {
     constexpr int kLen = Vec<KIND>::kLen;
-    if (a.n <= 256 * 2 * kLen) return launch_row<KIND, 256, 2, REST>(a, B, st);
-    if (a.n <= 256 * 8 * kLen) return launch_row<KIND, 256, 8, REST>(a, B, st);
-    if (a.n <= 512 * 8 * kLen) return launch_row<KIND, 512, 8, REST>(a, B, st);
-    if (a.n <= 1024 * 8 * kLen) return launch_row<KIND, 1024, 8, REST>(a, B, st);
-    if (a.n <= kRowSlots<KIND>) return launch_row<KIND, 1024, 16, REST>(a, B, st);
+    if (a.n <= 192 * 3 * kLen) return launch_row<KIND, 192, 3, REST>(a, B, st);
+    if (a.n <= 192 * 9 * kLen) return launch_row<KIND, 192, 9, REST>(a, B, st);
+    if (a.n <= 448 * 5 * kLen) return launch_row<KIND, 448, 5, REST>(a, B, st);
+    if (a.n <= 448 * 9 * kLen) return launch_row<KIND, 448, 9, REST>(a, B, st);
+    if (a.n <= 448 * 17 * kLen) return launch_row<KIND, 448, 17, REST>(a, B, st);
+    if (a.n <= kRowSlots<KIND>) return launch_row<KIND, 960, 17, REST>(a, B, st);
     return launch_split<KIND, REST>(a, B, st);
 }
 
