@@ -438,7 +438,7 @@ rdk_status_t rdk_philox_words(uint64_t seed, uint64_t offset, int32_t count, uin
  * tree_walk_kernel, verify_multi_kernel, verify_multi_round_kernel,
  * q_transpose_kernel, sparse_product_kernel, prep_a_split_kernel, exact_f32_split_kernel,
  * exact_reduce_kernel, prep_a_bf16_kernel, exact_bf16_kernel, topk_part_kernel, topk_merge_kernel, beam_merge_kernel, beam_reorder_kernel,
- * distill_row_kernel, distill_part_kernel, distill_finish_kernel, distill_grad_kernel.
+ * distill_row_kernel, distill_loop_kernel, distill_part_kernel, distill_finish_kernel, distill_grad_kernel.
  */
 rdk_status_t rdk_timing_select(const char *kernel_name);
 rdk_status_t rdk_timing_read(const char *kernel_name, int64_t *launches, double *total_ms);

@@ -14,7 +14,8 @@ constexpr int kMaxEntries = 128;          // teacher entries of a position: two 
 constexpr int kPerLane = kMaxEntries / kWave;
 constexpr int kDistillThreads = 256;
 constexpr int kGradVecs = 8;             // 16-byte vectors of a thread in the backward call
-constexpr int kPartSlots = 65536;         // at most, of a row in one workgroup: the bitmap of A
+constexpr int kLoopThreads = 448, kLoopVecs = 4;   // a row read in rounds
+constexpr int kPartVecs = 8;             // of a part of a row that several workgroups share
 constexpr float kLog2e = 1.44269504088896341f;
 
 struct DistillArgs {
@@ -22,7 +23,7 @@ struct DistillArgs {
     int64_t ldz;
     const int32_t *slot_of;   // target id -> slot, or NULL: ids are slots
     int ids;                  // ids below this have an entry there
-    int n, K, parts, part_slots, grad_parts;
+    int n, K, parts, grad_parts, in_place;
     float inv_t;
     const int32_t *top_ids;
     const float *top_logits, *teacher_lse, *weight;
@@ -87,54 +88,68 @@ __device__ __forceinline__ SoftStat wave_merge_at(SoftStat v, float c)
     return r;
 }
 
-// Statistics of a part of a row; REST: of the slots outside A alone.
+// Statistics of a part of a row, whose logits lie in the registers; REST: of the slots outside A alone.
 template <int KIND, bool REST>
-__global__ __launch_bounds__(kDistillThreads) void distill_part_kernel(DistillArgs a)
+__global__ __launch_bounds__(kDistillThreads + kWave) void distill_part_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
-    constexpr int kWaves = kDistillThreads / kWave;
-    __shared__ unsigned marked[REST ? kPartSlots / 32 : 1];
+    constexpr int kWaves = kDistillThreads / kWave, kSlots = kDistillThreads * kPartVecs * V::kLen;
+    __shared__ uint8_t marked[REST ? kDistillThreads * kPartVecs : 16];
     __shared__ SoftStat sh[kWaves];
     const int64_t row = blockIdx.x / a.parts;
-    const int part = blockIdx.x % a.parts, begin = part * a.part_slots, end = min(a.n, begin + a.part_slots);
+    const int part = blockIdx.x % a.parts, begin = part * kSlots, here = min(a.n - begin, kSlots), tid = threadIdx.x;
     if (a.weight && a.weight[row] == 0.f) return;
-    const void *zr = row_ptr<KIND>(a.z, a.ldz, row);
+    const char *zr = (const char *)row_ptr<KIND>(a.z, a.ldz, row) + (int64_t)begin * V::kSize;
     const float c = a.inv_t * kLog2e;
-    if (REST) {
-        for (int i = threadIdx.x; i < a.part_slots / 32; i += kDistillThreads) marked[i] = 0;
-        __syncthreads();
-        if (threadIdx.x < kWave) {
+    u32x4 raw[kPartVecs];
+    if (tid >= kDistillThreads) {
+        if (REST) {
             const Entries t = row_entries(a, row);
+            for (int i = lane_id() * 16; i < kDistillThreads * kPartVecs; i += kWave * 16) *(u32x4 *)(marked + i) = u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int j = 0; j < kPerLane; ++j)
-                if (t.slot[j] >= begin && t.slot[j] < end) atomicOr(&marked[(t.slot[j] - begin) / 32], 1u << ((t.slot[j] - begin) % 32));
+                if (t.slot[j] >= begin && t.slot[j] < begin + here) {
+                    const int q = (t.slot[j] - begin) / V::kLen, at = q % kDistillThreads * kPartVecs + q / kDistillThreads;
+                    atomicOr((unsigned *)marked + at / 4, 1u << (at % 4 * 8 + (t.slot[j] - begin) % V::kLen));
+                }
         }
-        __syncthreads();
+    } else {
+#pragma unroll
+        for (int j = 0; j < kPartVecs; ++j) {
+            const int left = here - (j * kDistillThreads + tid) * V::kLen;
+            raw[j] = left > 0 ? V::load_at(zr + j * kDistillThreads * 16, tid * 16, left) : V::fill();
+        }
     }
-    SoftStat st{-INFINITY, 0.f};
-    for (int i = begin + (int)threadIdx.x * V::kLen; i < end; i += kDistillThreads * V::kLen) {
+    if (REST) __syncthreads();
+    if (tid < kDistillThreads) {
         float v[V::kLen];
-        V::to(V::load(zr, i, end), v);
-        if (REST) {
-            const unsigned bits = marked[(i - begin) / 32] >> ((i - begin) % 32);
+        SoftStat st{-INFINITY, 0.f};
 #pragma unroll
-            for (int e = 0; e < V::kLen; ++e)
-                if (bits >> e & 1u) v[e] = -INFINITY;
+        for (int j = 0; j < kPartVecs; ++j) {
+            if (REST) {
+                const unsigned bits = marked[tid * kPartVecs + j];
+                if (bits) V::strike(raw[j], bits);
+            }
+            V::to(raw[j], v);
+#pragma unroll
+            for (int e = 0; e < V::kLen; ++e) st.m = fmaxf(st.m, v[e]);
         }
-        float mx = st.m;
+        const float ref = weight_reference(st.m);
 #pragma unroll
-        for (int e = 0; e < V::kLen; ++e) mx = fmaxf(mx, v[e]);
-        const float ref = weight_reference(mx);
-        float s = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
+        for (int j = 0; j < kPartVecs; ++j) {
+            V::again(raw[j]);
+            V::to(raw[j], v);
+            float sum = 0.f;
 #pragma unroll
-        for (int e = 0; e < V::kLen; ++e) s += soft_term(v[e], ref, c);
-        st.m = mx;
-        st.s = s;
+            for (int e = 0; e < V::kLen; ++e) sum += soft_term(v[e], ref, c);
+            st.s += sum;
+        }
+        st = wave_merge_at(st, c);
+        if (lane_id() == 0) sh[tid / kWave] = st;
     }
-    st = wave_merge_at(st, c);
-    if (lane_id() == 0) sh[threadIdx.x / kWave] = st;
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
+        SoftStat st = sh[0];
         for (int w = 1; w < kWaves; ++w) st = merge_at(st, sh[w], c);
         a.part[row * a.parts + part] = st;
     }
@@ -309,13 +324,14 @@ __device__ __forceinline__ void follow(const DistillArgs &a, int64_t row, const 
 // return in order) and adds up the loss; the entries' own gradient goes over what stands at their slots.
 // The exponentials, relative to the largest logit of their thread, stay in the registers for the gradient where 72 of them hold a thread's share
 // (the vector unit would be busy with them twice: 19 instructions a logit instead of 12, half as long as the row takes to stream), else
-// they are formed again.  The up to kLen - 1 logits behind the last whole vector of a row are one thread's each.
+// they are formed again: with seventeen vectors a thread (512 fp32 rows of 61000 54.3 us, 59.6 with them kept), and for bf16 rows in 960 threads
+// where no bits of A take registers too (1024 rows of 61000 52.9, kept 56.7; remainder counted 70.1, kept 63.3).  The up to kLen - 1 logits behind the last whole vector of a row are one thread's each.
 template <int KIND, int THREADS, int VECS, bool REST, bool GRAD>
 __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
     constexpr int kWaves = THREADS / kWave;
-    constexpr bool KEEP = GRAD && VECS * V::kLen <= 72;
+    constexpr bool KEEP = GRAD && VECS * V::kLen <= 72 && (VECS < 17) && (THREADS < 960 || KIND == RDK_LOGIT_F32 || REST);
     constexpr int kMarks = REST ? (int)((THREADS * VECS + 31) / 16 * 16) : 16;
     __shared__ __attribute__((aligned(16))) uint8_t marked[kMarks];   // a bit per slot of A, by the thread that holds it
     __shared__ SoftStat waves[kWaves], entries;
@@ -371,11 +387,7 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
 #pragma unroll
             for (int j = 0; j < VECS; ++j) {
                 const unsigned bits = marked[tid * VECS + j];
-                if (bits) {
-#pragma unroll
-                    for (int e = 0; e < V::kLen; ++e)
-                        if (bits >> e & 1u) V::set(raw[j], e, V::kFill);
-                }
+                if (bits) V::strike(raw[j], bits);
             }
             if (tid < behind && (marked[THREADS * VECS] >> tid & 1)) last = -INFINITY;
         }
@@ -455,60 +467,173 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
     }
 }
 
-// dz of a part of a row, whose logits lie in the registers.
+// The loss of a row too long for the registers, or for enough workgroups with it there, read in rounds by one workgroup; the bits of A for the whole
+// row in dynamic LDS.
+template <int KIND, bool REST>
+__global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(DistillArgs a)
+{
+    typedef Vec<KIND> V;
+    constexpr int kWaves = kLoopThreads / kWave, kRound = kLoopThreads * kLoopVecs;   // vectors
+    extern __shared__ __attribute__((aligned(16))) uint8_t marked_row[];               // a byte per vector of the row
+    __shared__ SoftStat waves[kWaves], entries;
+    __shared__ EntryShared kept;
+    const int64_t row = blockIdx.x;
+    const int tid = threadIdx.x, vectors = (a.n + V::kLen - 1) / V::kLen;
+    const bool follows = tid >= kLoopThreads;
+    const char *zr = (const char *)row_ptr<KIND>(a.z, a.ldz, row);
+    const float w = a.weight ? a.weight[row] : 1.f;
+    if (w == 0.f) {
+        if (tid == 0) {
+            a.loss[row] = 0.f;
+            a.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        return;
+    }
+    const float c = a.inv_t * kLog2e;
+    u32x4 raw[kLoopVecs];
+    auto load_round = [&](int base) {
+#pragma unroll
+        for (int j = 0; j < kLoopVecs; ++j) {
+            const int left = a.n - (base + j * kLoopThreads + tid) * V::kLen;
+            raw[j] = left > 0 ? V::load_at(zr + ((int64_t)base + j * kLoopThreads) * 16, tid * 16, left) : V::fill();
+        }
+    };
+    if (!follows) load_round(0);
+    if (REST) {
+        for (int i = tid * 16; i < vectors; i += (kLoopThreads + kWave) * 16) *(u32x4 *)(marked_row + i) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    if (follows) {
+        const Entries t = row_entries(a, row);
+#pragma unroll
+        for (int j = 0; j < kPerLane; ++j) {
+            if (REST && t.slot[j] >= 0) {
+                const int at = t.slot[j] / V::kLen;
+                atomicOr((unsigned *)marked_row + at / 4, 1u << (at % 4 * 8 + t.slot[j] % V::kLen));
+            }
+            kept.slot[lane_id() + j * kWave] = t.slot[j];
+        }
+    }
+    if (REST) __syncthreads();
+    if (follows) {
+        const Entries t = row_entries(a, row, kept.slot);
+        follow<KIND, REST>(a, row, zr, c, t, kept, &entries);
+    } else {
+        float v[V::kLen];
+        SoftStat st{-INFINITY, 0.f};
+        for (int base = 0; base < vectors; base += kRound) {
+            u32x4 now[kLoopVecs];
+#pragma unroll
+            for (int j = 0; j < kLoopVecs; ++j) now[j] = raw[j];
+            if (base + kRound < vectors) load_round(base + kRound);
+            float m = st.m;
+#pragma unroll
+            for (int j = 0; j < kLoopVecs; ++j) {
+                const int at = base + j * kLoopThreads + tid;
+                if (REST && at < vectors) {
+                    const unsigned bits = marked_row[at];
+                    if (bits) V::strike(now[j], bits);
+                }
+                V::to(now[j], v);
+#pragma unroll
+                for (int e = 0; e < V::kLen; ++e) m = fmaxf(m, v[e]);
+            }
+            const float ref = weight_reference(m);
+            float sum = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
+#pragma unroll
+            for (int j = 0; j < kLoopVecs; ++j) {
+                V::again(now[j]);
+                V::to(now[j], v);
+                float part = 0.f;
+#pragma unroll
+                for (int e = 0; e < V::kLen; ++e) part += soft_term(v[e], ref, c);
+                sum += part;
+            }
+            st = SoftStat{m, sum};
+        }
+        st = wave_merge_at(st, c);
+        if (lane_id() == 0) waves[tid / kWave] = st;
+    }
+    __syncthreads();
+    if (!follows) return;
+    SoftStat st = lane_id() < kWaves ? waves[lane_id()] : SoftStat{-INFINITY, 0.f};
+    st = wave_merge_at(st, c);
+    const SoftStat all = merge_at(st, REST ? entries : SoftStat{-INFINITY, 0.f}, c);
+    const float ref = weight_reference(all.m), rest = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
+    Entries t;
+    float zt[kPerLane];
+    Teacher o;
+    kept.get(t, zt, o);
+    const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
+    if (lane_id() == 0) {
+        a.loss[row] = (float)(w * loss);
+        a.stats[row] = make_float4(ref, all.s == 0.f ? 0.f : 1.f / all.s, outside_of(o.remainder, (float)o.r, o.held, all.s, rest), (float)o.constant);
+    }
+}
+
+// dz of a part of a row, whose logits lie in the registers; the entries as in distill_row_kernel.
 template <int KIND>
-__global__ __launch_bounds__(kDistillThreads) void distill_grad_kernel(DistillArgs a)
+__global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
     constexpr int kSlots = kDistillThreads * kGradVecs * V::kLen;
     const int64_t row = blockIdx.x / a.grad_parts;
-    const int begin = (int)(blockIdx.x % a.grad_parts) * kSlots, end = min(a.n, begin + kSlots), tid = threadIdx.x;
-    const void *zr = row_ptr<KIND>(a.z, a.ldz, row);
-    void *dr = const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row));
+    const int begin = (int)(blockIdx.x % a.grad_parts) * kSlots, here = min(a.n - begin, kSlots), tid = threadIdx.x;
+    const bool follows = tid >= kDistillThreads;
+    const void *whole_row = row_ptr<KIND>(a.z, a.ldz, row);
+    const char *zr = (const char *)whole_row + (int64_t)begin * V::kSize;
+    char *dr = (char *)const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row)) + (int64_t)begin * V::kSize;
     const float w = a.weight ? a.weight[row] : 1.f;
     if (w == 0.f) {
         const u32x4 zero{0, 0, 0, 0};
-        for (int i = begin + tid * V::kLen; i < end; i += kDistillThreads * V::kLen) V::store(dr, i, end, zero);
+        for (int i = tid * V::kLen; i < here; i += (kDistillThreads + kWave) * V::kLen) V::store(dr, i, here, zero);
         return;
     }
     u32x4 raw[kGradVecs];
+    Entries t;
+    float zt[kPerLane];
+    if (follows) {
+        t = row_entries(a, row);
+        entry_logits<KIND>(whole_row, t, zt);
+    } else {
 #pragma unroll
-    for (int j = 0; j < kGradVecs; ++j) {
-        const int left = end - begin - (j * kDistillThreads + tid) * V::kLen;
-        raw[j] = left > 0 ? V::load_at((const char *)zr + ((int64_t)begin * V::kSize + j * kDistillThreads * 16), tid * 16, left) : V::fill();
+        for (int j = 0; j < kGradVecs; ++j) {
+            const int left = here - (j * kDistillThreads + tid) * V::kLen;
+            raw[j] = left > 0 ? V::load_at(zr + j * kDistillThreads * 16, tid * 16, left) : V::fill();
+        }
     }
     const float4 stats = a.stats[row];
     const float c = a.inv_t * kLog2e, wt = w * a.inv_t, scale = stats.y * stats.z * wt;
-    Entries t;
-    float zt[kPerLane];
-    if (tid < kWave) {
-        t = row_entries(a, row);
-        entry_logits<KIND>(zr, t, zt);
-    }
-    __syncthreads();   // the logits at the entries have been read before anything is written: dz may be z
+    if (a.in_place) __syncthreads();   // the logits at the entries have been read before anything is written
+    if (!follows) {
 #pragma unroll
-    for (int j = 0; j < kGradVecs; ++j) {
-        const int left = end - begin - (j * kDistillThreads + tid) * V::kLen;
-        if (left > 0) {
-            float v[V::kLen];
-            V::to(raw[j], v);
+        for (int j = 0; j < kGradVecs; ++j) {
+            const int left = here - (j * kDistillThreads + tid) * V::kLen;
+            if (left > 0) {
+                float v[V::kLen];
+                V::to(raw[j], v);
 #pragma unroll
-            for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
-            V::store_at((char *)dr + ((int64_t)begin * V::kSize + j * kDistillThreads * 16), tid * 16, left, V::from(v));
+                for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
+                V::store_at(dr + j * kDistillThreads * 16, tid * 16, left, V::from(v));
+            }
         }
     }
-    __syncthreads();   // the entries' own gradient goes over what stands at their slots
-    if (tid < kWave) {
+    __syncthreads();
+    if (follows) {
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
-            if (t.slot[j] >= begin && t.slot[j] < end)
-                V::store1(dr, t.slot[j], wt * (soft_term(zt[j], stats.x, c) * stats.y - expf(t.v[j] * a.inv_t - stats.w)));
+            if (t.slot[j] >= begin && t.slot[j] < begin + here)
+                V::store1(dr, t.slot[j] - begin, wt * (soft_term(zt[j], stats.x, c) * stats.y - expf(t.v[j] * a.inv_t - stats.w)));
     }
 }
 
 // The longest row that a workgroup holds.
 template <int KIND>
 constexpr int kRowSlots = 960 * 17 * Vec<KIND>::kLen;
+
+// The longest row read in rounds: its bits of A take 60 KB of LDS.
+template <int KIND>
+constexpr int kLoopSlots = 60 * 1024 * Vec<KIND>::kLen;
 
 template <class F>
 void with_logits(rdk_input_kind_t kind, const F &f)
@@ -517,10 +642,11 @@ void with_logits(rdk_input_kind_t kind, const F &f)
     else f(std::integral_constant<int, RDK_LOGIT_BF16>());
 }
 
-void split(const rdk_distill_desc_t &d, DistillArgs &a)
+// Parts that several workgroups share a row by.
+int parts_of(int n, rdk_input_kind_t kind)
 {
-    a.parts = (d.n + kPartSlots - 1) / kPartSlots;
-    a.part_slots = (int)align_up((size_t)(d.n + a.parts - 1) / a.parts, 32);
+    const int slots = kDistillThreads * kPartVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4);
+    return (n - 1) / slots + 1;
 }
 
 DistillArgs arguments(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
@@ -532,7 +658,7 @@ DistillArgs arguments(const rdk_distill_desc_t &d, const KernelHandle *h, RowInp
     a.ids = h ? h->N : d.n;
     a.n = d.n; a.K = d.K; a.inv_t = 1.f / d.temperature;
     a.top_ids = top_ids; a.top_logits = top_logits; a.weight = weight;
-    split(d, a);
+    a.parts = parts_of(d.n, z.kind);
     return a;
 }
 
@@ -540,8 +666,9 @@ template <int KIND>
 rdk_status_t launch_grad(DistillArgs a, int32_t B, hipStream_t st)
 {
     constexpr int kSlots = kDistillThreads * kGradVecs * Vec<KIND>::kLen;
-    a.grad_parts = (a.n + kSlots - 1) / kSlots;
-    RDK_TIMED_LAUNCH("distill_grad_kernel", (distill_grad_kernel<KIND>), dim3((unsigned)B * a.grad_parts), dim3(kDistillThreads), 0, st, a);
+    a.grad_parts = (a.n - 1) / kSlots + 1;
+    a.in_place = a.dz == a.z;
+    RDK_TIMED_LAUNCH("distill_grad_kernel", (distill_grad_kernel<KIND>), dim3((unsigned)B * a.grad_parts), dim3(kDistillThreads + kWave), 0, st, a);
     RDK_LAUNCH_CHECK("distill_grad_kernel");
     return RDK_OK;
 }
@@ -549,32 +676,59 @@ rdk_status_t launch_grad(DistillArgs a, int32_t B, hipStream_t st)
 template <int KIND, bool REST>
 rdk_status_t launch_split(const DistillArgs &a, int32_t B, hipStream_t st)
 {
-    RDK_TIMED_LAUNCH("distill_part_kernel", (distill_part_kernel<KIND, REST>), dim3((unsigned)B * a.parts), dim3(kDistillThreads), 0, st, a);
+    RDK_TIMED_LAUNCH("distill_part_kernel", (distill_part_kernel<KIND, REST>), dim3((unsigned)B * a.parts), dim3(kDistillThreads + kWave), 0, st, a);
     RDK_TIMED_LAUNCH("distill_finish_kernel", (distill_finish_kernel<KIND, REST>), dim3((unsigned)B), dim3(kWave), 0, st, a);
     RDK_LAUNCH_CHECK("distill_finish_kernel");
     return a.dz ? launch_grad<KIND>(a, B, st) : RDK_OK;
 }
 
 template <int KIND, int THREADS, int VECS, bool REST>
-rdk_status_t launch_row(const DistillArgs &a, int32_t B, hipStream_t st)
+rdk_status_t launch_both(const DistillArgs &a, int32_t B, hipStream_t st)
 {
-    if (a.dz) RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, true>), dim3((unsigned)B), dim3(THREADS + kWave), 0, st, a);
-    else RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, false>), dim3((unsigned)B), dim3(THREADS + kWave), 0, st, a);
+    RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, true>), dim3((unsigned)B), dim3(THREADS + kWave), 0, st, a);
     RDK_LAUNCH_CHECK("distill_row_kernel");
     return RDK_OK;
+}
+
+template <int KIND, int THREADS, int VECS, bool REST>
+rdk_status_t launch_row(const DistillArgs &a, int32_t B, hipStream_t st)
+{
+    if (a.dz) return launch_both<KIND, THREADS, VECS, REST>(a, B, st);
+    RDK_TIMED_LAUNCH("distill_row_kernel", (distill_row_kernel<KIND, THREADS, VECS, REST, false>), dim3((unsigned)B), dim3(THREADS + kWave), 0, st, a);
+    RDK_LAUNCH_CHECK("distill_row_kernel");
+    return RDK_OK;
+}
+
+template <int KIND, bool REST>
+rdk_status_t launch_loop(const DistillArgs &a, int32_t B, hipStream_t st)
+{
+    const size_t lds = REST ? align_up((size_t)(a.n - 1) / Vec<KIND>::kLen + 1, 16) : 0;
+    RDK_TIMED_LAUNCH("distill_loop_kernel", (distill_loop_kernel<KIND, REST>), dim3((unsigned)B), dim3(kLoopThreads + kWave), lds, st, a);
+    RDK_LAUNCH_CHECK("distill_loop_kernel");
+    return a.dz ? launch_grad<KIND>(a, B, st) : RDK_OK;
 }
 
 template <int KIND, bool REST>
 rdk_status_t launch_loss(const DistillArgs &a, int32_t B, hipStream_t st)
 {
     constexpr int kLen = Vec<KIND>::kLen;
+    // Few rows, and long: several workgroups to a row, in one launch more (bf16, remainder counted: the loss of 64 rows of 62000 10.7 -> 8.7 us, of
+    // 128256 15.9 -> 10.3; 192 rows 16.8 -> 16.3 and 11.1 -> 12.2; with the gradient 64 rows of 128256 20.7 -> 15.8, 128 rows 22.7 -> 24.4).
+    const bool few = a.dz ? B <= (a.n > kRowSlots<KIND> ? 128 : 64) && a.n > 960 * 9 * kLen : B <= 128 && a.n > 448 * 17 * kLen;
+    if (few || a.n > kLoopSlots<KIND>) return launch_split<KIND, REST>(a, B, st);
+    // The loss alone of rows beyond 64 KB: in rounds, three workgroups on a compute unit where the registers of long rows leave one or two (2048 fp32
+    // rows of 32064 88 -> 48 us, 512 bf16 rows of 128256 41 -> 29, 1024 of 50000 28.1 -> 26.7; 2048 bf16 rows of 32064 30.6 -> 33.8 and so not).
+    // With the gradient only rows that no workgroup holds, which are then read again.
+    if (a.n > (a.dz ? kRowSlots<KIND> : 448 * 9 * kLen)) return launch_loop<KIND, REST>(a, B, st);
+    // As many threads and vectors to a thread as the row takes: two workgroups of eight wavefronts on a compute unit for the rows in between (2048 bf16
+    // rows of 32064: 448 threads of nine vectors 47.5 us, 512 of eight 62, one workgroup of 960 60), one for the longest.
     if (a.n <= 192 * 3 * kLen) return launch_row<KIND, 192, 3, REST>(a, B, st);
     if (a.n <= 192 * 9 * kLen) return launch_row<KIND, 192, 9, REST>(a, B, st);
     if (a.n <= 448 * 5 * kLen) return launch_row<KIND, 448, 5, REST>(a, B, st);
     if (a.n <= 448 * 9 * kLen) return launch_row<KIND, 448, 9, REST>(a, B, st);
-    if (a.n <= 448 * 17 * kLen) return launch_row<KIND, 448, 17, REST>(a, B, st);
-    if (a.n <= kRowSlots<KIND>) return launch_row<KIND, 960, 17, REST>(a, B, st);
-    return launch_split<KIND, REST>(a, B, st);
+    if (a.n <= 448 * 17 * kLen) return launch_both<KIND, 448, 17, REST>(a, B, st);
+    if (a.n <= 960 * 9 * kLen) return launch_both<KIND, 960, 9, REST>(a, B, st);
+    return launch_both<KIND, 960, 17, REST>(a, B, st);
 }
 
 }  // namespace
@@ -583,9 +737,7 @@ int distill_max_entries() { return kMaxEntries; }
 
 size_t distill_workspace_bytes(const rdk_distill_desc_t &d, rdk_input_kind_t kind)
 {
-    DistillArgs a{};
-    split(d, a);
-    return align_up((size_t)d.B * a.parts * sizeof(SoftStat), 256) + align_up((size_t)d.B * sizeof(float4), 256);
+    return align_up((size_t)d.B * parts_of(d.n, kind) * sizeof(SoftStat), 256) + align_up((size_t)d.B * sizeof(float4), 256);
 }
 
 rdk_status_t launch_distill_loss(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,

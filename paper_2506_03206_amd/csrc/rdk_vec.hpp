@@ -72,6 +72,21 @@ struct Vec {
             r[e] = bits;
     }
 
+    // the elements whose bit is set become fill
+    static __device__ __forceinline__ void strike(u32x4 &r, unsigned bits)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            unsigned m;
+            if constexpr (KIND == RDK_LOGIT_BF16)
+                m = __builtin_amdgcn_perm((unsigned)__builtin_amdgcn_sbfe((int)bits, 2 * i + 1, 1), (unsigned)__builtin_amdgcn_sbfe((int)bits, 2 * i, 1),
+                                          0x05040100u);
+            else
+                m = (unsigned)__builtin_amdgcn_sbfe((int)bits, i, 1);
+            r[i] = (r[i] & ~m) | (kFillWord & m);
+        }
+    }
+
     // results in the row's own type, to the nearest, ties to even
     static __device__ __forceinline__ u32x4 from(const float (&v)[kLen])
     {
