@@ -33,17 +33,18 @@ struct SelectShared {
     int count, wave[16];
 };
 
-// The k largest of at(0) .. at(count - 1) (distinct entries, 0 for none) into sh.sorted, descending; returns how many there are.  By halving:
-// the k-th largest entry is found bit by bit, with a pass over the set for each, so it is right for any set and slow.
-template <int THREADS, class At>
-__device__ __forceinline__ int select_exact(const At &at, int64_t count, int k, SelectShared &sh)
+// The k largest of a workgroup's entries (distinct, 0 for none) into sh.sorted, descending; returns how many there are.  each(f) calls f with every
+// entry of the calling thread.  By halving: the k-th largest entry is found bit by bit, with a pass over the set for each, so it is right for
+// any set and slow.
+template <int THREADS, class Each>
+__device__ __forceinline__ int select_exact(const Each &each, int k, SelectShared &sh)
 {
     const int wid = threadIdx.x / kWave;
     uint64_t least = 0;
     for (int bit = 63; bit >= 0; --bit) {
         const uint64_t tried = least | ((uint64_t)1 << bit);
         int c = 0;
-        for (int64_t i = threadIdx.x; i < count; i += THREADS) c += at(i) >= tried;
+        each([&](uint64_t e) { c += e >= tried; });
         c = (int)wave_sum((float)c);       // counts above 2^24 lose their last bits, where only "at least k" matters
         __syncthreads();                   // sh.wave has been read
         if (lane_id() == 0) sh.wave[wid] = c;
@@ -54,10 +55,9 @@ __device__ __forceinline__ int select_exact(const At &at, int64_t count, int k, 
     }
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
-    for (int64_t i = threadIdx.x; i < count; i += THREADS) {
-        const uint64_t e = at(i);
+    each([&](uint64_t e) {
         if (e != 0 && e >= least) sh.list[atomicAdd(&sh.count, 1)] = e;   // entries are distinct: at most k
-    }
+    });
     __syncthreads();
     const int n = sh.count;
     if ((int)threadIdx.x < n) {

@@ -8,18 +8,20 @@ namespace rdk {
 namespace {
 
 constexpr int kTopThreads = 256;
-constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+constexpr float kLog2e = 1.44269504088896341f;
 
 constexpr int kRoundVecs = 4;          // 16-byte vectors of a lane in a round
-constexpr int kQueue = 1024;           // vectors noted, entries sorted: what exceeds it takes the slow way
-constexpr int kMergeEntries = 2048;    // of a row's parts together
-constexpr int kBeamEntries = 4096;     // of a request's beams and their parts together
+constexpr int kQueue = 2048, kFound = 1024;   // vectors noted, entries sorted: what exceeds these takes the slow way
+constexpr int kMergeEntries = 4096;    // of a row's parts together
+constexpr int kBeamEntries = 16384;    // of a request's beams and their parts together
+constexpr int kTopWaves = kTopThreads / kWave;
 
 struct TopArgs {
     const void *x;
     int64_t ldx;
     int N, k, parts, part_len;
-    float inv_t, c, limit;  // c = log2(e) / temperature; rows with a maximum beyond +-limit take the slow way
+    float inv_t, c;         // c = log2(e) / temperature
+    float limit, margin;    // rows with a maximum beyond +-limit take the slow way; 60 / c
     // rows of beams that have no candidates among the ids are passed over
     const float *scores;
     const uint8_t *finished;
@@ -31,61 +33,52 @@ struct TopArgs {
 
 struct TopShared {
     SelectShared slow;
-    uint64_t found[kQueue];
-    uint32_t keys[kTopThreads], queue[kQueue];
-    float wave_m[kTopThreads / kWave], wave_s[kTopThreads / kWave];
-    float tau;
+    uint64_t found[kFound];
+    uint32_t queue[kQueue];
+    float wave_m[kTopWaves], wave_s[kTopWaves], bound[kTopWaves];
     int queued, count;
 };
 
-// A lower bound of the k-th largest of the values whose largest per lane are in sh.keys, to sixteen bits: the k-th largest of those.  By wave 0.
-template <int KIND>
-__device__ __forceinline__ float bound_of(const uint32_t (&own)[kTopThreads / kWave], int k)
+// The nth largest of the keys of 64 lanes, to their highest BITS bits, by halving.  (Rolled up: code that runs once is fetched while it runs.)
+template <int BITS>
+__device__ __forceinline__ uint32_t wave_nth(uint32_t key, int nth)
 {
+    key >>= 32 - BITS;
     uint32_t found = 0;
-#pragma unroll
-    for (int bit = 15; bit >= 0; --bit) {
+#pragma unroll 4
+    for (int bit = BITS - 1; bit >= 0; --bit) {
         const uint32_t tried = found | (1u << bit);
-        int n = 0;
-#pragma unroll
-        for (int i = 0; i < kTopThreads / kWave; ++i) n += __popcll(__ballot(own[i] >= tried));
-        if (n >= k) found = tried;
+        if (__popcll(__ballot(key >= tried)) >= nth) found = tried;
     }
-    const uint32_t key = found << 16;
-    // fewer than k lanes have an unmasked value: every unmasked one is wanted
-    if (key <= masked_key<KIND>()) return KIND == RDK_PROB_F32 ? __uint_as_float(1u) : -3.402823466e38f;
-    return key_value(key);
+    return found << (32 - BITS);
 }
 
-// Statistics of a part (m the largest value, s the sum of exp((x - m) / T)) and its k largest by halving: for rows that the fast way does not hold.
+// The value that the nth largest of the lanes' largest values has, as a number no entry that is wanted lies below.  With fewer lanes that have unmasked
+// values: every unmasked value is wanted.
 template <int KIND>
-__device__ __noinline__ int slow_part(const TopArgs &a, const void *xr, int begin, int end, TopShared &sh, SoftStat *stat)
+__device__ __forceinline__ float wave_bound(float largest, int nth)
 {
-    float m = KIND == RDK_PROB_F32 ? 0.f : -INFINITY, s = 0.f;
-    for (int i = begin + (int)threadIdx.x; i < end; i += kTopThreads) m = fmaxf(m, load1<KIND>(xr, i));
-    m = wave_max(m);
-    __syncthreads();
-    if (lane_id() == 0) sh.wave_m[threadIdx.x / kWave] = m;
-    __syncthreads();
-    for (int w = 0; w < kTopThreads / kWave; ++w) m = fmaxf(m, sh.wave_m[w]);
-    const float ref = weight_reference(m);
+    const uint32_t key = wave_nth<KIND == RDK_LOGIT_BF16 ? 16 : 32>(order_key(largest), nth);   // (a bf16 value's key ends in sixteen equal bits)
+    if (key <= masked_key<KIND>()) return KIND == RDK_PROB_F32 ? __uint_as_float(1u) : -3.402823466e38f;
+    return key_value(KIND == RDK_LOGIT_BF16 && !(key >> 31) ? key | 0xFFFFu : key);
+}
+
+// The sum of exp((x - m) / T) over a part, for a largest value m so far from zero that the product with 1 / T leaves the range.
+template <int KIND>
+__device__ __forceinline__ float wide_sum(const TopArgs &a, const void *xr, int begin, int end, float m, TopShared &sh)
+{
+    float s = 0.f;
     for (int i = begin + (int)threadIdx.x; i < end; i += kTopThreads) {
         const float x = load1<KIND>(xr, i);
-        s += KIND == RDK_PROB_F32 ? x : __builtin_amdgcn_exp2f((x - ref) * a.c);
+        s += KIND == RDK_PROB_F32 ? x : __builtin_amdgcn_exp2f((x - m) * a.c);
     }
     s = wave_sum(s);
+    __syncthreads();
     if (lane_id() == 0) sh.wave_s[threadIdx.x / kWave] = s;
     __syncthreads();
     s = 0.f;
-    for (int w = 0; w < kTopThreads / kWave; ++w) s += sh.wave_s[w];
-    *stat = SoftStat{m, s};
-    const uint32_t masked = masked_key<KIND>();
-    return select_exact<kTopThreads>(
-        [&](int64_t i) {
-            const uint32_t key = order_key(load1<KIND>(xr, begin + i));
-            return key > masked ? entry_of(key, (uint32_t)(begin + i)) : 0;
-        },
-        end - begin, a.k, sh.slow);
+    for (int w = 0; w < kTopWaves; ++w) s += sh.wave_s[w];
+    return s;
 }
 
 __device__ __forceinline__ void note(uint32_t *queue, int *count, uint32_t what)
@@ -95,14 +88,48 @@ __device__ __forceinline__ void note(uint32_t *queue, int *count, uint32_t what)
 }
 
 // The k largest of the entries found[0 .. n - 1] in sorted, descending, by counting for each how many are larger.
+template <int THREADS>
 __device__ __forceinline__ void sort_found(const uint64_t *found, int n, int k, uint64_t *sorted)
 {
-    for (int i = threadIdx.x; i < n; i += kTopThreads) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         const uint64_t own = found[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += found[j] > own;
+        int rank = 0, j = 0;
+#pragma unroll 1
+        for (; j + 8 <= n; j += 8)   // eight reads in flight
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rank += found[j + e] > own;
+#pragma unroll 1
+        for (; j < n; ++j) rank += found[j] > own;
         if (rank < k) sorted[rank] = own;
     }
+}
+
+// The first entries in order of ids whose value is exactly x, behind the `have` in sh.found until there are k.  By one wavefront.
+template <int KIND>
+__device__ __forceinline__ int take_equal(const void *xr, int begin, int whole, int end, float x, int have, int k, TopShared &sh)
+{
+    typedef Vec<KIND> V;
+    const uint64_t before = ((uint64_t)1 << lane_id()) - 1;
+#pragma unroll 1
+    for (int base = 0; base <= whole && have < k; base += kWave) {
+        const int at = base + lane_id(), i = begin + at * V::kLen;
+        const int left = at < whole ? V::kLen : at == whole ? end - i : 0;   // the vector that is not whole is the last
+        uint32_t equal = 0;
+        for (int e = 0; e < left; ++e) equal |= (uint32_t)(load1<KIND>(xr, i + e) == x) << e;
+        int rank = have, all = 0;
+        for (int e = 0; e < V::kLen; ++e) {
+            const uint64_t who = __ballot(equal >> e & 1);
+            rank += __popcll(who & before);
+            all += __popcll(who);
+        }
+        for (int e = 0; e < left; ++e)
+            if (equal >> e & 1) {
+                if (rank < k) sh.found[rank] = entry_of(order_key(x), (uint32_t)(i + e));
+                ++rank;
+            }
+        have += all;
+    }
+    return min(have, k);
 }
 
 template <int KIND>
@@ -119,97 +146,108 @@ __device__ __forceinline__ void write_row(int32_t *ids, float *values, float *ls
         lse[row] = KIND == RDK_PROB_F32 ? logf(st.s) : st.s == 0.f ? -INFINITY : weight_reference(st.m) * inv_t + logf(st.s);
 }
 
-// One pass over a part of a row.  Every lane keeps the largest value of its own; the k-th largest of those 256 is a lower bound of the part's k-th
-// largest that only some k of the part's values exceed, so few vectors have to be looked at again.  The bound is found after the first
-// round of loads and anew whenever the values seen have doubled; a vector whose largest value reaches it is noted by its place.  What was
-// noted is read again at the end (out of the cache), sifted by the final bound, and sorted.
+// One pass over a part of a row.  Every lane keeps the largest value of its own; if each of the four wavefronts has k / 4 lanes whose largest reaches
+// a bound of its own, the least of the four bounds is reached by k of the part's values, and few more exceed it: it is a lower bound of the k-th
+// largest.  It is found after the first round of loads and anew as the values seen grow by half (a wavefront reads what the others last
+// wrote: bounds only rise, so an old one is a bound too, and nothing waits); a vector whose largest value reaches it is noted by its place.
+// What was noted is read again at the end (out of the cache), sifted by the last bound, and sorted.  Where more was noted than there is room for
+// (values that rise along the row) the whole part is sifted; where more reaches the last bound than there is room for, it is the k-th
+// largest value itself and met by many (what masks leave): those above it are taken, and the first of those that equal it.
+// Only values that crowd in few lanes, and NaN, leave the search by halving.
 template <int KIND>
 __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
 {
     typedef Vec<KIND> V;
-    constexpr int kWaves = kTopThreads / kWave, kRound = kTopThreads * kRoundVecs * V::kLen;
+    constexpr int kRound = kTopThreads * kRoundVecs;    // vectors
     __shared__ TopShared sh;
     const int64_t row = blockIdx.x / a.parts;
-    const int part = blockIdx.x % a.parts, begin = part * a.part_len, end = min(a.N, begin + a.part_len);
+    const int part = blockIdx.x % a.parts, begin = part * a.part_len, end = max(begin, min(a.N, begin + a.part_len));
     const int tid = threadIdx.x, wid = tid / kWave;
     if (a.finished && a.finished[row]) return;
     if (a.scores && a.scores[row] == -INFINITY) return;
     const void *xr = row_ptr<KIND>(a.x, a.ldx, row);
-    const float none = KIND == RDK_PROB_F32 ? 0.f : -INFINITY;
-    float m = none, s = 0.f, ref = 0.f;     // ref: reference of the lane's exponents, times c
-    float tau = INFINITY;
-    u32x4 raw[kRoundVecs];
-    auto load_round = [&](int base) {
-        if (base + kRound <= end) {
+    const char *from = (const char *)xr + (int64_t)begin * V::kSize;
+    const int whole = (end - begin) / V::kLen, behind = (end - begin) % V::kLen;   // whole vectors; a value behind them is one thread's each
+    // wavefronts that have values at all, and how many lanes of each have to reach its bound
+    const int waves = min((max(whole, 1) + kWave - 1) / kWave, kTopWaves), share = (a.k + waves - 1) / waves;
+    constexpr float none = KIND == RDK_PROB_F32 ? 0.f : -INFINITY;
+    float m = none, s = 0.f, ref = 0.f, high = -INFINITY;   // ref: reference of the lane's exponents, times c; high: where it is replaced
+    float last = none;
+    // Exponents are relative to a value that the lane has seen, not the largest: it is replaced only when a vector exceeds it by 2^60, so the
+    // maximum is nothing that the exponentials wait for.
+    auto raise = [&](float x) __attribute__((always_inline)) {
+        const float held = fminf(fmaxf(x, -a.limit), a.limit), to = held * a.c;
+        s = s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f(ref - to);
+        ref = to;
+        high = held + a.margin;
+    };
+    auto publish = [&]() __attribute__((always_inline)) {
+        const float b = wid < waves ? wave_bound<KIND>(m, share) : INFINITY;
+        if (lane_id() == 0) __hip_atomic_store(&sh.bound[wid], b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    };
+    auto least_bound = [&]() __attribute__((always_inline)) {
+        float b = INFINITY;
 #pragma unroll
-            for (int j = 0; j < kRoundVecs; ++j) raw[j] = *(const u32x4_any *)((const char *)xr + (int64_t)(base + (j * kTopThreads + tid) * V::kLen) * V::kSize);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kRoundVecs; ++j) {
-                const int i = base + (j * kTopThreads + tid) * V::kLen;
-                raw[j] = i < end ? V::load(xr, i, end) : V::fill();
-            }
-        }
+        for (int w = 0; w < kTopWaves; ++w) b = fminf(b, __hip_atomic_load(&sh.bound[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
+        return b;
     };
     if (tid == 0) sh.queued = sh.count = 0;
-    load_round(begin);
+    if (tid < behind) {
+        last = load1<KIND>(from, whole * V::kLen + tid);
+        m = fmaxf(m, last);
+        if (KIND == RDK_PROB_F32) {
+            s = last;
+        } else {
+            if (last > high) raise(last);
+            s = __builtin_amdgcn_exp2f(fmaf(last, a.c, -ref));
+        }
+    }
+    float tau = INFINITY;
     int next_bound = 0, round = 0;
-    for (int base = begin; base < end; base += kRound, ++round) {
+    u32x4 raw[kRoundVecs];
+#pragma unroll 1
+    for (int base = -kRound; base < whole; base += kRound) {
         u32x4 now[kRoundVecs];
 #pragma unroll
         for (int j = 0; j < kRoundVecs; ++j) now[j] = raw[j];
-        if (base + kRound < end) load_round(base + kRound);
+        if (base + kRound < whole) {   // the round ahead
+#pragma unroll
+            for (int j = 0; j < kRoundVecs; ++j) {
+                raw[j] = V::fill();
+                if (base + kRound + j * kTopThreads + tid < whole)
+                    raw[j] = *(const u32x4_any *)(from + ((int64_t)base + kRound + j * kTopThreads) * 16 + (uint32_t)tid * 16);
+            }
+        }
+        if (base < 0) continue;
         float vm[kRoundVecs];
-        float v[V::kLen];
-        float mx = m;
 #pragma unroll
         for (int j = 0; j < kRoundVecs; ++j) {
+            float v[V::kLen], sum = 0.f;
             V::to(now[j], v);
-            vm[j] = v[0];
+            vm[j] = V::largest(v, none);
+            if constexpr (KIND == RDK_PROB_F32) {
 #pragma unroll
-            for (int e = 1; e < V::kLen; ++e) vm[j] = fmaxf(vm[j], v[e]);
-            mx = fmaxf(mx, vm[j]);
-        }
-        if constexpr (KIND == RDK_PROB_F32) {
+                for (int e = 0; e < V::kLen; ++e) sum += v[e];
+            } else {
+                if (vm[j] > high) raise(vm[j]);
 #pragma unroll
-            for (int j = 0; j < kRoundVecs; ++j) {
-                V::to(now[j], v);
-#pragma unroll
-                for (int e = 0; e < V::kLen; ++e) s += v[e];
+                for (int e = 0; e < V::kLen; ++e) sum += __builtin_amdgcn_exp2f(fmaf(v[e], a.c, -ref));
             }
-        } else {
-            const float to = fminf(fmaxf(mx, -a.limit), a.limit) * a.c;
-            s = s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f(ref - to);
-            ref = to;
-#pragma unroll
-            for (int j = 0; j < kRoundVecs; ++j) {
-                V::to(now[j], v);
-                float part_sum = 0.f;
-#pragma unroll
-                for (int e = 0; e < V::kLen; ++e) part_sum += __builtin_amdgcn_exp2f(fmaf(v[e], a.c, -to));
-                s += part_sum;
-            }
+            s += sum;
+            m = fmaxf(m, vm[j]);
         }
-        m = mx;
-        if (round == next_bound) {      // the same for the whole workgroup
-            next_bound = 2 * round + 1;
-            sh.keys[tid] = order_key(m) >> 16;
-            __syncthreads();
-            if (wid == 0) {
-                uint32_t own[kWaves];
-#pragma unroll
-                for (int i = 0; i < kWaves; ++i) own[i] = sh.keys[i * kWave + lane_id()];
-                const float bound = bound_of<KIND>(own, a.k);
-                if (tid == 0) sh.tau = bound;
-            }
-            __syncthreads();
-            tau = sh.tau;
+        if (round == next_bound) {
+            next_bound = round + 1 + round / 2;
+            publish();
+            if (round == 0) __syncthreads();
+            tau = least_bound();
         }
+        ++round;
 #pragma unroll
         for (int j = 0; j < kRoundVecs; ++j)
-            if (vm[j] >= tau) note(sh.queue, &sh.queued, (uint32_t)(base - begin) / V::kLen + j * kTopThreads + tid);
+            if (vm[j] >= tau) note(sh.queue, &sh.queued, (uint32_t)(base + j * kTopThreads + tid));
     }
-    // statistics of the part
+    // statistics of the part, and its last bound
     const float wave_m = wave_max(m);
     if constexpr (KIND != RDK_PROB_F32) {
         const float to = fminf(fmaxf(wave_m, -a.limit), a.limit) * a.c;
@@ -220,110 +258,161 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         sh.wave_m[wid] = wave_m;
         sh.wave_s[wid] = wave_s;
     }
-    sh.keys[tid] = order_key(m) >> 16;
+    if (round != 1) publish();
     __syncthreads();
+    tau = least_bound();
     SoftStat stat{none, 0.f};
-    for (int w = 0; w < kWaves; ++w) stat.m = fmaxf(stat.m, sh.wave_m[w]);
+#pragma unroll
+    for (int w = 0; w < kTopWaves; ++w) stat.m = fmaxf(stat.m, sh.wave_m[w]);
     if constexpr (KIND == RDK_PROB_F32) {
-        for (int w = 0; w < kWaves; ++w) stat.s += sh.wave_s[w];
+#pragma unroll
+        for (int w = 0; w < kTopWaves; ++w) stat.s += sh.wave_s[w];
     } else {
         const float held = fminf(fmaxf(stat.m, -a.limit), a.limit), to = held * a.c;
-        for (int w = 0; w < kWaves; ++w) {
-            const float from = fminf(fmaxf(sh.wave_m[w], -a.limit), a.limit) * a.c;
-            stat.s += sh.wave_s[w] == 0.f ? 0.f : sh.wave_s[w] * __builtin_amdgcn_exp2f(from - to);
+#pragma unroll
+        for (int w = 0; w < kTopWaves; ++w) {
+            const float by = fminf(fmaxf(sh.wave_m[w], -a.limit), a.limit) * a.c;
+            stat.s += sh.wave_s[w] == 0.f ? 0.f : sh.wave_s[w] * __builtin_amdgcn_exp2f(by - to);
         }
         stat.s *= __builtin_amdgcn_exp2f(-fmaf(held, a.c, -to));   // the rounding of the reference itself
     }
-    const bool slow_sum = stat.s != stat.s || (stat.m > -INFINITY && fabsf(stat.m) > a.limit);   // a NaN, or values whose exponents leave the range
-    if (wid == 0) {
-        uint32_t own[kWaves];
-#pragma unroll
-        for (int i = 0; i < kWaves; ++i) own[i] = sh.keys[i * kWave + lane_id()];
-        const float bound = bound_of<KIND>(own, a.k);
-        if (tid == 0) sh.tau = bound;
-    }
-    __syncthreads();
-    tau = sh.tau;
+    if (stat.m > -INFINITY && fabsf(stat.m) > a.limit) stat.s = wide_sum<KIND>(a, xr, begin, end, stat.m, sh);
+    const bool nan = stat.s != stat.s;
     const int queued = sh.queued;
-    for (int q = tid; q < min(queued, kQueue); q += kTopThreads) {
-        const int i = begin + (int)sh.queue[q] * V::kLen;
-        float v[V::kLen];
-        V::to(V::load(xr, i, end), v);
+    bool all = queued > kQueue, above = false;   // the whole part; only what lies above the bound
+    int n = 0;
+    float least = tau;
+#pragma unroll 1
+    while (!nan) {
+        const int count = all ? whole : queued;
+        for (int q = tid; q < count; q += kTopThreads) {
+            const int at = all ? q : (int)sh.queue[q];
+            float v[V::kLen];
+            V::to(*(const u32x4_any *)(from + (int64_t)at * 16), v);
 #pragma unroll
-        for (int e = 0; e < V::kLen; ++e)
-            if (v[e] >= tau) {
-                const int at = atomicAdd(&sh.count, 1);
-                if (at < kQueue) sh.found[at] = entry_of(order_key(v[e]), (uint32_t)(i + e));
-            }
+            for (int e = 0; e < V::kLen; ++e)
+                if (v[e] >= least) {
+                    const int to = atomicAdd(&sh.count, 1);
+                    if (to < kFound) sh.found[to] = entry_of(order_key(v[e]), (uint32_t)(begin + at * V::kLen + e));
+                }
+        }
+        if (tid < behind && last >= least) {
+            const int to = atomicAdd(&sh.count, 1);
+            if (to < kFound) sh.found[to] = entry_of(order_key(last), (uint32_t)(begin + whole * V::kLen + tid));
+        }
+        __syncthreads();
+        n = sh.count;
+        if (n <= kFound || above) break;
+        all = above = true;
+        least = key_value(order_key(tau) + 1);
+        __syncthreads();
+        if (tid == 0) sh.count = 0;
+        __syncthreads();
     }
-    __syncthreads();
-    int n = sh.count;
-    const uint64_t *sorted = sh.slow.sorted;
-    if (slow_sum || queued > kQueue || n > kQueue) {
-        n = slow_part<KIND>(a, xr, begin, end, sh, &stat);
+    if (above && n < a.k) {
+        __syncthreads();
+        if (wid == 0) {
+            const int filled = take_equal<KIND>(xr, begin, whole, end, tau, n, a.k, sh);
+            if (tid == 0) sh.count = filled;
+        }
+        __syncthreads();
+        n = sh.count;
+    }
+    if (nan || n > kFound) {
+        const uint32_t masked = masked_key<KIND>();
+        n = select_exact<kTopThreads>(
+            [&](auto f) {
+                for (int i = begin + tid; i < end; i += kTopThreads) {
+                    const uint32_t key = order_key(load1<KIND>(xr, i));
+                    f(key > masked ? entry_of(key, (uint32_t)i) : (uint64_t)0);
+                }
+            },
+            a.k, sh.slow);
     } else {
+        sort_found<kTopThreads>(sh.found, n, a.k, sh.slow.sorted);
         n = min(n, a.k);
-        sort_found(sh.found, sh.count, a.k, sh.slow.sorted);
         __syncthreads();
     }
     if (a.entries) {
-        if (tid < a.k) a.entries[(row * a.parts + part) * a.k + tid] = tid < n ? sorted[tid] : 0;
+        if (tid < a.k) a.entries[(row * a.parts + part) * a.k + tid] = tid < n ? sh.slow.sorted[tid] : 0;
         if (tid == 0) a.stat[row * a.parts + part] = stat;
         return;
     }
-    write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sorted, n, stat);
+    write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, stat);
 }
 
-// Partial statistics of a row brought together, by every lane of a wavefront alike.
+// Partial statistics of a row brought together, by a wavefront.
 template <int KIND>
 __device__ __forceinline__ SoftStat merge_stats(const SoftStat *stat, int parts, float c)
 {
-    SoftStat r{KIND == RDK_PROB_F32 ? 0.f : -INFINITY, 0.f};
-    for (int p = 0; p < parts; ++p) r.m = fmaxf(r.m, stat[p].m);
-    for (int p = 0; p < parts; ++p) {
+    constexpr float none = KIND == RDK_PROB_F32 ? 0.f : -INFINITY;
+    SoftStat r{none, 0.f};
+    for (int p = lane_id(); p < parts; p += kWave) {
         const SoftStat o = stat[p];
-        if (KIND == RDK_PROB_F32) r.s += o.s;
-        else r.s += o.s == 0.f ? 0.f : o.s * __builtin_amdgcn_exp2f((weight_reference(o.m) - weight_reference(r.m)) * c);
+        if (KIND == RDK_PROB_F32) {
+            r.m = fmaxf(r.m, o.m);
+            r.s += o.s;
+        } else {
+            const float m = fmaxf(r.m, o.m), ref = weight_reference(m);
+            r.s = (r.s == 0.f ? 0.f : r.s * __builtin_amdgcn_exp2f((weight_reference(r.m) - ref) * c)) +
+                  (o.s == 0.f ? 0.f : o.s * __builtin_amdgcn_exp2f((weight_reference(o.m) - ref) * c));
+            r.m = m;
+        }
     }
-    return r;
+    const float m = wave_max(r.m);
+    if (KIND != RDK_PROB_F32) r.s = r.s == 0.f ? 0.f : r.s * __builtin_amdgcn_exp2f((weight_reference(r.m) - weight_reference(m)) * c);
+    return SoftStat{m, wave_sum(r.s)};
 }
 
-// The k largest of `count` entries in LDS (0: none), in sh.slow.sorted, by the same bound.  Returns how many there are.
-__device__ __forceinline__ int select_entries(const uint64_t *entries, int count, int k, TopShared &sh)
+template <int THREADS>
+struct MergeShared {
+    SelectShared slow;
+    uint64_t found[kFound];
+    uint32_t keys[THREADS];
+    int count;
+};
+
+// The k largest of the workgroup's entries (EACH to a thread, 0: none) in sh.slow.sorted.  Returns how many there are.  As above, but the threads'
+// largest are looked at together: the wavefronts' shares of beams are nothing like alike.
+template <int THREADS, int EACH>
+__device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int k, MergeShared<THREADS> &sh)
 {
-    const int tid = threadIdx.x, wid = tid / kWave;
-    uint32_t best = 0;
-    for (int i = tid; i < count; i += kTopThreads) best = max(best, entry_key(entries[i]));
-    sh.keys[tid] = best >> 16;
+    constexpr int kWaves = THREADS / kWave;
+    const int tid = threadIdx.x;
+    uint64_t best = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) best = own[i] > best ? own[i] : best;
+    sh.keys[tid] = entry_key(best);
     if (tid == 0) sh.count = 0;
     __syncthreads();
-    if (wid == 0) {
-        uint32_t own[kTopThreads / kWave], found = 0;
+    uint32_t keys[kWaves], found = 0;   // every wavefront finds the k-th largest by itself
 #pragma unroll
-        for (int i = 0; i < kTopThreads / kWave; ++i) own[i] = sh.keys[i * kWave + lane_id()];
+    for (int w = 0; w < kWaves; ++w) keys[w] = sh.keys[w * kWave + lane_id()];
+#pragma unroll 2
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t tried = found | (1u << bit);
+        int n = 0;
 #pragma unroll
-        for (int bit = 15; bit >= 0; --bit) {
-            const uint32_t tried = found | (1u << bit);
-            int n = 0;
-#pragma unroll
-            for (int i = 0; i < kTopThreads / kWave; ++i) n += __popcll(__ballot(own[i] >= tried));
-            if (n >= k) found = tried;
-        }
-        if (tid == 0) sh.queued = (int)found;
+        for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(keys[w] >= tried));
+        if (n >= k) found = tried;
     }
-    __syncthreads();
-    const uint64_t least = max((uint64_t)(uint32_t)sh.queued << 48, (uint64_t)1);
-    for (int i = tid; i < count; i += kTopThreads) {
-        const uint64_t e = entries[i];
-        if (e >= least) {
+    const uint64_t least = found ? (uint64_t)found << 32 : 1;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+        if (own[i] >= least) {
             const int at = atomicAdd(&sh.count, 1);
-            if (at < kQueue) sh.found[at] = e;
+            if (at < kFound) sh.found[at] = own[i];
         }
-    }
     __syncthreads();
     const int n = sh.count;
-    if (n > kQueue) return select_exact<kTopThreads>([&](int64_t i) { return entries[i]; }, count, k, sh.slow);
-    sort_found(sh.found, n, k, sh.slow.sorted);
+    if (n > kFound)   // thousands that tie with the k-th
+        return select_exact<THREADS>(
+            [&](auto f) {
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) f(own[i]);
+            },
+            k, sh.slow);
+    sort_found<THREADS>(sh.found, n, k, sh.slow.sorted);
     __syncthreads();
     return min(n, k);
 }
@@ -337,18 +426,24 @@ struct TopMergeArgs {
     float *values, *lse;
 };
 
-// The parts of a row brought together.
-template <int KIND>
+// The parts of a row brought together.  Entries are dealt to the threads place by place of the sorted lists (the first of every part, then the
+// second, ...): the largest are with different threads then, and the bound is close.
+template <int KIND, int EACH>
 __global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a)
 {
-    __shared__ TopShared sh;
-    __shared__ uint64_t entries[kMergeEntries];
+    __shared__ MergeShared<kTopThreads> sh;
     const int64_t row = blockIdx.x;
     const int count = a.parts * a.k;
-    for (int i = threadIdx.x; i < count; i += kTopThreads) entries[i] = a.entries[row * count + i];
-    __syncthreads();
-    const int n = select_entries(entries, count, a.k, sh);
-    write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, merge_stats<KIND>(a.stat + row * a.parts, a.parts, a.c));
+    uint64_t own[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int at = i * kTopThreads + (int)threadIdx.x;
+        own[i] = at < count ? a.entries[row * count + at % a.parts * a.k + at / a.parts] : 0;
+    }
+    SoftStat stat{0.f, 0.f};
+    if (threadIdx.x < kWave) stat = merge_stats<KIND>(a.stat + row * a.parts, a.parts, a.c);
+    const int n = select_entries<kTopThreads, EACH>(own, a.k, sh);
+    write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, stat);
 }
 
 struct BeamArgs {
@@ -363,41 +458,50 @@ struct BeamArgs {
 };
 
 // One request: scores of its beams' candidates, and the K best of them.
-template <int KIND>
-__global__ __launch_bounds__(kTopThreads) void beam_merge_kernel(BeamArgs a)
+template <int KIND, int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamArgs a)
 {
-    __shared__ TopShared sh;
+    __shared__ MergeShared<THREADS> sh;
     __shared__ float beam_m[kWave], beam_log[kWave], beam_score[kWave];
     __shared__ int beam_state[kWave];        // 0: no candidates, 1: finished, 2: live
-    extern __shared__ uint64_t scored[];     // [W, parts, k]
     const int64_t g = blockIdx.x, b0 = g * a.W;
-    const int tid = threadIdx.x, per = a.parts * a.k, count = a.W * per;
-    if (tid < a.W) {
-        const float score = a.scores[b0 + tid];
-        const int state = score == -INFINITY ? 0 : a.finished && a.finished[b0 + tid] ? 1 : 2;
-        beam_score[tid] = score;
-        beam_state[tid] = state;
-        if (state == 2) {
-            const SoftStat st = merge_stats<KIND>(a.stat + (b0 + tid) * a.parts, a.parts, kLog2e);
-            beam_m[tid] = weight_reference(st.m);
-            beam_log[tid] = KIND == RDK_PROB_F32 ? st.s : logf(st.s);
+    const int tid = threadIdx.x, lists = a.W * a.parts, count = lists * a.k;
+    uint64_t own[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {         // (of beams without a row this is whatever lay there, and not used)
+        const int at = i * THREADS + tid;
+        own[i] = at < count ? a.entries[b0 * a.parts * a.k + at % lists * a.k + at / lists] : 0;
+    }
+    for (int w = tid / kWave; w < a.W; w += THREADS / kWave) {
+        const float score = a.scores[b0 + w];
+        const int state = score == -INFINITY ? 0 : a.finished && a.finished[b0 + w] ? 1 : 2;
+        SoftStat st{0.f, 0.f};
+        if (state == 2) st = merge_stats<KIND>(a.stat + (b0 + w) * a.parts, a.parts, kLog2e);
+        if (lane_id() == 0) {
+            beam_score[w] = score;
+            beam_state[w] = state;
+            beam_m[w] = weight_reference(st.m);
+            beam_log[w] = KIND == RDK_PROB_F32 ? st.s : logf(st.s);
         }
     }
     __syncthreads();
-    for (int i = tid; i < count; i += kTopThreads) {
-        const int w = i / per, state = beam_state[w];
-        uint64_t e = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int at = i * THREADS + tid, list = at % lists, w = list / a.parts;
+        const int state = at < count ? beam_state[w] : 0;
+        uint64_t e = own[i];
         if (state == 1) {
-            if (i == w * per) e = entry_of(order_key(beam_score[w]), (uint32_t)w * a.N + a.eos);
-        } else if (state == 2 && (e = a.entries[b0 * per + i]) != 0) {
+            e = at / lists == 0 && list == w * a.parts ? entry_of(order_key(beam_score[w]), (uint32_t)w * a.N + a.eos) : 0;
+        } else if (state == 2 && e != 0) {
             const float x = key_value(entry_key(e));
             const float score = beam_score[w] + (KIND == RDK_PROB_F32 ? logf(x / beam_log[w]) : (x - beam_m[w]) - beam_log[w]);
             e = score == -INFINITY ? 0 : entry_of(order_key(score), (uint32_t)w * a.N + entry_id(e));
+        } else {
+            e = 0;
         }
-        scored[i] = e;
+        own[i] = e;
     }
-    __syncthreads();
-    const int n = select_entries(scored, count, a.K, sh);
+    const int n = select_entries<THREADS, EACH>(own, a.K, sh);
     if (tid < a.K) {
         const bool in = tid < n;
         const uint64_t e = in ? sh.slow.sorted[tid] : 0;
@@ -449,6 +553,7 @@ TopArgs part_args(RowInput x, int N, int k, int parts, float temperature)
     a.part_len = (int)align_up(((size_t)N + parts - 1) / parts, 64);
     a.inv_t = 1.f / temperature;
     a.c = a.inv_t * kLog2e;
+    a.margin = 60.f / a.c;
     a.limit = 1.2676506e30f / (a.c > 1.f ? a.c : 1.f);   // 2^100: the product with c stays in range
     return a;
 }
@@ -481,8 +586,12 @@ rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, flo
     with_kind(x.kind, [&](auto kind) {
         RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<decltype(kind)::value>), dim3((unsigned)d.B * parts), dim3(kTopThreads), 0, st, a);
         if (parts > 1) {
+            constexpr int KIND = decltype(kind)::value;
             const TopMergeArgs m{a.entries, a.stat, d.k, parts, a.inv_t, a.c, ids, values, lse};
-            RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<decltype(kind)::value>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m);
+            if (parts * d.k <= 4 * kTopThreads)
+                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 4>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m);
+            else
+                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 16>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m);
         }
     });
     RDK_LAUNCH_CHECK("topk_part_kernel");
@@ -515,17 +624,17 @@ rdk_status_t launch_beam_select(const rdk_beam_desc_t &d, RowInput x, const floa
     b.entries = w.entries; b.stat = w.stat; b.scores = scores; b.finished = finished;
     b.W = d.W; b.N = d.N; b.k = k; b.K = d.K; b.parts = parts; b.eos = d.eos;
     b.scores_out = scores_out; b.parent = parent; b.token = token; b.finished_out = finished_out;
-    rdk_status_t rc = RDK_OK;
     with_kind(x.kind, [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        static LdsGrant grant;
-        rc = grant((const void *)&beam_merge_kernel<KIND>, kMaxTop * kWave * sizeof(uint64_t));
-        if (rc != RDK_OK) return;
         RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<KIND>), dim3((unsigned)(d.G * d.W) * parts), dim3(kTopThreads), 0, st, a);
-        RDK_TIMED_LAUNCH("beam_merge_kernel", (beam_merge_kernel<KIND>), dim3((unsigned)d.G), dim3(kTopThreads),
-                         (size_t)d.W * parts * k * sizeof(uint64_t), st, b);
+        const int count = d.W * parts * k;
+        if (count <= 4 * 256)
+            RDK_TIMED_LAUNCH("beam_merge_kernel", (beam_merge_kernel<KIND, 256, 4>), dim3((unsigned)d.G), dim3(256), 0, st, b);
+        else if (count <= 16 * 256)
+            RDK_TIMED_LAUNCH("beam_merge_kernel", (beam_merge_kernel<KIND, 256, 16>), dim3((unsigned)d.G), dim3(256), 0, st, b);
+        else
+            RDK_TIMED_LAUNCH("beam_merge_kernel", (beam_merge_kernel<KIND, 1024, 16>), dim3((unsigned)d.G), dim3(1024), 0, st, b);
     });
-    if (rc != RDK_OK) return rc;
     RDK_LAUNCH_CHECK("beam_merge_kernel");
     return RDK_OK;
 }

@@ -4,6 +4,15 @@
 
 namespace rdk {
 
+// The largest of three as one instruction (fmaxf of values taken apart from bit patterns costs two more, which would quiet signalling NaN: a NaN
+// among the operands shows in the sums that every user forms beside it).
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 
@@ -55,6 +64,14 @@ struct Vec {
         for (int e = 0; e < kLen - 1; ++e)   // the vector is not whole
             if (e < left) set(r, e, one(p, e));
         return r;
+    }
+
+    // the largest element and m
+    static __device__ __forceinline__ float largest(const float (&v)[kLen], float m)
+    {
+#pragma unroll
+        for (int e = 0; e < kLen; e += 2) m = max3(v[e], v[e + 1], m);
+        return m;
     }
 
     // elements i .. i + kLen - 1 of a row that ends at `end`
