@@ -11,7 +11,8 @@ constexpr int kTopThreads = 256;
 constexpr float kLog2e = 1.44269504088896341f;
 
 constexpr int kRoundVecs = 4;          // 16-byte vectors of a lane in a round
-constexpr int kQueue = 2048, kFound = 1024;   // vectors noted, entries sorted: what exceeds these takes the slow way
+constexpr int kNoted = 512, kFound = 1024;   // vectors noted by a wavefront, entries sorted: what exceeds these takes a slower way
+constexpr int kSift = 4;               // noted vectors read at a time
 constexpr int kMergeEntries = 4096;    // of a row's parts together
 constexpr int kBeamEntries = 16384;    // of a request's beams and their parts together
 constexpr int kTopWaves = kTopThreads / kWave;
@@ -25,7 +26,8 @@ struct TopArgs {
     // rows of beams that have no candidates among the ids are passed over
     const float *scores;
     const uint8_t *finished;
-    uint64_t *entries;      // [rows, parts, k], 0 where a part has fewer; or NULL: the outputs of topk itself
+    int W;                  // rows that are merged: the beams of a request, 1 otherwise
+    uint64_t *entries;      // [rows / W, k, parts, W], 0 where a part has fewer; or NULL: the outputs of topk itself
     SoftStat *stat;         // [rows, parts]
     int32_t *ids;
     float *values, *lse;
@@ -34,9 +36,10 @@ struct TopArgs {
 struct TopShared {
     SelectShared slow;
     uint64_t found[kFound];
-    uint32_t queue[kQueue];
+    float2 queue[kTopWaves][kNoted];   // of a wavefront's vectors: the largest value and the place
+    int noted[kTopWaves];
     float wave_m[kTopWaves], wave_s[kTopWaves], bound[kTopWaves];
-    int queued, count;
+    int count;
 };
 
 // The nth largest of the keys of 64 lanes, to their highest BITS bits, by halving.  (Rolled up: code that runs once is fetched while it runs.)
@@ -53,14 +56,14 @@ __device__ __forceinline__ uint32_t wave_nth(uint32_t key, int nth)
     return found << (32 - BITS);
 }
 
-// The value that the nth largest of the lanes' largest values has, as a number no entry that is wanted lies below.  With fewer lanes that have unmasked
-// values: every unmasked value is wanted.
-template <int KIND>
+// A value that no entry that is wanted lies below: the nth largest of the lanes' largest values, to the highest BITS bits of its key (sixteen are all
+// that a bf16 value has).  With fewer lanes that have unmasked values: every unmasked value is wanted.
+template <int KIND, int BITS>
 __device__ __forceinline__ float wave_bound(float largest, int nth)
 {
-    const uint32_t key = wave_nth<KIND == RDK_LOGIT_BF16 ? 16 : 32>(order_key(largest), nth);   // (a bf16 value's key ends in sixteen equal bits)
+    const uint32_t key = wave_nth<BITS>(order_key(largest), nth);
     if (key <= masked_key<KIND>()) return KIND == RDK_PROB_F32 ? __uint_as_float(1u) : -3.402823466e38f;
-    return key_value(KIND == RDK_LOGIT_BF16 && !(key >> 31) ? key | 0xFFFFu : key);
+    return key_value(KIND == RDK_LOGIT_BF16 && !(key >> 31) ? key | 0xFFFFu : key);   // (the key of a negative bf16 value ends in ones)
 }
 
 // The sum of exp((x - m) / T) over a part, for a largest value m so far from zero that the product with 1 / T leaves the range.
@@ -81,10 +84,28 @@ __device__ __forceinline__ float wide_sum(const TopArgs &a, const void *xr, int 
     return s;
 }
 
-__device__ __forceinline__ void note(uint32_t *queue, int *count, uint32_t what)
+// Appends value(e) to a list in LDS for every e < E that takes(e), with room for `most`; places beyond that are counted, and nothing is written there.
+// One addition to the count for the wavefront: each costs the way to LDS and back.
+template <int E, class Takes, class Value, class T>
+__device__ __forceinline__ void append(T *list, int *count, int most, const Takes &takes, const Value &value)
 {
-    const int at = atomicAdd(count, 1);
-    if (at < kQueue) queue[at] = what;
+    uint64_t who[E];
+    int all = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        who[e] = __ballot(takes(e));
+        all += __popcll(who[e]);
+    }
+    if (all == 0) return;
+    int at = 0;
+    if (lane_id() == __ffsll((unsigned long long)__ballot(1)) - 1) at = atomicAdd(count, all);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int to = at + __builtin_amdgcn_mbcnt_hi((unsigned)(who[e] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who[e], 0));
+        if (takes(e) && to < most) list[to] = value(e);
+        at += __popcll(who[e]);
+    }
 }
 
 // The k largest of the entries found[0 .. n - 1] in sorted, descending, by counting for each how many are larger.
@@ -151,8 +172,9 @@ __device__ __forceinline__ void write_row(int32_t *ids, float *values, float *ls
 // largest.  It is found after the first round of loads and anew as the values seen grow by half (a wavefront reads what the others last
 // wrote: bounds only rise, so an old one is a bound too, and nothing waits); a vector whose largest value reaches it is noted by its place.
 // What was noted is read again at the end (out of the cache), sifted by the last bound, and sorted.  Where more was noted than there is room for
-// (values that rise along the row) the whole part is sifted; where more reaches the last bound than there is room for, it is the k-th
-// largest value itself and met by many (what masks leave): those above it are taken, and the first of those that equal it.
+// (values that rise along the row) the whole part is sifted; where more reaches the last bound than there is room for, by the bound to its last
+// bit; and where that is still more, it is the k-th largest value itself and met by many (what masks leave): those above it are
+// taken, and the first of those that equal it.
 // Only values that crowd in few lanes, and NaN, leave the search by halving.
 template <int KIND>
 __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
@@ -181,8 +203,8 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         ref = to;
         high = held + a.margin;
     };
-    auto publish = [&]() __attribute__((always_inline)) {
-        const float b = wid < waves ? wave_bound<KIND>(m, share) : INFINITY;
+    auto publish = [&](auto bits) __attribute__((always_inline)) {
+        const float b = wid < waves ? wave_bound<KIND, decltype(bits)::value>(m, share) : INFINITY;
         if (lane_id() == 0) __hip_atomic_store(&sh.bound[wid], b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     };
     auto least_bound = [&]() __attribute__((always_inline)) {
@@ -191,7 +213,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         for (int w = 0; w < kTopWaves; ++w) b = fminf(b, __hip_atomic_load(&sh.bound[w], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP));
         return b;
     };
-    if (tid == 0) sh.queued = sh.count = 0;
+    if (tid == 0) sh.count = 0;
     if (tid < behind) {
         last = load1<KIND>(from, whole * V::kLen + tid);
         m = fmaxf(m, last);
@@ -203,22 +225,22 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         }
     }
     float tau = INFINITY;
-    int next_bound = 0, round = 0;
-    u32x4 raw[kRoundVecs];
-#pragma unroll 1
-    for (int base = -kRound; base < whole; base += kRound) {
-        u32x4 now[kRoundVecs];
+    int next_bound = 0, round = 0, noted = 0;
+    // Always as many loads, of the last vector where the round has none of its own: the compiler counts loads in flight, and would wait for all of
+    // them behind a branch that has some of its own (1024 rows of 151936 bf16 logits 61 us).
+    auto load_round = [&](u32x4 (&raw)[kRoundVecs], int base, auto first) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kRoundVecs; ++j) now[j] = raw[j];
-        if (base + kRound < whole) {   // the round ahead
-#pragma unroll
-            for (int j = 0; j < kRoundVecs; ++j) {
-                raw[j] = V::fill();
-                if (base + kRound + j * kTopThreads + tid < whole)
-                    raw[j] = *(const u32x4_any *)(from + ((int64_t)base + kRound + j * kTopThreads) * 16 + (uint32_t)tid * 16);
-            }
+        for (int j = 0; j < kRoundVecs; ++j) {
+            const u32x4_any *at = (const u32x4_any *)(from + (uint64_t)(uint32_t)min(base + j * kTopThreads + tid, whole - 1) * 16);
+            raw[j] = decltype(first)::value ? *at : __builtin_nontemporal_load(at);   // a part of one round is read again at once
         }
-        if (base < 0) continue;
+    };
+    auto take_round = [&](u32x4 (&now)[kRoundVecs], int base) __attribute__((always_inline)) {
+        if (base + kRound > whole) {
+#pragma unroll
+            for (int j = 0; j < kRoundVecs; ++j)
+                if (base + j * kTopThreads + tid >= whole) now[j] = V::fill();
+        }
         float vm[kRoundVecs];
 #pragma unroll
         for (int j = 0; j < kRoundVecs; ++j) {
@@ -234,18 +256,41 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
                 for (int e = 0; e < V::kLen; ++e) sum += __builtin_amdgcn_exp2f(fmaf(v[e], a.c, -ref));
             }
             s += sum;
-            m = fmaxf(m, vm[j]);
         }
+        m = max3(m, max3(vm[0], vm[1], vm[2]), vm[3]);
         if (round == next_bound) {
             next_bound = round + 1 + round / 2;
-            publish();
+            publish(std::integral_constant<int, 16>());
             if (round == 0) __syncthreads();
             tau = least_bound();
         }
         ++round;
+        // every wavefront notes in a list of its own, whose length it alone knows
+        uint64_t who[kRoundVecs], any = 0;
 #pragma unroll
-        for (int j = 0; j < kRoundVecs; ++j)
-            if (vm[j] >= tau) note(sh.queue, &sh.queued, (uint32_t)(base + j * kTopThreads + tid));
+        for (int j = 0; j < kRoundVecs; ++j) any |= who[j] = __ballot(vm[j] >= tau);
+        if (any) {
+#pragma unroll
+            for (int j = 0; j < kRoundVecs; ++j) {
+                const int to = noted + __builtin_amdgcn_mbcnt_hi((unsigned)(who[j] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)who[j], 0));
+                if (vm[j] >= tau && to < kNoted) sh.queue[wid][to] = make_float2(vm[j], __int_as_float(base + j * kTopThreads + tid));
+                noted += __popcll(who[j]);
+            }
+        }
+    };
+    static_assert(kRoundVecs == 4 && kTopWaves == 4, "the largest of a round is formed of four");
+    if (whole > 0) {
+        u32x4 raw[kRoundVecs], ahead[kRoundVecs];   // in turn: the round at hand, and the next one on its way
+        load_round(raw, 0, std::true_type());
+#pragma unroll 1
+        for (int base = 0;; base += 2 * kRound) {
+            load_round(ahead, base + kRound, std::false_type());
+            take_round(raw, base);
+            if (base + kRound >= whole) break;
+            load_round(raw, base + 2 * kRound, std::false_type());
+            take_round(ahead, base + kRound);
+            if (base + 2 * kRound >= whole) break;
+        }
     }
     // statistics of the part, and its last bound
     const float wave_m = wave_max(m);
@@ -257,8 +302,9 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     if (lane_id() == 0) {
         sh.wave_m[wid] = wave_m;
         sh.wave_s[wid] = wave_s;
+        sh.noted[wid] = noted;
     }
-    if (round != 1) publish();
+    if (round != 1) publish(std::integral_constant<int, 16>());
     __syncthreads();
     tau = least_bound();
     SoftStat stat{none, 0.f};
@@ -278,38 +324,52 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     }
     if (stat.m > -INFINITY && fabsf(stat.m) > a.limit) stat.s = wide_sum<KIND>(a, xr, begin, end, stat.m, sh);
     const bool nan = stat.s != stat.s;
-    const int queued = sh.queued;
-    bool all = queued > kQueue, above = false;   // the whole part; only what lies above the bound
-    int n = 0;
+    bool all = max(max(sh.noted[0], sh.noted[1]), max(sh.noted[2], sh.noted[3])) > kNoted;   // the whole part is sifted
+    int n = 0, stage = 0;   // 0: what reaches the bound; 1: the bound to the last bit; 2: what exceeds it
     float least = tau;
 #pragma unroll 1
     while (!nan) {
-        const int count = all ? whole : queued;
-        for (int q = tid; q < count; q += kTopThreads) {
-            const int at = all ? q : (int)sh.queue[q];
-            float v[V::kLen];
-            V::to(*(const u32x4_any *)(from + (int64_t)at * 16), v);
+        const int count = all ? whole : noted, stride = all ? kTopThreads : kWave, own = all ? tid : lane_id();
+#pragma unroll 1
+        for (int first = 0; first < count; first += kSift * stride) {   // (alike for the wavefront, for which append() speaks)
+            u32x4 raw[kSift];
+            int at[kSift];
 #pragma unroll
-            for (int e = 0; e < V::kLen; ++e)
-                if (v[e] >= least) {
-                    const int to = atomicAdd(&sh.count, 1);
-                    if (to < kFound) sh.found[to] = entry_of(order_key(v[e]), (uint32_t)(begin + at * V::kLen + e));
-                }
+            for (int j = 0; j < kSift; ++j) {   // together on their way
+                const int q = first + j * stride + own;
+                const float2 seen = !all && q < count ? sh.queue[wid][q] : make_float2(INFINITY, __int_as_float(q));
+                at[j] = q < count && seen.x >= least ? __float_as_int(seen.y) : -1;
+                raw[j] = V::fill();
+                if (at[j] >= 0) raw[j] = *(const u32x4_any *)(from + (int64_t)at[j] * 16);
+            }
+#pragma unroll 1
+            for (int j = 0; j < kSift && first + j * stride < count; ++j) {
+                float v[V::kLen];
+                V::to(raw[0], v);
+                append<V::kLen>(
+                    sh.found, &sh.count, kFound, [&](int e) { return v[e] >= least; },
+                    [&](int e) { return entry_of(order_key(v[e]), (uint32_t)(begin + at[0] * V::kLen + e)); });
+#pragma unroll
+                for (int i = 0; i + 1 < kSift; ++i) raw[i] = raw[i + 1], at[i] = at[i + 1];
+            }
         }
-        if (tid < behind && last >= least) {
-            const int to = atomicAdd(&sh.count, 1);
-            if (to < kFound) sh.found[to] = entry_of(order_key(last), (uint32_t)(begin + whole * V::kLen + tid));
-        }
+        if (tid < behind)
+            append<1>(
+                sh.found, &sh.count, kFound, [&](int) { return last >= least; },
+                [&](int) { return entry_of(order_key(last), (uint32_t)(begin + whole * V::kLen + tid)); });
         __syncthreads();
         n = sh.count;
-        if (n <= kFound || above) break;
-        all = above = true;
-        least = key_value(order_key(tau) + 1);
+        if (n <= kFound || stage == 2) break;
+        all = true;
+        stage = KIND == RDK_LOGIT_BF16 ? 2 : stage + 1;
+        if (stage == 1) publish(std::integral_constant<int, 32>());
         __syncthreads();
         if (tid == 0) sh.count = 0;
+        tau = least_bound();
+        least = stage == 2 ? key_value(order_key(tau) + 1) : tau;
         __syncthreads();
     }
-    if (above && n < a.k) {
+    if (stage == 2 && n < a.k) {
         __syncthreads();
         if (wid == 0) {
             const int filled = take_equal<KIND>(xr, begin, whole, end, tau, n, a.k, sh);
@@ -334,7 +394,9 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         __syncthreads();
     }
     if (a.entries) {
-        if (tid < a.k) a.entries[(row * a.parts + part) * a.k + tid] = tid < n ? sh.slow.sorted[tid] : 0;
+        // the best of every part and beam first, then the second best of every one, ...
+        const int64_t group = row / a.W;
+        if (tid < a.k) a.entries[((group * a.k + tid) * a.parts + part) * a.W + (row - group * a.W)] = tid < n ? sh.slow.sorted[tid] : 0;
         if (tid == 0) a.stat[row * a.parts + part] = stat;
         return;
     }
@@ -372,40 +434,49 @@ struct MergeShared {
     int count;
 };
 
-// The k largest of the workgroup's entries (EACH to a thread, 0: none) in sh.slow.sorted.  Returns how many there are.  As above, but the threads'
-// largest are looked at together: the wavefronts' shares of beams are nothing like alike.
+// The k largest of the workgroup's `count` entries in sh.slow.sorted; returns how many there are.  Thread t holds the entries t, t + THREADS, ... in
+// own (0: none).  By a bound as above: the entries come best places first, so no entry of a thread is much larger than its first.  The
+// largest of four wavefronts are looked at together; sixteen find a bound each, of which the least is taken (beams stand next to one
+// another: every wavefront has its share of the best ones).
 template <int THREADS, int EACH>
-__device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int k, MergeShared<THREADS> &sh)
+__device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int count, int k, MergeShared<THREADS> &sh)
 {
     constexpr int kWaves = THREADS / kWave;
     const int tid = threadIdx.x;
     uint64_t best = 0;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) best = own[i] > best ? own[i] : best;
-    sh.keys[tid] = entry_key(best);
     if (tid == 0) sh.count = 0;
-    __syncthreads();
-    uint32_t keys[kWaves], found = 0;   // every wavefront finds the k-th largest by itself
+    uint32_t bound = 0;
+    if constexpr (kWaves <= 4) {
+        sh.keys[tid] = entry_key(best);
+        __syncthreads();
+        uint32_t keys[kWaves];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) keys[w] = sh.keys[w * kWave + lane_id()];
-#pragma unroll 2
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t tried = found | (1u << bit);
-        int n = 0;
+        for (int w = 0; w < kWaves; ++w) keys[w] = sh.keys[w * kWave + lane_id()];
+#pragma unroll 4
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t tried = bound | (1u << bit);
+            int n = 0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(keys[w] >= tried));
-        if (n >= k) found = tried;
-    }
-    const uint64_t least = found ? (uint64_t)found << 32 : 1;
-#pragma unroll
-    for (int i = 0; i < EACH; ++i)
-        if (own[i] >= least) {
-            const int at = atomicAdd(&sh.count, 1);
-            if (at < kFound) sh.found[at] = own[i];
+            for (int w = 0; w < kWaves; ++w) n += __popcll(__ballot(keys[w] >= tried));
+            if (n >= k) bound = tried;
         }
+    } else {
+        const int waves = min((count + kWave - 1) / kWave, kWaves);
+        const uint32_t b = tid / kWave < waves ? wave_nth<32>(entry_key(best), (k + waves - 1) / waves) : 0xFFFFFFFFu;
+        if (lane_id() == 0) sh.keys[tid / kWave] = b;
+        __syncthreads();
+        bound = sh.keys[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) bound = min(bound, sh.keys[w]);
+    }
+    const uint64_t least = bound ? (uint64_t)bound << 32 : 1;
+    append<EACH>(
+        sh.found, &sh.count, kFound, [&](int i) { return own[i] >= least; }, [&](int i) { return own[i]; });
     __syncthreads();
     const int n = sh.count;
-    if (n > kFound)   // thousands that tie with the k-th
+    if (n > kFound)   // thousands that tie with the k-th, or beams of which few have all the best
         return select_exact<THREADS>(
             [&](auto f) {
 #pragma unroll
@@ -426,8 +497,7 @@ struct TopMergeArgs {
     float *values, *lse;
 };
 
-// The parts of a row brought together.  Entries are dealt to the threads place by place of the sorted lists (the first of every part, then the
-// second, ...): the largest are with different threads then, and the bound is close.
+// The parts of a row brought together.
 template <int KIND, int EACH>
 __global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a)
 {
@@ -438,11 +508,11 @@ __global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a)
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
         const int at = i * kTopThreads + (int)threadIdx.x;
-        own[i] = at < count ? a.entries[row * count + at % a.parts * a.k + at / a.parts] : 0;
+        own[i] = at < count ? a.entries[row * count + at] : 0;
     }
     SoftStat stat{0.f, 0.f};
     if (threadIdx.x < kWave) stat = merge_stats<KIND>(a.stat + row * a.parts, a.parts, a.c);
-    const int n = select_entries<kTopThreads, EACH>(own, a.k, sh);
+    const int n = select_entries<kTopThreads, EACH>(own, count, a.k, sh);
     write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, stat);
 }
 
@@ -466,11 +536,12 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamArgs a)
     __shared__ int beam_state[kWave];        // 0: no candidates, 1: finished, 2: live
     const int64_t g = blockIdx.x, b0 = g * a.W;
     const int tid = threadIdx.x, lists = a.W * a.parts, count = lists * a.k;
+    const float per_beam = 1.f / a.W;
     uint64_t own[EACH];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {         // (of beams without a row this is whatever lay there, and not used)
         const int at = i * THREADS + tid;
-        own[i] = at < count ? a.entries[b0 * a.parts * a.k + at % lists * a.k + at / lists] : 0;
+        own[i] = at < count ? a.entries[g * count + at] : 0;
     }
     for (int w = tid / kWave; w < a.W; w += THREADS / kWave) {
         const float score = a.scores[b0 + w];
@@ -487,11 +558,12 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamArgs a)
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-        const int at = i * THREADS + tid, list = at % lists, w = list / a.parts;
+        const int at = i * THREADS + tid;
+        const int w = at - (int)(((float)at + 0.5f) * per_beam) * a.W;   // at % W (numbers below 2^15: exact)
         const int state = at < count ? beam_state[w] : 0;
         uint64_t e = own[i];
         if (state == 1) {
-            e = at / lists == 0 && list == w * a.parts ? entry_of(order_key(beam_score[w]), (uint32_t)w * a.N + a.eos) : 0;
+            e = at < a.W ? entry_of(order_key(beam_score[w]), (uint32_t)w * a.N + a.eos) : 0;
         } else if (state == 2 && e != 0) {
             const float x = key_value(entry_key(e));
             const float score = beam_score[w] + (KIND == RDK_PROB_F32 ? logf(x / beam_log[w]) : (x - beam_m[w]) - beam_log[w]);
@@ -501,7 +573,7 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamArgs a)
         }
         own[i] = e;
     }
-    const int n = select_entries<THREADS, EACH>(own, a.K, sh);
+    const int n = select_entries<THREADS, EACH>(own, count, a.K, sh);
     if (tid < a.K) {
         const bool in = tid < n;
         const uint64_t e = in ? sh.slow.sorted[tid] : 0;
@@ -522,13 +594,26 @@ void with_kind(rdk_input_kind_t kind, const F &f)
     else f(std::integral_constant<int, RDK_LOGIT_BF16>());
 }
 
-// In how many parts a row is read, so that a batch of few rows fills the chip.
-int parts_of(int64_t rows, int N, int most)
+// How a row is read in parts, so that a batch of few rows fills the chip.  Four workgroups are on a compute unit at a time: 1000 rows and more are not
+// split, and 500 are not either, since the merge is a launch (512 rows of 128256 bf16 logits: 30 us in one part, 39 in two).  A part holds
+// whole rounds of loads, or at least 4096 values.
+struct Parts {
+    int count, len;
+};
+Parts parts_of(int64_t rows, int N, rdk_input_kind_t kind, int most)
 {
-    const int want = (int)((1024 + rows - 1) / rows), maxs = (N + 4095) / 4096;
-    int p = want < maxs ? want : maxs;
-    p = p < most ? p : most;
-    return p < 1 ? 1 : p;
+    const int round = kTopThreads * kRoundVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4), want = (int)(1000 / rows);
+    if (want <= 1 || N <= 4096 || most <= 1) return Parts{1, (int)align_up(N, 64)};
+    int64_t len = ((int64_t)N - 1) / (want < most ? want : most) + 1;
+    if (len < 4096) len = 4096;
+    if (len > round && want <= most) len = len / round * round;
+    len = (int64_t)align_up((size_t)len, 64);
+    int count = (int)((N - 1) / len) + 1;
+    if (count > most) {
+        len = (int64_t)align_up((size_t)((N - 1) / most + 1), 64);
+        count = (int)((N - 1) / len) + 1;
+    }
+    return Parts{count, (int)len};
 }
 
 struct TopWs {
@@ -546,11 +631,10 @@ TopWs carve(int64_t rows, int parts, int k, void *ws, size_t *bytes)
     return w;
 }
 
-TopArgs part_args(RowInput x, int N, int k, int parts, float temperature)
+TopArgs part_args(RowInput x, int N, int k, Parts parts, float temperature)
 {
     TopArgs a{};
-    a.x = x.ptr; a.ldx = x.ld; a.N = N; a.k = k; a.parts = parts;
-    a.part_len = (int)align_up(((size_t)N + parts - 1) / parts, 64);
+    a.x = x.ptr; a.ldx = x.ld; a.N = N; a.k = k; a.parts = parts.count; a.part_len = parts.len; a.W = 1;
     a.inv_t = 1.f / temperature;
     a.c = a.inv_t * kLog2e;
     a.margin = 60.f / a.c;
@@ -563,11 +647,11 @@ TopArgs part_args(RowInput x, int N, int k, int parts, float temperature)
 int select_max_entries() { return kMaxTop; }
 int select_max_ids() { return 1 << 30; }   // places in a row, a round of loads behind its end among them, are 32-bit numbers
 
-static int topk_parts(const rdk_topk_desc_t &d) { return parts_of(d.B, d.N, kMergeEntries / d.k); }
+static Parts topk_parts(const rdk_topk_desc_t &d, rdk_input_kind_t kind) { return parts_of(d.B, d.N, kind, kMergeEntries / d.k); }
 
 size_t topk_workspace_bytes(const rdk_topk_desc_t &d, rdk_input_kind_t kind)
 {
-    const int parts = topk_parts(d);
+    const int parts = topk_parts(d, kind).count;
     size_t bytes = 0;
     if (parts > 1) carve(d.B, parts, d.k, nullptr, &bytes);
     return bytes;
@@ -575,8 +659,9 @@ size_t topk_workspace_bytes(const rdk_topk_desc_t &d, rdk_input_kind_t kind)
 
 rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, float *values, float *lse, void *ws, hipStream_t st)
 {
-    const int parts = topk_parts(d);
-    TopArgs a = part_args(x, d.N, d.k, parts, d.temperature);
+    const Parts split = topk_parts(d, x.kind);
+    const int parts = split.count;
+    TopArgs a = part_args(x, d.N, d.k, split, d.temperature);
     a.ids = ids; a.values = values; a.lse = lse;
     if (parts > 1) {
         const TopWs w = carve(d.B, parts, d.k, ws, nullptr);
@@ -598,28 +683,26 @@ rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, flo
     return RDK_OK;
 }
 
-static int beam_parts(const rdk_beam_desc_t &d, int k)
-{
-    const int most = kBeamEntries / (d.W * k);
-    return parts_of((int64_t)d.G * d.W, d.N, most < 1 ? 1 : most);
-}
+static Parts beam_parts(const rdk_beam_desc_t &d, rdk_input_kind_t kind, int k) { return parts_of((int64_t)d.G * d.W, d.N, kind, kBeamEntries / (d.W * k)); }
 
 size_t beam_select_workspace_bytes(const rdk_beam_desc_t &d, rdk_input_kind_t kind)
 {
     const int k = d.K < d.N ? d.K : d.N;
     size_t bytes = 0;
-    carve((int64_t)d.G * d.W, beam_parts(d, k), k, nullptr, &bytes);
+    carve((int64_t)d.G * d.W, beam_parts(d, kind, k).count, k, nullptr, &bytes);
     return bytes;
 }
 
 rdk_status_t launch_beam_select(const rdk_beam_desc_t &d, RowInput x, const float *scores, const uint8_t *finished, float *scores_out,
                                 int32_t *parent, int32_t *token, uint8_t *finished_out, void *ws, hipStream_t st)
 {
-    const int k = d.K < d.N ? d.K : d.N, parts = beam_parts(d, k);
+    const int k = d.K < d.N ? d.K : d.N;
+    const Parts split = beam_parts(d, x.kind, k);
+    const int parts = split.count;
     const TopWs w = carve((int64_t)d.G * d.W, parts, k, ws, nullptr);
-    TopArgs a = part_args(x, d.N, k, parts, 1.f);
+    TopArgs a = part_args(x, d.N, k, split, 1.f);
     a.scores = scores; a.finished = finished;
-    a.entries = w.entries; a.stat = w.stat;
+    a.entries = w.entries; a.stat = w.stat; a.W = d.W;
     BeamArgs b{};
     b.entries = w.entries; b.stat = w.stat; b.scores = scores; b.finished = finished;
     b.W = d.W; b.N = d.N; b.k = k; b.K = d.K; b.parts = parts; b.eos = d.eos;
