@@ -594,15 +594,18 @@ void with_kind(rdk_input_kind_t kind, const F &f)
     else f(std::integral_constant<int, RDK_LOGIT_BF16>());
 }
 
-// How a row is read in parts, so that a batch of few rows fills the chip.  Four workgroups are on a compute unit at a time: 1000 rows and more are not
-// split, and 500 are not either, since the merge is a launch (512 rows of 128256 bf16 logits: 30 us in one part, 39 in two).  A part holds
-// whole rounds of loads, or at least 4096 values.
+// How a row is read in parts, so that a batch of few rows fills the chip: two workgroups to a compute unit, parts of whole rounds of loads or at least
+// 4096 values (16 requests of 8 beams over 128256 bf16 ids: 256, 512, 1024, 2048 workgroups 22.1, 21.0, 22.3, 22.5 us; 64 of 4 26.7, 24.0, 27.0,
+// 29.8).  Where the merge of the parts is a launch that a whole row does without (topk), rows of up to six rounds and batches of 192 rows and
+// more are not split: in one part and in two to four 192 rows of 32000 bf16 logits take 11.0 and 13.3 us, 128 rows 10.5 and 12.6, 192 of
+// 128256 23.9 and 25.9; but 128 rows of 128256 21.2 and 19.5.
 struct Parts {
     int count, len;
 };
-Parts parts_of(int64_t rows, int N, rdk_input_kind_t kind, int most)
+Parts parts_of(int64_t rows, int N, rdk_input_kind_t kind, int most, bool merges)
 {
-    const int round = kTopThreads * kRoundVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4), want = (int)(1000 / rows);
+    const int round = kTopThreads * kRoundVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4);
+    const int want = !merges && (rows >= 192 || N <= 6 * round) ? 1 : (int)(512 / rows);
     if (want <= 1 || N <= 4096 || most <= 1) return Parts{1, (int)align_up(N, 64)};
     int64_t len = ((int64_t)N - 1) / (want < most ? want : most) + 1;
     if (len < 4096) len = 4096;
@@ -647,7 +650,7 @@ TopArgs part_args(RowInput x, int N, int k, Parts parts, float temperature)
 int select_max_entries() { return kMaxTop; }
 int select_max_ids() { return 1 << 30; }   // places in a row, a round of loads behind its end among them, are 32-bit numbers
 
-static Parts topk_parts(const rdk_topk_desc_t &d, rdk_input_kind_t kind) { return parts_of(d.B, d.N, kind, kMergeEntries / d.k); }
+static Parts topk_parts(const rdk_topk_desc_t &d, rdk_input_kind_t kind) { return parts_of(d.B, d.N, kind, kMergeEntries / d.k, false); }
 
 size_t topk_workspace_bytes(const rdk_topk_desc_t &d, rdk_input_kind_t kind)
 {
@@ -683,7 +686,7 @@ rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, flo
     return RDK_OK;
 }
 
-static Parts beam_parts(const rdk_beam_desc_t &d, rdk_input_kind_t kind, int k) { return parts_of((int64_t)d.G * d.W, d.N, kind, kBeamEntries / (d.W * k)); }
+static Parts beam_parts(const rdk_beam_desc_t &d, rdk_input_kind_t kind, int k) { return parts_of((int64_t)d.G * d.W, d.N, kind, kBeamEntries / (d.W * k), true); }
 
 size_t beam_select_workspace_bytes(const rdk_beam_desc_t &d, rdk_input_kind_t kind)
 {
