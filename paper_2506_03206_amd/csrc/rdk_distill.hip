@@ -490,15 +490,20 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
         return;
     }
     const float c = a.inv_t * kLog2e;
-    u32x4 raw[kLoopVecs];
-    auto load_round = [&](int base) {
+    const int whole = a.n / V::kLen, behind = a.n % V::kLen;   // whole vectors (there are some: rows are long), logits behind them
+    // Always as many loads, of the last vector where the round has none of its own: the compiler counts loads in flight, and would wait for all of
+    // them behind a branch that has some of its own.
+    auto load_round = [&](u32x4 (&raw)[kLoopVecs], int base) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kLoopVecs; ++j) {
-            const int left = a.n - (base + j * kLoopThreads + tid) * V::kLen;
-            raw[j] = left > 0 ? V::load_at(zr + ((int64_t)base + j * kLoopThreads) * 16, tid * 16, left) : V::fill();
-        }
+        for (int j = 0; j < kLoopVecs; ++j)
+            raw[j] = *(const u32x4_any *)(zr + (uint64_t)(uint32_t)min(base + j * kLoopThreads + tid, whole - 1) * 16);
     };
-    if (!follows) load_round(0);
+    u32x4 raw[kLoopVecs], ahead[kLoopVecs];
+    float last = -INFINITY;
+    if (!follows) {
+        load_round(raw, 0);
+        if (tid < behind) last = load1<KIND>(zr, whole * V::kLen + tid);
+    }
     if (REST) {
         for (int i = tid * 16; i < vectors; i += (kLoopThreads + kWave) * 16) *(u32x4 *)(marked_row + i) = u32x4{0, 0, 0, 0};
         __syncthreads();
@@ -519,24 +524,21 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
         const Entries t = row_entries(a, row, kept.slot);
         follow<KIND, REST>(a, row, zr, c, t, kept, &entries);
     } else {
-        float v[V::kLen];
-        SoftStat st{-INFINITY, 0.f};
-        for (int base = 0; base < vectors; base += kRound) {
-            u32x4 now[kLoopVecs];
-#pragma unroll
-            for (int j = 0; j < kLoopVecs; ++j) now[j] = raw[j];
-            if (base + kRound < vectors) load_round(base + kRound);
-            float m = st.m;
+        if (REST && tid < behind && (marked_row[whole] >> tid & 1)) last = -INFINITY;
+        SoftStat st{last, last == -INFINITY ? 0.f : 1.f};
+        if (last != last) st.s = last;
+        auto take_round = [&](u32x4 (&now)[kLoopVecs], int base) __attribute__((always_inline)) {
+            float v[V::kLen], m = st.m;
 #pragma unroll
             for (int j = 0; j < kLoopVecs; ++j) {
                 const int at = base + j * kLoopThreads + tid;
-                if (REST && at < vectors) {
+                if (at >= whole) now[j] = V::fill();
+                if (REST && at < whole) {
                     const unsigned bits = marked_row[at];
                     if (bits) V::strike(now[j], bits);
                 }
                 V::to(now[j], v);
-#pragma unroll
-                for (int e = 0; e < V::kLen; ++e) m = fmaxf(m, v[e]);
+                m = V::largest(v, m);
             }
             const float ref = weight_reference(m);
             float sum = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
@@ -550,6 +552,15 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
                 sum += part;
             }
             st = SoftStat{m, sum};
+        };
+#pragma unroll 1
+        for (int base = 0;; base += 2 * kRound) {
+            load_round(ahead, base + kRound);
+            take_round(raw, base);
+            if (base + kRound >= whole) break;
+            load_round(raw, base + 2 * kRound);
+            take_round(ahead, base + kRound);
+            if (base + 2 * kRound >= whole) break;
         }
         st = wave_merge_at(st, c);
         if (lane_id() == 0) waves[tid / kWave] = st;
