@@ -1,12 +1,25 @@
 // The states of beams after a selection: rows of device buffers copied by an index of parents, in place or from one buffer into another.
 //
-// A thread owns one unit (up to 16 bytes) of a row's bytes for every beam of a request: it reads the units of all rows that change before it
-// writes any of them, so a reorder in place needs no scratch and no order between threads.
+// A thread owns one unit (16 bytes, less at the end of a piece) of a row's bytes for every beam of a request: it reads the units of all rows that
+// change before it writes any of them, so a reorder in place needs no scratch and no order between threads.  Units lie at any address
+// (the memory pipe takes them: five beams with rows of 8 pieces of 65934 bytes move at 4.3 TB/s, in units as small as the sizes' common
+// divisor at 1.4).  Bound by HBM: 5.8 to 6.1 TB/s of the bytes of rows that change and are needed, where a copy kernel reaches 6.0 to 6.4;
+// non-temporal accesses are worth an eighth (16 requests of 4 beams, 0.54 GB of caches: 137 us without, 131 stores alone, 120 both).
 #include "rdk_vec.hpp"
 
 namespace rdk {
 
 namespace {
+
+// Units at any address (as members: a template argument would lose the alignment).
+struct Unit16 { typedef unsigned type __attribute__((ext_vector_type(4), aligned(1))); };
+struct Unit8 { typedef unsigned type __attribute__((ext_vector_type(2), aligned(1))); };
+struct Unit4 { typedef unsigned type __attribute__((aligned(1))); };
+struct Unit2 { typedef unsigned short type __attribute__((aligned(1))); };
+struct Unit1 { typedef unsigned char type; };
+
+// The parents of a request, which nothing writes meanwhile: read by the scalar unit, once for a wavefront.
+typedef const __attribute__((address_space(4))) int *Parents;
 
 constexpr int kStatesPerLaunch = 24, kReorderThreads = 256, kMaxBeams = 64;
 
@@ -15,10 +28,10 @@ struct StateArg {
     char *dst;
     int64_t src_stride, dst_stride, src_pitch, dst_pitch;
     int64_t units;          // per row: segments * units per segment
-    int64_t per_segment;    // units of a segment
+    int64_t per_segment;    // units of a segment, the last of which may have less than 16 bytes
+    int64_t segment_bytes;
     unsigned first_block;   // of the launch
     unsigned blocks;        // per request
-    unsigned unit;          // bytes
 };
 struct StateArgs {
     StateArg s[kStatesPerLaunch];
@@ -28,36 +41,25 @@ struct StateArgs {
 
 // The units of the rows I .. MOST - 1: all are read on the way down, and written on the way back up.  (One variable a row: an array of them is
 // made one wide register tuple, copied at every branch.)
-template <class T, int I, int MOST>
+template <class U, int I, int MOST>
 struct Rows {
-    static __device__ __forceinline__ void move(const char *src, char *dst, int64_t src_stride, int64_t dst_stride, const int *parent, int W, int K,
-                                                bool in_place)
+    typedef typename U::type T;
+    static __device__ __forceinline__ void move(const char *src, char *dst, int64_t src_stride, int64_t dst_stride, Parents parent, int W, int K, bool in_place)
     {
         const int p = I < K ? parent[I] : -1;
         const bool moves = (unsigned)p < (unsigned)W && !(in_place && p == I);   // the same for the workgroup
-        T v{};
+        T v;
         if (moves) v = __builtin_nontemporal_load((const T *)(src + p * src_stride));
-        Rows<T, I + 1, MOST>::move(src, dst, src_stride, dst_stride, parent, W, K, in_place);
+        Rows<U, I + 1, MOST>::move(src, dst, src_stride, dst_stride, parent, W, K, in_place);
         if (moves) __builtin_nontemporal_store(v, (T *)(dst + I * dst_stride));
     }
 };
-template <class T, int MOST>
-struct Rows<T, MOST, MOST> {
-    static __device__ __forceinline__ void move(const char *, char *, int64_t, int64_t, const int *, int, int, bool) {}
+template <class U, int MOST>
+struct Rows<U, MOST, MOST> {
+    static __device__ __forceinline__ void move(const char *, char *, int64_t, int64_t, Parents, int, int, bool) {}
 };
 
 // MOST: rows held in registers, K or more.
-template <class T, int MOST>
-__device__ __forceinline__ void reorder_unit(const StateArgs &a, const StateArg &s, int64_t g, int64_t u, const int *parent, bool in_place)
-{
-    int64_t seg = 0;
-    if (s.units != s.per_segment) seg = (s.units >> 32) == 0 ? (uint32_t)u / (uint32_t)s.per_segment : u / s.per_segment;
-    const int64_t off = (u - seg * s.per_segment) * (int64_t)sizeof(T);
-    const char *src = s.src + g * a.W * s.src_stride + seg * s.src_pitch + off;
-    char *dst = s.dst + g * a.K * s.dst_stride + seg * s.dst_pitch + off;
-    Rows<T, 0, MOST>::move(src, dst, s.src_stride, s.dst_stride, parent, a.W, a.K, in_place);
-}
-
 template <int MOST>
 __global__ __launch_bounds__(kReorderThreads, MOST <= 8 ? 8 : MOST <= 16 ? 5 : MOST <= 32 ? 3 : 1) void beam_reorder_kernel(StateArgs a)
 {
@@ -67,15 +69,25 @@ __global__ __launch_bounds__(kReorderThreads, MOST <= 8 ? 8 : MOST <= 16 ? 5 : M
     const unsigned b = blockIdx.x - s.first_block, g = b / s.blocks;
     const int64_t u = (int64_t)(b - g * s.blocks) * kReorderThreads + threadIdx.x;
     if (u >= s.units) return;
-    const int *parent = a.parent + (int64_t)g * a.K;
+    const Parents parent = (Parents)(a.parent + (int64_t)g * a.K);
     const bool in_place = a.in_place >> n & 1;
-    switch (s.unit) {
-        case 16: reorder_unit<u32x4, MOST>(a, s, g, u, parent, in_place); break;
-        case 8: reorder_unit<uint64_t, MOST>(a, s, g, u, parent, in_place); break;
-        case 4: reorder_unit<uint32_t, MOST>(a, s, g, u, parent, in_place); break;
-        case 2: reorder_unit<uint16_t, MOST>(a, s, g, u, parent, in_place); break;
-        default: reorder_unit<uint8_t, MOST>(a, s, g, u, parent, in_place); break;
+    int64_t seg = 0;
+    if (s.units != s.per_segment) seg = (s.units >> 32) == 0 ? (uint32_t)u / (uint32_t)s.per_segment : u / s.per_segment;
+    const int64_t off = (u - seg * s.per_segment) * 16;
+    const char *src = s.src + (int64_t)g * a.W * s.src_stride + seg * s.src_pitch + off;
+    char *dst = s.dst + (int64_t)g * a.K * s.dst_stride + seg * s.dst_pitch + off;
+    auto move = [&](auto unit, int at) __attribute__((always_inline)) {
+        Rows<decltype(unit), 0, MOST>::move(src + at, dst + at, s.src_stride, s.dst_stride, parent, a.W, a.K, in_place);
+    };
+    const int left = s.segment_bytes - off < 16 ? (int)(s.segment_bytes - off) : 16;
+    if (left == 16) {
+        move(Unit16(), 0);
+        return;
     }
+    if (left & 8) move(Unit8(), 0);
+    if (left & 4) move(Unit4(), left & 8);
+    if (left & 2) move(Unit2(), left & 12);
+    if (left & 1) move(Unit1(), left & 14);
 }
 
 template <class F>
@@ -108,11 +120,8 @@ rdk_status_t launch_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t 
             s.src = (const char *)t.src; s.dst = (char *)t.dst;
             s.src_stride = t.src_stride; s.dst_stride = t.dst_stride;
             s.src_pitch = t.segments > 1 ? t.src_pitch : 0; s.dst_pitch = t.segments > 1 ? t.dst_pitch : 0;
-            uint64_t bits = (uintptr_t)t.src | (uintptr_t)t.dst | (uint64_t)t.src_stride | (uint64_t)t.dst_stride | (uint64_t)s.src_pitch |
-                            (uint64_t)s.dst_pitch | (uint64_t)t.segment_bytes;
-            s.unit = 16;
-            while (bits & (s.unit - 1)) s.unit /= 2;
-            s.per_segment = t.segment_bytes / s.unit;
+            s.segment_bytes = t.segment_bytes;
+            s.per_segment = (t.segment_bytes + 15) / 16;
             s.units = t.segments * s.per_segment;
             const uint64_t per = ((uint64_t)s.units + kReorderThreads - 1) / kReorderThreads;
             if (a.count && blocks + per * G > 0x7FFFFFFFull) break;
