@@ -327,10 +327,10 @@ rdk_status_t rdk_tree_walk(int32_t S, int32_t nodes, int32_t C, const int32_t *c
  *   values[b, :] = the entries themselves (logits are not divided by the temperature), widened to fp32; -inf (logits) or 0 (weights) beside -1.
  *   lse[b]       = log sum_j exp(x_bj / temperature) for logits, log sum_j x_bj for weights (temperature 1); -inf for a row that is
  *                  masked altogether; NaN for a row with a NaN or a logit of +inf.  May be NULL.
- * ids and values are [B, k] without gaps.  1 <= k <= min(N, 128), temperature > 0 and finite.  The ids and values are exact, whatever the
+ * ids and values are [B, k] without gaps.  1 <= k <= min(N, 128), B < 2^24, temperature a positive normal number.  The ids and values are exact, whatever the
  * input; sums run in fp32.  Rows that crowd out the fast way (thousands of entries that tie with the k-th) take a slower one.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, N, k, ldx, temperature), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x or the workspace),
- * RDK_ERR_UNSUPPORTED (k above 128, N above 2^30; weights with a temperature other than 1), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ * RDK_ERR_UNSUPPORTED (k above 128, N above 2^30, B from 2^24 on; weights with a temperature other than 1), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */
 typedef struct {
     int32_t B, N, k;            /* rows, ids, entries kept per row */
@@ -356,12 +356,12 @@ rdk_status_t rdk_topk(const rdk_topk_desc_t *desc, const void *x, rdk_input_kind
  * where the teacher has mass on them.  A drafter row that is masked altogether has s = 0 everywhere.  NaN in a row that counts shows in its loss.
  *   rdk_distill_loss       forward: loss [B] and stats [B, 4] fp32, which the backward call reads (contents not part of the interface).
  *   rdk_distill_grad       backward: dz [B, ldd] of z's type from stats; weight is what comes from above (d / d loss[b], times whatever
- *                          weight the forward call had).  Same z, top_ids, top_logits and temperature as in the forward call.  No workspace.
+ *                          weight the forward call had: a row whose weight was 0 there has 0 here).  Same z, top_ids, top_logits and temperature as in the forward call.  No workspace.
  *   rdk_distill_loss_grad  both at once, for weights known beforehand; z is read once where a row fits the registers.  stats may be NULL.
  * dz may be z itself (same stride), else they must not overlap.  Sums and statistics are held in fp32; a bf16 gradient is rounded once.
- * 1 <= K <= 128; top_ids and top_logits without gaps.
+ * 1 <= K <= 128, B < 2^22, temperature a positive normal number; top_ids and top_logits without gaps.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, n, K, strides, temperature, n other than the kernel's), RDK_ERR_DTYPE, RDK_ERR_ALIGN (z, dz, workspace),
- * RDK_ERR_UNSUPPORTED (K above 128; rows of probabilities), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ * RDK_ERR_UNSUPPORTED (K above 128, B from 2^22 on; rows of probabilities), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */
 typedef struct {
     int32_t B, n, K;            /* positions, drafter slots, teacher entries per position */
@@ -388,7 +388,7 @@ rdk_status_t rdk_distill_loss_grad(const rdk_distill_desc_t *desc, const rdk_ker
  * ascending id): scores_out, parent (beam 0 .. W-1), token, finished_out (the beam was finished, or token == eos), all [G, K]; score -inf,
  * parent -1, token -1, finished 0 where there are fewer.  NaN and +inf in a live row make its scores NaN, which rank first.
  * finished and finished_out may be NULL; eos = -1: no id ends a beam (finished must be NULL then).  Outputs must not overlap the inputs.
- * 1 <= W <= 64, 1 <= K <= 128, N <= 2^30, W N < 2^31, G W < 2^31.
+ * 1 <= W <= 64, 1 <= K <= 128, N <= 2^30, W N < 2^31, G W < 2^24.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (G, W, N, K, ldx, eos, an output that overlaps its input), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x, workspace),
  * RDK_ERR_UNSUPPORTED (limits), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */

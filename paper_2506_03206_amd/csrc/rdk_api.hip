@@ -1,4 +1,5 @@
 // C ABI of the RDK library: argument checks, storage / workspace carving, dispatch to the launchers.
+#include <cfloat>
 #include <atomic>
 #include <chrono>
 #include <cstdlib>
@@ -636,14 +637,17 @@ rdk_status_t rdk_redistribute_verify(const rdk_kernel_t *kernel, rdk_linear_mode
     return launch_sparse_fused(h, c, workspace, (hipStream_t)stream);
 }
 
-static bool temperature_ok(float t) { return t > 0.f && t < INFINITY; }
+static bool temperature_ok(float t) { return t >= FLT_MIN && t <= FLT_MAX; }   // 1 / t and its product with log2(e) are numbers
+
+// Rows of a call: a workgroup each, of at most 256 or 1024 threads, which a launch counts in 32 bits.
+constexpr int32_t kMostRows = (1 << 24) - 1, kMostWideRows = (1 << 22) - 1;
 
 static rdk_status_t check_topk(const rdk_topk_desc_t *d, rdk_input_kind_t kind)
 {
     if (!d) return RDK_ERR_NULL;
     if (!kind_ok(kind)) return RDK_ERR_DTYPE;
     if (d->B < 1 || d->N < 1 || d->k < 1 || d->k > d->N || !temperature_ok(d->temperature)) return RDK_ERR_SHAPE;
-    if (d->k > select_max_entries() || d->N > select_max_ids() || (kind == RDK_PROB_F32 && d->temperature != 1.f)) return RDK_ERR_UNSUPPORTED;
+    if (d->k > select_max_entries() || d->N > select_max_ids() || d->B > kMostRows || (kind == RDK_PROB_F32 && d->temperature != 1.f)) return RDK_ERR_UNSUPPORTED;
     return RDK_OK;
 }
 
@@ -675,7 +679,7 @@ static rdk_status_t check_distill(const rdk_distill_desc_t *d, rdk_input_kind_t 
     if (!d) return RDK_ERR_NULL;
     if (!kind_ok(kind)) return RDK_ERR_DTYPE;
     if (d->B < 1 || d->n < 1 || d->K < 1 || !temperature_ok(d->temperature)) return RDK_ERR_SHAPE;
-    if (d->K > distill_max_entries() || kind == RDK_PROB_F32) return RDK_ERR_UNSUPPORTED;
+    if (d->K > distill_max_entries() || d->B > kMostWideRows || kind == RDK_PROB_F32) return RDK_ERR_UNSUPPORTED;
     return RDK_OK;
 }
 
@@ -760,7 +764,7 @@ static rdk_status_t check_beam(const rdk_beam_desc_t *d, rdk_input_kind_t kind)
     if (!kind_ok(kind)) return RDK_ERR_DTYPE;
     if (d->G < 1 || d->W < 1 || d->N < 1 || d->K < 1 || d->eos < -1 || d->eos >= d->N) return RDK_ERR_SHAPE;
     if (d->W > reorder_max_beams() || d->K > select_max_entries() || d->N > select_max_ids()) return RDK_ERR_UNSUPPORTED;
-    if ((int64_t)d->W * d->N > INT32_MAX || (int64_t)d->G * d->W > INT32_MAX) return RDK_ERR_UNSUPPORTED;
+    if ((int64_t)d->W * d->N > INT32_MAX || (int64_t)d->G * d->W > kMostRows) return RDK_ERR_UNSUPPORTED;
     return RDK_OK;
 }
 

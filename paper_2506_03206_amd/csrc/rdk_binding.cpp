@@ -12,6 +12,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <algorithm>
 #include <vector>
 
 #include <ATen/ATen.h>
@@ -539,7 +540,7 @@ PyObject *beam_select(PyObject *const *a)
     return status(unlocked([&] { return rdk_beam_select(&d, xi.p, xi.kind, xi.ld, si, fi, so, parent, token, fo, w.p, w.bytes, st); }));
 }
 
-// One state of beams for rdk_beam_reorder: its rows as pieces with at most one gap between them.
+// One state of beams for rdk_beam_reorder: its rows as pieces with at most one gap between them, in the order in which they lie in memory.
 rdk_state_t state_of(const at::Tensor &src, const at::Tensor &dst)
 {
     need(src.is_cuda() && dst.is_cuda() && src.scalar_type() == dst.scalar_type() && src.dim() >= 1 && dst.dim() == src.dim(),
@@ -553,14 +554,16 @@ rdk_state_t state_of(const at::Tensor &src, const at::Tensor &dst)
     s.segments = 1;
     int64_t piece = 1;   // elements
     bool whole = true;   // no gap met so far
+    std::vector<int64_t> inner;
     for (int64_t i = src.dim() - 1; i >= 1; --i) {
+        need(dst.size(i) == src.size(i), "a state and its destination have rows of one shape");
+        if (src.size(i) == 0) piece = 0;
+        if (src.size(i) != 1) inner.push_back(i);
+    }
+    if (piece == 0) inner.clear();
+    std::stable_sort(inner.begin(), inner.end(), [&](int64_t a, int64_t b) { return src.stride(a) < src.stride(b); });
+    for (const int64_t i : inner) {
         const int64_t n = src.size(i);
-        need(dst.size(i) == n, "a state and its destination have rows of one shape");
-        if (n == 1) continue;
-        if (n == 0) {
-            piece = 0;
-            break;
-        }
         if (whole && src.stride(i) == piece && dst.stride(i) == piece) {
             piece *= n;
             continue;

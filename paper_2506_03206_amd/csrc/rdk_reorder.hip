@@ -22,6 +22,8 @@ struct Unit1 { typedef unsigned char type; };
 typedef const __attribute__((address_space(4))) int *Parents;
 
 constexpr int kStatesPerLaunch = 24, kReorderThreads = 256, kMaxBeams = 64;
+constexpr unsigned kMostBlocks = 0xFFFFFFFFu / kReorderThreads;   // of a launch: its threads are counted in 32 bits
+constexpr unsigned kMostPerRequest = 1u << 20;                    // of a request; longer rows are moved by several launches
 
 struct StateArg {
     const char *src;
@@ -32,10 +34,12 @@ struct StateArg {
     int64_t segment_bytes;
     unsigned first_block;   // of the launch
     unsigned blocks;        // per request
+    int first_request;      // of the launch
+    int64_t first_unit;
 };
 struct StateArgs {
     StateArg s[kStatesPerLaunch];
-    int count, G, W, K, in_place;   // in_place: a bit per state
+    int count, W, K, in_place;   // in_place: a bit per state
     const int32_t *parent;
 };
 
@@ -66,16 +70,17 @@ __global__ __launch_bounds__(kReorderThreads, MOST <= 8 ? 8 : MOST <= 16 ? 5 : M
     int n = 0;
     while (n + 1 < a.count && blockIdx.x >= a.s[n + 1].first_block) ++n;
     const StateArg &s = a.s[n];
-    const unsigned b = blockIdx.x - s.first_block, g = b / s.blocks;
-    const int64_t u = (int64_t)(b - g * s.blocks) * kReorderThreads + threadIdx.x;
-    if (u >= s.units) return;
-    const Parents parent = (Parents)(a.parent + (int64_t)g * a.K);
+    const unsigned b = blockIdx.x - s.first_block, request = b / s.blocks;
+    const int64_t g = s.first_request + (int64_t)request;
+    const Parents parent = (Parents)(a.parent + g * a.K);
     const bool in_place = a.in_place >> n & 1;
+    const int64_t u = s.first_unit + (int64_t)(b - request * s.blocks) * kReorderThreads + threadIdx.x;
+    if (u >= s.units) return;
     int64_t seg = 0;
     if (s.units != s.per_segment) seg = (s.units >> 32) == 0 ? (uint32_t)u / (uint32_t)s.per_segment : u / s.per_segment;
     const int64_t off = (u - seg * s.per_segment) * 16;
-    const char *src = s.src + (int64_t)g * a.W * s.src_stride + seg * s.src_pitch + off;
-    char *dst = s.dst + (int64_t)g * a.K * s.dst_stride + seg * s.dst_pitch + off;
+    const char *src = s.src + g * a.W * s.src_stride + seg * s.src_pitch + off;
+    char *dst = s.dst + g * a.K * s.dst_stride + seg * s.dst_pitch + off;
     auto move = [&](auto unit, int at) __attribute__((always_inline)) {
         Rows<decltype(unit), 0, MOST>::move(src + at, dst + at, s.src_stride, s.dst_stride, parent, a.W, a.K, in_place);
     };
@@ -106,10 +111,12 @@ int reorder_max_beams() { return kMaxBeams; }
 
 rdk_status_t launch_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *parent, const rdk_state_t *states, int32_t count, hipStream_t st)
 {
+    int32_t request = 0;   // of the state at hand, the first that no launch has, and its first unit
+    int64_t unit = 0;
     for (int done = 0; done < count;) {
         StateArgs a{};
-        a.G = G; a.W = W; a.K = K; a.parent = parent;
-        uint64_t blocks = 0;
+        a.W = W; a.K = K; a.parent = parent;
+        unsigned blocks = 0;
         while (done < count && a.count < kStatesPerLaunch) {
             const rdk_state_t &t = states[done];
             if (t.segments == 0 || t.segment_bytes == 0) {   // nothing of it is filled
@@ -123,18 +130,30 @@ rdk_status_t launch_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t 
             s.segment_bytes = t.segment_bytes;
             s.per_segment = (t.segment_bytes + 15) / 16;
             s.units = t.segments * s.per_segment;
-            const uint64_t per = ((uint64_t)s.units + kReorderThreads - 1) / kReorderThreads;
-            if (a.count && blocks + per * G > 0x7FFFFFFFull) break;
-            s.first_block = (unsigned)blocks;
-            s.blocks = (unsigned)per;
-            blocks += per * G;
+            const uint64_t per = ((uint64_t)(s.units - unit) + kReorderThreads - 1) / kReorderThreads;
+            s.first_block = blocks;
+            s.blocks = per < kMostPerRequest ? (unsigned)per : kMostPerRequest;
+            s.first_request = request;
+            s.first_unit = unit;
+            const unsigned room = (kMostBlocks - blocks) / s.blocks, left = (unsigned)(G - request);
+            if (room == 0) break;
+            const unsigned requests = left < room ? left : room;
+            blocks += requests * s.blocks;
             if (t.src == t.dst) a.in_place |= 1 << a.count;
             a.s[a.count++] = s;
-            ++done;
+            request += (int32_t)requests;
+            if (request == G) {
+                request = 0;
+                unit += (int64_t)s.blocks * kReorderThreads;
+            }
+            if (unit >= s.units) {
+                unit = 0;
+                ++done;
+            }
         }
         if (!a.count) break;
         with_rows(K, [&](auto rows) {
-            RDK_TIMED_LAUNCH("beam_reorder_kernel", (beam_reorder_kernel<decltype(rows)::value>), dim3((unsigned)blocks), dim3(kReorderThreads), 0, st, a);
+            RDK_TIMED_LAUNCH("beam_reorder_kernel", (beam_reorder_kernel<decltype(rows)::value>), dim3(blocks), dim3(kReorderThreads), 0, st, a);
         });
         RDK_LAUNCH_CHECK("beam_reorder_kernel");
     }

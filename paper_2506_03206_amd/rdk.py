@@ -465,7 +465,7 @@ def rdk_beam_select(x, scores, K=None, x_kind="logit", finished=None, eos=-1, ou
 
 def rdk_beam_reorder(states, parent, W=None, out=None):
     """Row i of request g of every state becomes row parent[g, i]: in place, or into `out` ([G*K, ...] each).  states: tensors
-    [G*W, ...] whose rows have at most one gap (a cache of which a part is filled).  Returns the reordered states."""
+    [G*W, ...] whose rows have at most one gap (a cache of which a part is filled) in the order of their memory.  Returns the reordered states."""
     _check((_native or native()).beam_reorder(states, parent, parent.shape[1] if W is None else W, out), "rdk_beam_reorder")
     return list(states) if out is None else list(out)
 

@@ -232,6 +232,38 @@ def test_caches_of_which_a_part_is_filled():
     assert torch.equal(wide[:, :, :9], small.repeat_interleave(W, 0)) and (wide[:, :, 9:] == 0).all()
 
 
+def test_rows_whose_memory_has_another_order():
+    """Caches stored position by position and looked at head by head, and a source and a destination of one such order."""
+    from paper_2506_03206_amd import rdk
+    G, W, H, room, D = 2, 3, 5, 11, 6
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    parent = torch.randint(0, W, (G, W), generator=g, device="cuda", dtype=torch.int32)
+    for n in (room, 7):
+        memory = torch.randn((G * W, room, H, D), generator=g, device="cuda")
+        x = memory[:, :n].transpose(1, 2)                                            # [rows, heads, positions, D]
+        before = memory.clone()
+        out = torch.zeros((G * W, n, H, D), device="cuda")
+        rdk.rdk_beam_reorder([x], parent, W, [out.transpose(1, 2)])
+        assert torch.equal(out, moved(before[:, :n], parent, W))
+        rdk.rdk_beam_reorder([x], parent)
+        assert torch.equal(memory[:, :n], moved(before[:, :n], parent, W)) and torch.equal(memory[:, n:], before[:, n:])
+    with pytest.raises(AssertionError):                                              # rows of one shape, but not of one order
+        rdk.rdk_beam_reorder([x], parent, W, [torch.zeros((G * W, H, n, D), device="cuda")])
+
+
+def test_more_requests_than_a_launch_has_workgroups():
+    from paper_2506_03206_amd import rdk
+    G = (1 << 24) + 5                                                                # a workgroup each, and 2^24 - 1 at once
+    x = torch.arange(2 * G, device="cuda").to(torch.uint8).view(2 * G, 1)
+    parent = torch.ones((G, 1), dtype=torch.int32, device="cuda")
+    out = torch.zeros((G, 1), dtype=torch.uint8, device="cuda")
+    other = torch.full((G, 1), 7, dtype=torch.uint8, device="cuda")
+    twin = torch.stack([other, x.view(G, 2, 1)[:, 0]], 1).reshape(2 * G, 1)
+    rdk.rdk_beam_reorder([x, twin], parent, 2, [out, other])
+    assert torch.equal(out[:, 0], x[1::2, 0]) and torch.equal(other[:, 0], x[0::2, 0])
+
+
 def test_offsets_beyond_32_bits():
     from paper_2506_03206_amd import rdk
     W, n, stride = 3, 1 << 20, (1 << 32) + 4096

@@ -127,6 +127,29 @@ def test_reorder_refusals(rdk):
     assert call(state(dst=0x10000000), K=3) == SHAPE                                  # in place, but fewer rows
 
 
+def test_limits_of_a_launch(rdk):
+    """More rows than a launch has workgroups for, and temperatures whose reciprocal is no number."""
+    L, need = rdk.lib(), ctypes.c_size_t()
+
+    def topk(B, t=1.0):
+        d = rdk.TopkDesc(B=B, N=10, k=3, temperature=t)
+        return L.rdk_topk_workspace_bytes(ctypes.byref(d), 1, ctypes.byref(need))
+
+    def distill(B, t=1.0):
+        d = rdk.DistillDesc(B=B, n=10, K=3, temperature=t)
+        return L.rdk_distill_workspace_bytes(ctypes.byref(d), 1, ctypes.byref(need))
+
+    def beam(G, W):
+        d = rdk.BeamDesc(G=G, W=W, N=10, K=3, eos=-1)
+        return L.rdk_beam_select_workspace_bytes(ctypes.byref(d), 1, ctypes.byref(need))
+
+    assert topk((1 << 24) - 1) == 0 and topk(1 << 24) == UNSUPPORTED
+    assert distill((1 << 22) - 1) == 0 and distill(1 << 22) == UNSUPPORTED
+    assert beam(((1 << 24) - 1) // 3, 3) == 0 and beam(1 << 18, 64) == UNSUPPORTED
+    for call in (topk, distill):
+        assert call(4, 1.2e-38) == 0 and call(4, 1e-39) == SHAPE and call(4, 3e38) == 0
+
+
 def test_descriptors_match_the_header(rdk, tmp_path):
     src = tmp_path / "layout.c"
     mirrors = {"rdk_topk_desc_t": rdk.TopkDesc, "rdk_distill_desc_t": rdk.DistillDesc, "rdk_beam_desc_t": rdk.BeamDesc, "rdk_state_t": rdk.State}
