@@ -398,21 +398,27 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     }
     if (a.entries) {
         // the best of every part and beam first, then the second best of every one, ...
-        const int64_t group = row / a.W;
-        if (tid < a.k) a.entries[((group * a.k + tid) * a.parts + part) * a.W + (row - group * a.W)] = tid < n ? sh.slow.sorted[tid] : 0;
+        const uint32_t group = (uint32_t)row / (uint32_t)a.W, beam = (uint32_t)row % (uint32_t)a.W;
+        if (tid < a.k) a.entries[(((int64_t)group * a.k + tid) * a.parts + part) * a.W + beam] = tid < n ? sh.slow.sorted[tid] : 0;
         if (tid == 0) a.stat[row * a.parts + part] = stat;
         return;
     }
     write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, stat);
 }
 
-// Partial statistics of a row brought together, by a wavefront.
+// A lane's first partial statistics of a row.
 template <int KIND>
-__device__ __forceinline__ SoftStat merge_stats(const SoftStat *stat, int parts, float c)
+__device__ __forceinline__ SoftStat first_stat(const SoftStat *stat, int parts)
 {
-    constexpr float none = KIND == RDK_PROB_F32 ? 0.f : -INFINITY;
-    SoftStat r{none, 0.f};
-    for (int p = lane_id(); p < parts; p += kWave) {
+    return lane_id() < parts ? stat[lane_id()] : SoftStat{KIND == RDK_PROB_F32 ? 0.f : -INFINITY, 0.f};
+}
+
+// Partial statistics of a row brought together, by a wavefront that has read the first.
+template <int KIND>
+__device__ __forceinline__ SoftStat merge_stats(SoftStat first, const SoftStat *stat, int parts, float c)
+{
+    SoftStat r = first;
+    for (int p = lane_id() + kWave; p < parts; p += kWave) {
         const SoftStat o = stat[p];
         if (KIND == RDK_PROB_F32) {
             r.m = fmaxf(r.m, o.m);
@@ -441,7 +447,7 @@ struct MergeShared {
 // own (0: none).  By a bound as above: the entries come best places first, so no entry of a thread is much larger than its first.  The
 // largest of four wavefronts are looked at together; sixteen find a bound each, of which the least is taken (beams stand next to one
 // another: every wavefront has its share of the best ones).
-template <int THREADS, int EACH>
+template <int THREADS, int EACH, int BITS>
 __device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int count, int k, MergeShared<THREADS> &sh)
 {
     constexpr int kWaves = THREADS / kWave;
@@ -458,7 +464,7 @@ __device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int c
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) keys[w] = sh.keys[w * kWave + lane_id()];
 #pragma unroll 4
-        for (int bit = 31; bit >= 0; --bit) {
+        for (int bit = 31; bit >= 32 - BITS; --bit) {
             const uint32_t tried = bound | (1u << bit);
             int n = 0;
 #pragma unroll
@@ -467,7 +473,7 @@ __device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int c
         }
     } else {
         const int waves = min((count + kWave - 1) / kWave, kWaves);
-        const uint32_t b = tid / kWave < waves ? wave_nth<32>(entry_key(best), (k + waves - 1) / waves) : 0xFFFFFFFFu;
+        const uint32_t b = tid / kWave < waves ? wave_nth<BITS>(entry_key(best), (k + waves - 1) / waves) : 0xFFFFFFFFu;
         if (lane_id() == 0) sh.keys[tid / kWave] = b;
         __syncthreads();
         bound = sh.keys[0];
@@ -515,8 +521,8 @@ __global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a)
         own[i] = at < count ? a.entries[row * count + at] : 0;
     }
     SoftStat stat{0.f, 0.f};
-    if (threadIdx.x < kWave) stat = merge_stats<KIND>(a.stat + row * a.parts, a.parts, a.c);
-    const int n = select_entries<kTopThreads, EACH>(own, count, a.k, sh);
+    if (threadIdx.x < kWave) stat = merge_stats<KIND>(first_stat<KIND>(a.stat + row * a.parts, a.parts), a.stat + row * a.parts, a.parts, a.c);
+    const int n = select_entries<kTopThreads, EACH, KIND == RDK_LOGIT_BF16 ? 16 : 24>(own, count, a.k, sh);
     write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, stat);
 }
 
@@ -548,16 +554,29 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamArgs a)
         const int at = i * THREADS + tid;
         own[i] = at < count ? a.entries[g * count + at] : 0;
     }
-    for (int w = tid / kWave; w < a.W; w += THREADS / kWave) {
-        const float score = a.scores[b0 + w];
-        const int state = score == -INFINITY ? 0 : a.finished && a.finished[b0 + w] ? 1 : 2;
-        SoftStat st{0.f, 0.f};
-        if (state == 2) st = merge_stats<KIND>(a.stat + (b0 + w) * a.parts, a.parts, kLog2e);
-        if (lane_id() == 0) {
-            beam_score[w] = score;
-            beam_state[w] = state;
-            beam_m[w] = weight_reference(st.m);
-            beam_log[w] = KIND == RDK_PROB_F32 ? st.s : logf(st.s);
+    constexpr int kWaves = THREADS / kWave, kAhead = 4;
+    const float scores = lane_id() < a.W ? a.scores[b0 + lane_id()] : -INFINITY;   // a beam to a lane
+    const int over = a.finished && lane_id() < a.W ? a.finished[b0 + lane_id()] : 0;
+#pragma unroll 1
+    for (int first = tid / kWave; first < a.W; first += kAhead * kWaves) {
+        SoftStat ahead[kAhead];   // (of beams without a row whatever lay there, and not used)
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) ahead[j] = first_stat<KIND>(a.stat + (b0 + min(first + j * kWaves, a.W - 1)) * a.parts, a.parts);
+#pragma unroll 1
+        for (int j = 0; j < kAhead && first + j * kWaves < a.W; ++j) {
+            const int w = first + j * kWaves;
+            const float score = __shfl(scores, w);
+            const int state = score == -INFINITY ? 0 : __shfl(over, w) ? 1 : 2;
+            SoftStat st = merge_stats<KIND>(ahead[0], a.stat + (b0 + w) * a.parts, a.parts, kLog2e);
+            if (state != 2) st = SoftStat{0.f, 0.f};
+            if (lane_id() == 0) {
+                beam_score[w] = score;
+                beam_state[w] = state;
+                beam_m[w] = weight_reference(st.m);
+                beam_log[w] = KIND == RDK_PROB_F32 ? st.s : logf(st.s);
+            }
+#pragma unroll
+            for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
         }
     }
     __syncthreads();
@@ -578,7 +597,7 @@ __global__ __launch_bounds__(THREADS) void beam_merge_kernel(BeamArgs a)
         }
         own[i] = e;
     }
-    const int n = select_entries<THREADS, EACH>(own, count, a.K, sh);
+    const int n = select_entries<THREADS, EACH, 24>(own, count, a.K, sh);
     if (tid < a.K) {
         const bool in = tid < n;
         const uint64_t e = in ? sh.slow.sorted[tid] : 0;
