@@ -52,7 +52,7 @@ struct Rows {
     {
         const int p = I < K ? parent[I] : -1;
         const bool moves = (unsigned)p < (unsigned)W && !(in_place && p == I);   // the same for the workgroup
-        T v;
+        T v{};   // (unset, the same code takes 2 to 8 % longer: 0.54 GB of caches 111 to 124 us, set 108 to 119)
         if (moves) v = __builtin_nontemporal_load((const T *)(src + p * src_stride));
         Rows<U, I + 1, MOST>::move(src, dst, src_stride, dst_stride, parent, W, K, in_place);
         if (moves) __builtin_nontemporal_store(v, (T *)(dst + I * dst_stride));
