@@ -3,8 +3,8 @@
 // A thread owns one unit (16 bytes, less at the end of a piece) of a row's bytes for every beam of a request: it reads the units of all rows that
 // change before it writes any of them, so a reorder in place needs no scratch and no order between threads.  Units lie at any address
 // (the memory pipe takes them: five beams with rows of 8 pieces of 65934 bytes move at 4.3 TB/s, in units as small as the sizes' common
-// divisor at 1.4).  Bound by HBM: 5.8 to 6.1 TB/s of the bytes of rows that change and are needed, where a copy kernel reaches 6.0 to 6.4;
-// non-temporal accesses are worth an eighth (16 requests of 4 beams, 0.54 GB of caches: 137 us without, 131 stores alone, 120 both).
+// divisor at 1.4).  Bound by HBM: 5.8 to 6.2 TB/s of the bytes of rows that change and are needed, where a copy kernel reaches 6.0 to 6.4;
+// non-temporal accesses are worth an eighth (16 requests of 4 beams, 0.54 GB of caches: 137 us without, 131 stores alone, 119 both).
 #include "rdk_vec.hpp"
 
 namespace rdk {
