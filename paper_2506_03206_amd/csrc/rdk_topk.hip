@@ -22,7 +22,7 @@ struct TopArgs {
     int64_t ldx;
     int N, k, parts, part_len;
     float inv_t, c;         // c = log2(e) / temperature
-    float limit, margin;    // rows with a maximum beyond +-limit take the slow way; 60 / c
+    float limit, margin;    // rows of logits with a maximum beyond +-limit are summed anew; 60 / c
     // rows of beams that have no candidates among the ids are passed over
     const float *scores;
     const uint8_t *finished;
@@ -66,14 +66,13 @@ __device__ __forceinline__ float wave_bound(float largest, int nth)
     return key_value(KIND == RDK_LOGIT_BF16 && !(key >> 31) ? key | 0xFFFFu : key);   // (the key of a negative bf16 value ends in ones)
 }
 
-// The sum of exp((x - m) / T) over a part, for a largest value m so far from zero that the product with 1 / T leaves the range.
+// The sum of exp((x - m) / T) over a part, for a largest value m so far from zero that the rounding of its product with 1 / T is no small number.
 template <int KIND>
 __device__ __forceinline__ float wide_sum(const TopArgs &a, const void *xr, int begin, int end, float m, TopShared &sh)
 {
     float s = 0.f;
     for (int i = begin + (int)threadIdx.x; i < end; i += kTopThreads) {
-        const float x = load1<KIND>(xr, i);
-        s += KIND == RDK_PROB_F32 ? x : __builtin_amdgcn_exp2f((x - m) * a.c);
+        s += __builtin_amdgcn_exp2f((load1<KIND>(xr, i) - m) * a.c);
     }
     s = wave_sum(s);
     __syncthreads();
@@ -199,7 +198,8 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     float m = none, s = 0.f, ref = 0.f, high = -INFINITY;   // ref: reference of the lane's exponents, times c; high: where it is replaced
     float last = none;
     // Exponents are relative to a value that the lane has seen, not the largest: it is replaced only when a vector exceeds it by 2^60, so the
-    // maximum is nothing that the exponentials wait for.
+    // maximum is nothing that the exponentials wait for.  References are rounded products of a value and c, and kept within +-limit,
+    // where the rounding is below 1 (at 1e10 it is hundreds, and its exponential no number); rows whose maximum lies outside are summed anew.
     auto raise = [&](float x) __attribute__((always_inline)) {
         const float held = fminf(fmaxf(x, -a.limit), a.limit), to = held * a.c;
         s = s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f(ref - to);
@@ -324,8 +324,8 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
             stat.s += sh.wave_s[w] == 0.f ? 0.f : sh.wave_s[w] * __builtin_amdgcn_exp2f(by - to);
         }
         stat.s *= __builtin_amdgcn_exp2f(-fmaf(held, a.c, -to));   // the rounding of the reference itself
+        if (stat.m > -INFINITY && fabsf(stat.m) > a.limit) stat.s = wide_sum<KIND>(a, xr, begin, end, stat.m, sh);
     }
-    if (stat.m > -INFINITY && fabsf(stat.m) > a.limit) stat.s = wide_sum<KIND>(a, xr, begin, end, stat.m, sh);
     const bool nan = stat.s != stat.s;
     bool all = max(max(sh.noted[0], sh.noted[1]), max(sh.noted[2], sh.noted[3])) > kNoted;   // the whole part is sifted
     int n = 0, stage = 0;   // 0: what reaches the bound; 1: the bound to the last bit; 2: what exceeds it
@@ -665,7 +665,8 @@ TopArgs part_args(RowInput x, int N, int k, Parts parts, float temperature)
     a.inv_t = 1.f / temperature;
     a.c = a.inv_t * kLog2e;
     a.margin = 60.f / a.c;
-    a.limit = 1.2676506e30f / (a.c > 1.f ? a.c : 1.f);   // 2^100: the product with c stays in range
+    // 2^24 / c: the product of a value and c is rounded by 1/2 at most, and exp2 of that is no more than a factor of the sums.  (2^100 at most: c may be tiny.)
+    a.limit = a.c > 0x1p-76f ? 0x1p24f / a.c : 0x1p100f;
     return a;
 }
 
