@@ -353,7 +353,8 @@ rdk_status_t rdk_topk(const rdk_topk_desc_t *desc, const void *x, rdk_input_kind
  *     loss[b] = w (sum_A t (log t - log s) + r (log r - log rho)),
  *     dz[b, j] = w / T (s_j - t_j) on A,  w / T s_j (1 - r / rho) elsewhere;    without a slot outside A as if teacher_lse were NULL.
  * A row of weight 0 has loss 0 and gradient 0 whatever its logits hold (they are not read).  Masked logits (-inf) have s = 0: the loss is +inf
- * where the teacher has mass on them.  A drafter row that is masked altogether has s = 0 everywhere.  NaN in a row that counts shows in its loss.
+ * where the teacher has mass on them, and only there (finite logits, however far apart, give what the formulas give).  A drafter row that is masked
+ * altogether has s = 0 everywhere.  NaN in a row that counts shows in its loss.
  *   rdk_distill_loss       forward: loss [B] and stats [B, 4] fp32, which the backward call reads (contents not part of the interface).
  *   rdk_distill_grad       backward: dz [B, ldd] of z's type from stats; weight is what comes from above (d / d loss[b], times whatever
  *                          weight the forward call had: a row whose weight was 0 there has 0 here).  Same z, top_ids, top_logits and temperature as in the forward call.  No workspace.

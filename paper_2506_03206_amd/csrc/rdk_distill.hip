@@ -3,7 +3,9 @@
 // With s = softmax(z / T) and the teacher's probabilities t on the slots A of its entries:  loss = sum_A t (log t - log s), and where the teacher's
 // remainder r is counted too, + r (log r - log rho) with rho = sum of s outside A.  Gradient:  (s - t) / T on A,  s (1 - r / rho) / T outside.
 // rho is summed over the slots outside A by themselves (a bitmap of A in LDS): as 1 - sum_A s it would be lost to rounding for a drafter
-// that is sure of its top entries.
+// that is sure of its top entries.  The sum is relative to the largest logit outside A and never brought to the row's: a drafter surer still has a rho that
+// fp32 does not hold beside 1, where log rho and the softmax over the slots outside alone are ordinary numbers.  With e_j = exp((z_j - that logit) / T)
+// the gradient outside is (rho / sum e - r / sum e) e_j / T, whose first term may vanish.
 #include "rdk_vec.hpp"
 
 namespace rdk {
@@ -28,7 +30,7 @@ struct DistillArgs {
     const int32_t *top_ids;
     const float *top_logits, *teacher_lse, *weight;
     float *loss;
-    float4 *stats;            // reference of the exponents, 1 / sum, coefficient of s outside A, constant of t
+    float4 *stats;            // what stats_of() says
     SoftStat *part;           // [B, parts]
     void *dz;
     int64_t ldd;
@@ -226,27 +228,39 @@ __device__ __forceinline__ SoftStat entry_stat(const Entries &t, const float (&z
     return st;
 }
 
-// Factor of s outside A in the gradient.
-__device__ __forceinline__ float outside_of(bool remainder, float r, int held, float total, float rest)
+// Factor of exp((z - rest.m) / T) outside A in the gradient, with inv = 1 / the row's sum, relative to ref.  (Without the remainder rest is the row's.)
+__device__ __forceinline__ float outside_of(bool remainder, float r, int held, float inv, float ref, SoftStat rest, float c)
 {
-    if (!remainder) return held ? 1.f : 0.f;
-    return rest == 0.f ? 1.f : 1.f - r * total / rest;
+    if (!remainder) return held ? inv : 0.f;
+    return rest.s == 0.f ? 0.f : soft_term(weight_reference(rest.m), ref, c) * inv - r / rest.s;
 }
 
-// The row's loss, by one wavefront: sums relative to ref, of the whole row and of its slots outside A.
+// What the backward call reads of a row: a reference of exponents, 1 / the row's sum, the factor of exp((z - reference) / T) outside A, the constant of t.
+// The reference is the row's, unless the largest logit outside A lies more than kFar powers of two below: then exponentials outside would leave the range that is
+// left below them, the reference is that logit, and 1 / sum, relative to the largest logit at the entries, has its sign turned.
+constexpr float kFar = 24.f;
+__device__ __forceinline__ float4 stats_of(const Teacher &o, float inv, float ref, SoftStat rest, float outside, float c)
+{
+    const float down = (weight_reference(rest.m) - ref) * c;
+    if (!o.remainder || rest.s == 0.f) return make_float4(ref, inv, outside, (float)o.constant);
+    if (down < -kFar) return make_float4(rest.m, -inv, outside, (float)o.constant);
+    return make_float4(ref, inv, inv - (float)o.r / (rest.s * __builtin_amdgcn_exp2f(down)), (float)o.constant);
+}
+
+// The row's loss, by one wavefront: total is the sum of the whole row relative to ref, rest that of its slots outside A relative to its own largest logit.
 __device__ __forceinline__ double loss_of(const DistillArgs &a, const Entries &t, const float (&zt)[kPerLane], const Teacher &o, float ref, float total,
-                                          float rest)
+                                          SoftStat rest)
 {
     const double log_total = log((double)total);
     double loss = 0.;
 #pragma unroll
     for (int j = 0; j < kPerLane; ++j)
         if (o.p[j] != 0.f) {
-            const double log_s = total == 0.f ? -INFINITY : (double)(zt[j] - ref) * a.inv_t - log_total;
+            const double log_s = total == 0.f ? -INFINITY : ((double)zt[j] - ref) * a.inv_t - log_total;
             loss += o.p[j] * (o.log_t[j] - log_s);
         }
     loss = wave_sum(loss);
-    if (o.remainder && o.r != 0.) loss += rest == 0.f ? INFINITY : o.r * log(o.r * total / rest);
+    if (o.remainder && o.r != 0.) loss += rest.s == 0.f ? INFINITY : o.r * (log(o.r * total / rest.s) - ((double)rest.m - ref) * a.inv_t);
     return loss;
 }
 
@@ -271,11 +285,11 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
     for (int p = lane_id(); p < a.parts; p += kWave) st = merge_at(st, a.part[row * a.parts + p], c);
     st = wave_merge_at(st, c);
     const SoftStat at = REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f}, all = merge_at(st, at, c);
-    const float ref = weight_reference(all.m), rest = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
-    const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
+    const float ref = weight_reference(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
+    const double loss = loss_of(a, t, zt, o, ref, all.s, st);
     if (threadIdx.x == 0) {
         a.loss[row] = (float)(w * loss);
-        a.stats[row] = make_float4(ref, all.s == 0.f ? 0.f : 1.f / all.s, outside_of(o.remainder, (float)o.r, o.held, all.s, rest), (float)o.constant);
+        a.stats[row] = stats_of(o, inv, ref, st, outside_of(o.remainder, (float)o.r, o.held, inv, ref, st, c), c);
     }
 }
 
@@ -425,18 +439,16 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
         if (lane_id() == 0) waves[tid / kWave] = st;
     }
     __syncthreads();   // (the logits at the entries have been read too: dz may be z)
-    float top = REST ? entries.m : -INFINITY;
-    for (int k = 0; k < kWaves; ++k) top = fmaxf(top, waves[k].m);
-    const float ref = weight_reference(top);
-    float rest = 0.f;
-    for (int k = 0; k < kWaves; ++k) rest += waves[k].s == 0.f ? 0.f : waves[k].s * soft_term(weight_reference(waves[k].m), ref, c);
-    float total = rest;
-    if (REST) total += entries.s == 0.f ? 0.f : entries.s * soft_term(weight_reference(entries.m), ref, c);
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    const float outside = outside_of(REST && kept.remainder, (float)kept.r, kept.held, total, rest), wt = w * a.inv_t;
+    SoftStat rest{-INFINITY, 0.f};
+    for (int k = 0; k < kWaves; ++k) rest.m = fmaxf(rest.m, waves[k].m);
+    const float rest_ref = weight_reference(rest.m);
+    for (int k = 0; k < kWaves; ++k) rest.s += waves[k].s == 0.f ? 0.f : waves[k].s * soft_term(weight_reference(waves[k].m), rest_ref, c);
+    const SoftStat all = REST ? merge_at(rest, entries, c) : rest;
+    const float ref = weight_reference(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
+    const float outside = outside_of(REST && kept.remainder, (float)kept.r, kept.held, inv, ref, rest, c), wt = w * a.inv_t;
     if (GRAD) {
-        const float scale = wt * inv * outside;
-        const float own_scale = own_s == 0.f ? 0.f : scale * soft_term(own_ref, ref, c);
+        const float scale = wt * outside;
+        const float own_scale = own_s == 0.f ? 0.f : scale * soft_term(own_ref, rest_ref, c);
         if (!follows) {
 #pragma unroll
             for (int j = 0; j < VECS; ++j)
@@ -446,7 +458,7 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
                         V::to(raw[j], v);
                     }
 #pragma unroll
-                    for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], ref, c);
+                    for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], rest_ref, c);
                     V::store_at((char *)dr + j * THREADS * 16, tid * 16, V::kLen, V::from(v));
                 }
             if (tid < behind) V::store1(dr, whole * V::kLen + tid, own_scale * e_last);
@@ -457,10 +469,10 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
     Teacher o;
     if (follows) {
         kept.get(t, zt, o);
-        const double loss = loss_of(a, t, zt, o, ref, total, rest);
+        const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
         if (lane_id() == 0) {
             a.loss[row] = (float)(w * loss);
-            if (a.stats) a.stats[row] = make_float4(ref, inv, outside, (float)o.constant);
+            if (a.stats) a.stats[row] = stats_of(o, inv, ref, rest, outside, c);
         }
     }
     if (!GRAD) return;
@@ -575,72 +587,88 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
     SoftStat st = lane_id() < kWaves ? waves[lane_id()] : SoftStat{-INFINITY, 0.f};
     st = wave_merge_at(st, c);
     const SoftStat all = merge_at(st, REST ? entries : SoftStat{-INFINITY, 0.f}, c);
-    const float ref = weight_reference(all.m), rest = st.s == 0.f ? 0.f : st.s * soft_term(weight_reference(st.m), ref, c);
+    const float ref = weight_reference(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
     Entries t;
     float zt[kPerLane];
     Teacher o;
     kept.get(t, zt, o);
-    const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
+    const double loss = loss_of(a, t, zt, o, ref, all.s, st);
     if (lane_id() == 0) {
         a.loss[row] = (float)(w * loss);
-        a.stats[row] = make_float4(ref, all.s == 0.f ? 0.f : 1.f / all.s, outside_of(o.remainder, (float)o.r, o.held, all.s, rest), (float)o.constant);
+        a.stats[row] = stats_of(o, inv, ref, st, outside_of(o.remainder, (float)o.r, o.held, inv, ref, st, c), c);
     }
 }
 
 // dz of a part of a row, whose logits lie in the registers; the entries as in distill_row_kernel.  Bound by HBM: 1024 bf16 rows of
 // 16384 (an eighth of weight 0) 8 us = 7.8 TB/s read and written, z out of the last-level cache, which holds it from the forward call.
+// A row of two references (stats_of) needs the logits of all its entries: over z itself they stand only until another workgroup writes its part, so
+// the first one goes over the whole of such a row.
 template <int KIND>
 __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(DistillArgs a)
 {
     typedef Vec<KIND> V;
     constexpr int kSlots = kDistillThreads * kGradVecs * V::kLen;
     const int64_t row = blockIdx.x / a.grad_parts;
-    const int begin = (int)(blockIdx.x % a.grad_parts) * kSlots, here = min(a.n - begin, kSlots), tid = threadIdx.x;
+    const int part = blockIdx.x % a.grad_parts, begin = part * kSlots, tid = threadIdx.x;
     const bool follows = tid >= kDistillThreads;
-    const void *whole_row = row_ptr<KIND>(a.z, a.ldz, row);
-    const char *zr = (const char *)whole_row + (int64_t)begin * V::kSize;
-    char *dr = (char *)const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row)) + (int64_t)begin * V::kSize;
+    const char *zr = (const char *)row_ptr<KIND>(a.z, a.ldz, row);
+    char *dr = (char *)const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row));
     const float w = a.weight ? a.weight[row] : 1.f;
     if (w == 0.f) {
+        const int end = min(a.n, begin + kSlots);
         const u32x4 zero{0, 0, 0, 0};
-        for (int i = tid * V::kLen; i < here; i += (kDistillThreads + kWave) * V::kLen) V::store(dr, i, here, zero);
+        for (int i = begin + tid * V::kLen; i < end; i += (kDistillThreads + kWave) * V::kLen) V::store(dr, i, end, zero);
         return;
     }
     u32x4 raw[kGradVecs];
     Entries t;
     float zt[kPerLane];
+    auto load_part = [&](int from) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kGradVecs; ++j) {
+            const int left = min(a.n - from, kSlots) - (j * kDistillThreads + tid) * V::kLen;
+            raw[j] = left > 0 ? V::load_at(zr + (int64_t)from * V::kSize + j * kDistillThreads * 16, tid * 16, left) : V::fill();
+        }
+    };
     if (follows) {
         t = row_entries(a, row);
-        entry_logits<KIND>(whole_row, t, zt);
+        entry_logits<KIND>(zr, t, zt);
     } else {
-#pragma unroll
-        for (int j = 0; j < kGradVecs; ++j) {
-            const int left = here - (j * kDistillThreads + tid) * V::kLen;
-            raw[j] = left > 0 ? V::load_at(zr + j * kDistillThreads * 16, tid * 16, left) : V::fill();
-        }
+        load_part(begin);
     }
     const float4 stats = a.stats[row];
-    const float c = a.inv_t * kLog2e, wt = w * a.inv_t, scale = stats.y * stats.z * wt;
+    const bool two = stats.y < 0.f, alone = two && a.in_place && a.grad_parts > 1;
+    if (alone && part > 0) return;
+    const int end = alone ? a.n : min(a.n, begin + kSlots);
+    const float c = a.inv_t * kLog2e, wt = w * a.inv_t, scale = stats.z * wt;
     if (a.in_place) __syncthreads();   // the logits at the entries have been read before anything is written
     if (!follows) {
+#pragma unroll 1
+        for (int from = begin;;) {
 #pragma unroll
-        for (int j = 0; j < kGradVecs; ++j) {
-            const int left = here - (j * kDistillThreads + tid) * V::kLen;
-            if (left > 0) {
-                float v[V::kLen];
-                V::to(raw[j], v);
+            for (int j = 0; j < kGradVecs; ++j) {
+                const int left = min(a.n - from, kSlots) - (j * kDistillThreads + tid) * V::kLen;
+                if (left > 0) {
+                    float v[V::kLen];
+                    V::to(raw[j], v);
 #pragma unroll
-                for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
-                V::store_at(dr + j * kDistillThreads * 16, tid * 16, left, V::from(v));
+                    for (int e = 0; e < V::kLen; ++e) v[e] = scale * soft_term(v[e], stats.x, c);
+                    V::store_at(dr + (int64_t)from * V::kSize + j * kDistillThreads * 16, tid * 16, left, V::from(v));
+                }
             }
+            from += kSlots;
+            if (from >= end) break;
+            load_part(from);
         }
     }
     __syncthreads();
     if (follows) {
+        const float ref = two ? weight_reference(wave_max(fmaxf(zt[0], zt[1]))) : stats.x, inv = fabsf(stats.y);
+        static_assert(kPerLane == 2, "the largest logit at the entries is formed of two to a lane");
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
-            if (t.slot[j] >= begin && t.slot[j] < begin + here)
-                V::store1(dr, t.slot[j] - begin, wt * (soft_term(zt[j], stats.x, c) * stats.y - expf(t.v[j] * a.inv_t - stats.w)));
+            if (t.slot[j] >= begin && t.slot[j] < end)
+                V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - expf(t.v[j] * a.inv_t - stats.w)));
     }
 }
 
@@ -666,8 +694,14 @@ int parts_of(int n, rdk_input_kind_t kind)
     return (n - 1) / slots + 1;
 }
 
+int grad_parts_of(int n, rdk_input_kind_t kind)
+{
+    const int slots = kDistillThreads * kGradVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4);
+    return (n - 1) / slots + 1;
+}
+
 DistillArgs arguments(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
-                      const float *weight)
+                      const float *weight, void *dz, int64_t ldd)
 {
     DistillArgs a{};
     a.z = z.ptr; a.ldz = z.ld;
@@ -676,15 +710,15 @@ DistillArgs arguments(const rdk_distill_desc_t &d, const KernelHandle *h, RowInp
     a.n = d.n; a.K = d.K; a.inv_t = 1.f / d.temperature;
     a.top_ids = top_ids; a.top_logits = top_logits; a.weight = weight;
     a.parts = parts_of(d.n, z.kind);
+    a.grad_parts = grad_parts_of(d.n, z.kind);
+    a.dz = dz; a.ldd = ldd;
+    a.in_place = dz == z.ptr;
     return a;
 }
 
 template <int KIND>
-rdk_status_t launch_grad(DistillArgs a, int32_t B, hipStream_t st)
+rdk_status_t launch_grad(const DistillArgs &a, int32_t B, hipStream_t st)
 {
-    constexpr int kSlots = kDistillThreads * kGradVecs * Vec<KIND>::kLen;
-    a.grad_parts = (a.n - 1) / kSlots + 1;
-    a.in_place = a.dz == a.z;
     RDK_TIMED_LAUNCH("distill_grad_kernel", (distill_grad_kernel<KIND>), dim3((unsigned)B * a.grad_parts), dim3(kDistillThreads + kWave), 0, st, a);
     RDK_LAUNCH_CHECK("distill_grad_kernel");
     return RDK_OK;
@@ -761,12 +795,11 @@ rdk_status_t launch_distill_loss(const rdk_distill_desc_t &d, const KernelHandle
                                  const float *teacher_lse, const float *weight, float *loss, float *stats, void *dz, int64_t ldd, void *ws,
                                  hipStream_t st)
 {
-    DistillArgs a = arguments(d, h, z, top_ids, top_logits, weight);
+    DistillArgs a = arguments(d, h, z, top_ids, top_logits, weight, dz, ldd);
     a.teacher_lse = teacher_lse;
     a.loss = loss;
     a.part = (SoftStat *)ws;
     a.stats = stats ? (float4 *)stats : (float4 *)((char *)ws + align_up((size_t)d.B * a.parts * sizeof(SoftStat), 256));
-    a.dz = dz; a.ldd = ldd;
     rdk_status_t rc = RDK_OK;
     with_logits(z.kind, [&](auto k) {
         constexpr int KIND = decltype(k)::value;
@@ -778,9 +811,8 @@ rdk_status_t launch_distill_loss(const rdk_distill_desc_t &d, const KernelHandle
 rdk_status_t launch_distill_grad(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
                                  const float *stats, const float *weight, void *dz, int64_t ldd, hipStream_t st)
 {
-    DistillArgs a = arguments(d, h, z, top_ids, top_logits, weight);
+    DistillArgs a = arguments(d, h, z, top_ids, top_logits, weight, dz, ldd);
     a.stats = (float4 *)const_cast<float *>(stats);
-    a.dz = dz; a.ldd = ldd;
     rdk_status_t rc = RDK_OK;
     with_logits(z.kind, [&](auto k) { rc = launch_grad<decltype(k)::value>(a, d.B, st); });
     return rc;
