@@ -432,11 +432,33 @@ T *plain_or_none(PyObject *o, at::ScalarType type, int64_t count, const char *wh
     return o == Py_None ? nullptr : plain<T>(o, type, count, what);
 }
 
+// What a call writes, held for the call.
 template <class T>
-T *plain_attr(PyObject *obj, PyObject *name, at::ScalarType type, int64_t count, const char *what)
+struct Output {
+    at::Tensor t;
+    T *p;
+};
+
+template <class T>
+Output<T> output(PyObject *obj, PyObject *name, at::ScalarType type, int64_t count, const char *what)
 {
     Ref a(PyObject_GetAttr(obj, name));
-    return plain<T>(a.o, type, count, what);
+    T *p = plain<T>(a.o, type, count, what);
+    return {THPVariable_Unpack(a.o), p};
+}
+
+// Outputs count as written for torch: a backward pass that saved one of them before raises torch's error for tensors modified in place.  (Tensors made
+// for inference have no version.)
+void count_written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+PyObject *status(rdk_status_t rc, std::initializer_list<const at::Tensor *> written)
+{
+    if (rc == RDK_OK)
+        for (const at::Tensor *t : written) count_written(*t);
+    return status(rc);
 }
 
 int32_t extent(const at::Tensor &t, int64_t dim, const char *what)
@@ -461,11 +483,12 @@ PyObject *topk(PyObject *const *a)
     if (rc != RDK_OK) return status(rc);
     const int64_t count = (int64_t)d.B * d.k;
     const char *what = "the outputs were made for another batch shape";
-    int32_t *ids = plain_attr<int32_t>(o, g.ids, at::kInt, count, what);
-    float *values = plain_attr<float>(o, g.values, at::kFloat, count, what), *lse = plain_attr<float>(o, g.lse, at::kFloat, d.B, what);
+    const Output<int32_t> ids = output<int32_t>(o, g.ids, at::kInt, count, what);
+    const Output<float> values = output<float>(o, g.values, at::kFloat, count, what), lse = output<float>(o, g.lse, at::kFloat, d.B, what);
     const Scratch w = workspace(o, g.out_ws, bytes, x);
     void *st = stream();
-    return status(unlocked([&] { return rdk_topk(&d, xi.p, xi.kind, xi.ld, ids, values, lse, w.p, w.bytes, st); }));
+    return status(unlocked([&] { return rdk_topk(&d, xi.p, xi.kind, xi.ld, ids.p, values.p, lse.p, w.p, w.bytes, st); }),
+                  {&ids.t, &values.t, &lse.t});
 }
 
 // kernel or None, z, top_ids, top_logits, teacher_lse or None, temperature, weight or None, outputs, part (0: loss, 1: loss and gradient, 2: gradient)
@@ -489,27 +512,30 @@ PyObject *distill(PyObject *const *a)
     const float *lse = plain_or_none<float>(a[4], at::kFloat, d.B, "teacher_lse: float32 [B] on the device");
     const float *weight = plain_or_none<float>(a[6], at::kFloat, d.B, "weight: float32 [B] on the device");
     const char *what = "the outputs were made for another batch shape";
-    float *loss = plain_attr<float>(o, g.loss, at::kFloat, d.B, what), *stats = plain_attr<float>(o, g.stats, at::kFloat, 4 * (int64_t)d.B, what);
+    const Output<float> loss = output<float>(o, g.loss, at::kFloat, d.B, what), stats = output<float>(o, g.stats, at::kFloat, 4 * (int64_t)d.B, what);
+    at::Tensor grad;
     void *zp = ptr(z), *st = stream(), *dz = nullptr;
     int64_t ldd = 0;
     if (part) {
         Ref r(PyObject_GetAttr(o, g.grad));
-        const at::Tensor &t = tensor(r.o, "the outputs hold no gradient");
-        need(t.scalar_type() == z.scalar_type() && t.dim() == 2 && t.size(0) == d.B && t.size(1) == d.n, "the gradient has z's shape and type");
-        ldd = rows(t);
-        dz = ptr(t);
+        grad = tensor(r.o, "the outputs hold no gradient");
+        need(grad.scalar_type() == z.scalar_type() && grad.dim() == 2 && grad.size(0) == d.B && grad.size(1) == d.n,
+             "the gradient has z's shape and type");
+        ldd = rows(grad);
+        dz = ptr(grad);
     }
     if (part == 2)
-        return status(unlocked([&] { return rdk_distill_grad(&d, k, zp, kind, ldz, ids, logits, stats, weight, dz, ldd, st); }));
+        return status(unlocked([&] { return rdk_distill_grad(&d, k, zp, kind, ldz, ids, logits, stats.p, weight, dz, ldd, st); }), {&grad});
     size_t bytes = 0;
     const rdk_status_t rc = rdk_distill_workspace_bytes(&d, kind, &bytes);
     if (rc != RDK_OK) return status(rc);
     const Scratch w = workspace(o, g.out_ws, bytes, z);
     if (part == 1)
         return status(unlocked([&] {
-            return rdk_distill_loss_grad(&d, k, zp, kind, ldz, ids, logits, lse, weight, loss, stats, dz, ldd, w.p, w.bytes, st);
-        }));
-    return status(unlocked([&] { return rdk_distill_loss(&d, k, zp, kind, ldz, ids, logits, lse, weight, loss, stats, w.p, w.bytes, st); }));
+            return rdk_distill_loss_grad(&d, k, zp, kind, ldz, ids, logits, lse, weight, loss.p, stats.p, dz, ldd, w.p, w.bytes, st);
+        }), {&loss.t, &stats.t, &grad});
+    return status(unlocked([&] { return rdk_distill_loss(&d, k, zp, kind, ldz, ids, logits, lse, weight, loss.p, stats.p, w.p, w.bytes, st); }),
+                  {&loss.t, &stats.t});
 }
 
 // x, scores, K, x_kind, finished or None, eos, outputs
@@ -532,12 +558,13 @@ PyObject *beam_select(PyObject *const *a)
     const rdk_status_t rc = rdk_beam_select_workspace_bytes(&d, xi.kind, &bytes);
     if (rc != RDK_OK) return status(rc);
     const char *what = "the outputs were made for another batch shape";
-    float *so = plain_attr<float>(o, g.scores, at::kFloat, out, what);
-    int32_t *parent = plain_attr<int32_t>(o, g.parent, at::kInt, out, what), *token = plain_attr<int32_t>(o, g.token, at::kInt, out, what);
-    uint8_t *fo = plain_attr<uint8_t>(o, g.finished, at::kByte, out, what);
+    const Output<float> so = output<float>(o, g.scores, at::kFloat, out, what);
+    const Output<int32_t> parent = output<int32_t>(o, g.parent, at::kInt, out, what), token = output<int32_t>(o, g.token, at::kInt, out, what);
+    const Output<uint8_t> fo = output<uint8_t>(o, g.finished, at::kByte, out, what);
     const Scratch w = workspace(o, g.out_ws, bytes, x);
     void *st = stream();
-    return status(unlocked([&] { return rdk_beam_select(&d, xi.p, xi.kind, xi.ld, si, fi, so, parent, token, fo, w.p, w.bytes, st); }));
+    return status(unlocked([&] { return rdk_beam_select(&d, xi.p, xi.kind, xi.ld, si, fi, so.p, parent.p, token.p, fo.p, w.p, w.bytes, st); }),
+                  {&so.t, &parent.t, &token.t, &fo.t});
 }
 
 // One state of beams for rdk_beam_reorder: its rows as pieces with at most one gap between them, in the order in which they lie in memory.
@@ -605,7 +632,9 @@ PyObject *beam_reorder(PyObject *const *a)
         states.push_back(state_of(src, dst));
     }
     void *st = stream();
-    return status(unlocked([&] { return rdk_beam_reorder(G, W, K, pi, states.data(), (int32_t)count, st); }));
+    const rdk_status_t rc = unlocked([&] { return rdk_beam_reorder(G, W, K, pi, states.data(), (int32_t)count, st); });
+    for (Py_ssize_t i = 0; rc == RDK_OK && i < count; ++i) count_written(held[2 * i + 1]);
+    return status(rc);
 }
 
 #define RDK_METHOD(NAME, COUNT) {#NAME, (PyCFunction)(void (*)(void))(&guarded<NAME, COUNT>), METH_FASTCALL, nullptr}

@@ -438,7 +438,8 @@ class _Distill(torch.autograd.Function):
 
 
 def rdk_distill(kernel, z, top_ids, top_logits, teacher_lse=None, temperature=1.0):
-    """rdk_distill_loss under torch's automatic differentiation: the losses [B], whose gradient reaches z."""
+    """rdk_distill_loss under torch's automatic differentiation: the losses [B], whose gradient reaches z.  z, top_ids and top_logits are kept
+    for the backward pass, which raises torch's error where a call has written over them meanwhile (rdk_topk into the same outputs)."""
     return _Distill.apply(z, kernel, top_ids, top_logits, teacher_lse, temperature)
 
 
