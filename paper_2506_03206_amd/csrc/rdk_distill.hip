@@ -237,8 +237,10 @@ __device__ __forceinline__ float outside_of(bool remainder, float r, int held, f
 
 // What the backward call reads of a row: a reference of exponents, 1 / the row's sum, the factor of exp((z - reference) / T) outside A, the constant of t.
 // The reference is the row's, unless the largest logit outside A lies more than kFar powers of two below: then exponentials outside would leave the range that is
-// left below them, the reference is that logit, and 1 / sum, relative to the largest logit at the entries, has its sign turned.
+// left below them, the reference is that logit, and 1 / sum, relative to the largest logit at the entries, has its sign turned.  A row of weight 0, which the
+// forward call does not look at, has a factor that no other row has.
 constexpr float kFar = 24.f;
+__device__ __forceinline__ float4 passed_over() { return make_float4(0.f, 0.f, -INFINITY, 0.f); }
 __device__ __forceinline__ float4 stats_of(const Teacher &o, float inv, float ref, SoftStat rest, float outside, float c)
 {
     const float down = (weight_reference(rest.m) - ref) * c;
@@ -272,7 +274,7 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
     if (w == 0.f) {
         if (threadIdx.x == 0) {
             a.loss[row] = 0.f;
-            a.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+            a.stats[row] = passed_over();
         }
         return;
     }
@@ -368,7 +370,7 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
         }
         if (tid == 0) {
             a.loss[row] = 0.f;
-            if (a.stats) a.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (a.stats) a.stats[row] = passed_over();
         }
         return;
     }
@@ -502,7 +504,7 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
     if (w == 0.f) {
         if (tid == 0) {
             a.loss[row] = 0.f;
-            a.stats[row] = make_float4(0.f, 0.f, 0.f, 0.f);
+            a.stats[row] = passed_over();
         }
         return;
     }
@@ -614,7 +616,8 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(D
     const char *zr = (const char *)row_ptr<KIND>(a.z, a.ldz, row);
     char *dr = (char *)const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row));
     const float w = a.weight ? a.weight[row] : 1.f;
-    if (w == 0.f) {
+    const float4 stats = a.stats[row];
+    if (w == 0.f || stats.z == passed_over().z) {
         const int end = min(a.n, begin + kSlots);
         const u32x4 zero{0, 0, 0, 0};
         for (int i = begin + tid * V::kLen; i < end; i += (kDistillThreads + kWave) * V::kLen) V::store(dr, i, end, zero);
@@ -636,7 +639,6 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(D
     } else {
         load_part(begin);
     }
-    const float4 stats = a.stats[row];
     const bool two = stats.y < 0.f, alone = two && a.in_place && a.grad_parts > 1;
     if (alone && part > 0) return;
     const int end = alone ? a.n : min(a.n, begin + kSlots);
