@@ -192,8 +192,10 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     const void *xr = row_ptr<KIND>(a.x, a.ldx, row);
     const char *from = (const char *)xr + (int64_t)begin * V::kSize;
     const int whole = (end - begin) / V::kLen, behind = (end - begin) % V::kLen;   // whole vectors; a value behind them is one thread's each
-    // wavefronts that have values at all, and how many lanes of each have to reach its bound
-    const int waves = min((max(whole, 1) + kWave - 1) / kWave, kTopWaves), share = (a.k + waves - 1) / waves;
+    // wavefronts that have values, and how many lanes of each have to reach its bound.  The last one is left out where it has fewer lanes with values: it would
+    // find no bound, and every value would be wanted (4 rows of 1600 bf16 logits, 128 kept 79 us, 11 without it).
+    const int most = min((max(whole, 1) + kWave - 1) / kWave, kTopWaves), lanes = whole - (most - 1) * kWave;
+    const int waves = most > 1 && lanes < (a.k + most - 1) / most ? most - 1 : most, share = (a.k + waves - 1) / waves;
     constexpr float none = KIND == RDK_PROB_F32 ? 0.f : -INFINITY;
     float m = none, s = 0.f, ref = 0.f, high = -INFINITY;   // ref: reference of the lane's exponents, times c; high: where it is replaced
     float last = none;
