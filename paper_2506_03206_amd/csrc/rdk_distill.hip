@@ -171,37 +171,44 @@ __device__ __forceinline__ void entry_logits(const void *zr, const Entries &t, f
 struct Teacher {
     double log_t[kPerLane];    // log t of the lane's entries
     float p[kPerLane];         // t, 0 for entries that do not count
-    double constant;           // log t = v / T - constant
+    double shift;              // log t = (v - the largest v that counts) / T - shift: a number of ordinary size wherever the logits lie
     int held;
     bool remainder;            // the mass outside A counts
     double r;                  // the teacher's
 };
+
+// The largest teacher logit that counts.
+__device__ __forceinline__ float largest_logit(const Entries &t)
+{
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kPerLane; ++j)
+        if (t.slot[j] >= 0) m = fmaxf(m, t.v[j]);
+    return weight_reference(wave_max(m));
+}
+
 template <bool REST>
 __device__ __forceinline__ Teacher teacher_of(const DistillArgs &a, int64_t row, const Entries &t)
 {
     Teacher o;
     o.held = 0;
-    float vmax = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < kPerLane; ++j) {
-        o.held += __popcll(__ballot(t.slot[j] >= 0));
-        if (t.slot[j] >= 0) vmax = fmaxf(vmax, t.v[j]);
-    }
+    for (int j = 0; j < kPerLane; ++j) o.held += __popcll(__ballot(t.slot[j] >= 0));
+    const float vmax = largest_logit(t);
     o.remainder = REST && o.held < a.n;
     if (o.remainder) {
-        o.constant = a.teacher_lse[row];
+        o.shift = a.teacher_lse[row] - (double)vmax * a.inv_t;
     } else {
-        vmax = weight_reference(wave_max(vmax));
         double sum = 0.;
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
             if (t.slot[j] >= 0) sum += expf((t.v[j] - vmax) * a.inv_t);
-        o.constant = (double)vmax * a.inv_t + log(wave_sum(sum));
+        o.shift = log(wave_sum(sum));
     }
     double mass = 0.;
 #pragma unroll
     for (int j = 0; j < kPerLane; ++j) {
-        o.log_t[j] = (double)t.v[j] * a.inv_t - o.constant;
+        o.log_t[j] = ((double)t.v[j] - vmax) * a.inv_t - o.shift;
         o.p[j] = t.slot[j] >= 0 ? expf((float)o.log_t[j]) : 0.f;
         mass += o.p[j];
     }
@@ -235,7 +242,7 @@ __device__ __forceinline__ float outside_of(bool remainder, float r, int held, f
     return rest.s == 0.f ? 0.f : soft_term(weight_reference(rest.m), ref, c) * inv - r / rest.s;
 }
 
-// What the backward call reads of a row: a reference of exponents, 1 / the row's sum, the factor of exp((z - reference) / T) outside A, the constant of t.
+// What the backward call reads of a row: a reference of exponents, 1 / the row's sum, the factor of exp((z - reference) / T) outside A, the teacher's shift.
 // The reference is the row's, unless the largest logit outside A lies more than kFar powers of two below: then exponentials outside would leave the range that is
 // left below them, the reference is that logit, and 1 / sum, relative to the largest logit at the entries, has its sign turned.  A row of weight 0, which the
 // forward call does not look at, has a factor that no other row has.
@@ -244,9 +251,9 @@ __device__ __forceinline__ float4 passed_over() { return make_float4(0.f, 0.f, -
 __device__ __forceinline__ float4 stats_of(const Teacher &o, float inv, float ref, SoftStat rest, float outside, float c)
 {
     const float down = (weight_reference(rest.m) - ref) * c;
-    if (!o.remainder || rest.s == 0.f) return make_float4(ref, inv, outside, (float)o.constant);
-    if (down < -kFar) return make_float4(rest.m, -inv, outside, (float)o.constant);
-    return make_float4(ref, inv, inv - (float)o.r / (rest.s * __builtin_amdgcn_exp2f(down)), (float)o.constant);
+    if (!o.remainder || rest.s == 0.f) return make_float4(ref, inv, outside, (float)o.shift);
+    if (down < -kFar) return make_float4(rest.m, -inv, outside, (float)o.shift);
+    return make_float4(ref, inv, inv - (float)o.r / (rest.s * __builtin_amdgcn_exp2f(down)), (float)o.shift);
 }
 
 // The row's loss, by one wavefront: total is the sum of the whole row relative to ref, rest that of its slots outside A relative to its own largest logit.
@@ -297,7 +304,7 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
 
 // A row's entries between the steps of the wavefront that follows them.
 struct EntryShared {
-    double log_t[kMaxEntries], constant, r;
+    double log_t[kMaxEntries], shift, r;
     int slot[kMaxEntries], held, remainder;
     float zt[kMaxEntries], p[kMaxEntries];
 
@@ -309,7 +316,7 @@ struct EntryShared {
             log_t[k] = o.log_t[j]; zt[k] = z[j]; p[k] = o.p[j];
         }
         if (lane_id() == 0) {
-            constant = o.constant; r = o.r; held = o.held; remainder = o.remainder;
+            shift = o.shift; r = o.r; held = o.held; remainder = o.remainder;
         }
     }
     __device__ __forceinline__ void get(Entries &t, float (&z)[kPerLane], Teacher &o) const
@@ -319,7 +326,7 @@ struct EntryShared {
             const int k = lane_id() + j * kWave;
             o.log_t[j] = log_t[k]; t.slot[j] = slot[k]; z[j] = zt[k]; o.p[j] = p[k];
         }
-        o.constant = constant; o.r = r; o.held = held; o.remainder = remainder;
+        o.shift = shift; o.r = r; o.held = held; o.remainder = remainder;
     }
 };
 
@@ -665,12 +672,12 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(D
     }
     __syncthreads();
     if (follows) {
-        const float ref = two ? weight_reference(wave_max(fmaxf(zt[0], zt[1]))) : stats.x, inv = fabsf(stats.y);
+        const float vmax = largest_logit(t), ref = two ? weight_reference(wave_max(fmaxf(zt[0], zt[1]))) : stats.x, inv = fabsf(stats.y);
         static_assert(kPerLane == 2, "the largest logit at the entries is formed of two to a lane");
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
             if (t.slot[j] >= begin && t.slot[j] < end)
-                V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - expf(t.v[j] * a.inv_t - stats.w)));
+                V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - expf((t.v[j] - vmax) * a.inv_t - stats.w)));
     }
 }
 
