@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_part_kernel(D
 {
     typedef Vec<KIND> V;
     constexpr int kWaves = kDistillThreads / kWave, kSlots = kDistillThreads * kPartVecs * V::kLen;
-    __shared__ uint8_t marked[REST ? kDistillThreads * kPartVecs : 16];
+    __shared__ __attribute__((aligned(16))) uint8_t marked[REST ? kDistillThreads * kPartVecs : 16];
     __shared__ SoftStat sh[kWaves];
     const int64_t row = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts, begin = part * kSlots, here = min(a.n - begin, kSlots), tid = threadIdx.x;
