@@ -3,9 +3,9 @@
 // With s = softmax(z / T) and the teacher's probabilities t on the slots A of its entries:  loss = sum_A t (log t - log s), and where the teacher's
 // remainder r is counted too, + r (log r - log rho) with rho = sum of s outside A.  Gradient:  (s - t) / T on A,  s (1 - r / rho) / T outside.
 // rho is summed over the slots outside A by themselves (a bitmap of A in LDS): as 1 - sum_A s it would be lost to rounding for a drafter
-// that is sure of its top entries.  The sum is relative to the largest logit outside A and never brought to the row's: a drafter surer still has a rho that
-// fp32 does not hold beside 1, where log rho and the softmax over the slots outside alone are ordinary numbers.  With e_j = exp((z_j - that logit) / T)
-// the gradient outside is (rho / sum e - r / sum e) e_j / T, whose first term may vanish.
+// that is sure of its top entries.  Of a drafter surer still (88 T between its best logit and all outside) it is nothing that fp32 holds beside the row's sum: the
+// sum outside is then relative to the largest logit outside, log rho is formed of the two references in 64 bits, and the gradient outside is s - r times the softmax
+// over these slots alone.
 #include "rdk_vec.hpp"
 
 namespace rdk {
@@ -235,41 +235,69 @@ __device__ __forceinline__ SoftStat entry_stat(const Entries &t, const float (&z
     return st;
 }
 
-// Factor of exp((z - rest.m) / T) outside A in the gradient, with inv = 1 / the row's sum, relative to ref.  (Without the remainder rest is the row's.)
-__device__ __forceinline__ float outside_of(bool remainder, float r, int held, float inv, float ref, SoftStat rest, float c)
+// A row's sums brought together.
+struct RowSums {
+    float ref, total, inv;   // the row's largest logit, its sum relative to that, and the reciprocal
+    float out_ref, rest;     // the sum of the slots outside A (without the remainder: of the row) and what it is relative to
+    float down;              // exp((out_ref - ref) / T)
+    bool far;                // out_ref is not ref
+};
+
+// Outside A exponentials are relative to the row's largest logit, of which rho is a quotient with the row's sum (of a drafter near its teacher the errors of
+// the two cancel in the loss), unless all outside lies more than kFar powers of two below: what is left of the range below that would not hold
+// them.  Then they are relative to the largest logit outside.
+constexpr float kFar = 24.f;
+__device__ __forceinline__ RowSums sums_of(const SoftStat *outside, int parts, SoftStat entries, float c)
 {
-    if (!remainder) return held ? inv : 0.f;
-    return rest.s == 0.f ? 0.f : soft_term(weight_reference(rest.m), ref, c) * inv - r / rest.s;
+    RowSums u;
+    float top = -INFINITY;
+    for (int k = 0; k < parts; ++k) top = fmaxf(top, outside[k].m);
+    u.ref = weight_reference(fmaxf(top, entries.m));
+    u.far = top > -INFINITY && (top - u.ref) * c < -kFar;
+    u.out_ref = u.far ? top : u.ref;
+    u.down = u.far ? soft_term(top, u.ref, c) : 1.f;
+    u.rest = 0.f;
+    for (int k = 0; k < parts; ++k)
+        u.rest += outside[k].s == 0.f ? 0.f : outside[k].s * soft_term(weight_reference(outside[k].m), u.out_ref, c);
+    u.total = u.rest * u.down + (entries.s == 0.f ? 0.f : entries.s * soft_term(weight_reference(entries.m), u.ref, c));
+    u.inv = u.total == 0.f ? 0.f : 1.f / u.total;
+    return u;
+}
+
+// Factor of exp((z - out_ref) / T) outside A in the gradient.
+__device__ __forceinline__ float outside_of(bool remainder, float r, int held, const RowSums &u)
+{
+    if (!remainder) return held ? u.inv : 0.f;
+    if (u.rest == 0.f) return 0.f;
+    return u.far ? u.down * u.inv - r / u.rest : u.inv * (1.f - r * u.total / u.rest);
 }
 
 // What the backward call reads of a row: a reference of exponents, 1 / the row's sum, the factor of exp((z - reference) / T) outside A, the teacher's shift.
-// The reference is the row's, unless the largest logit outside A lies more than kFar powers of two below: then exponentials outside would leave the range that is
-// left below them, the reference is that logit, and 1 / sum, relative to the largest logit at the entries, has its sign turned.  A row of weight 0, which the
-// forward call does not look at, has a factor that no other row has.
-constexpr float kFar = 24.f;
+// Where the reference is not the row's largest logit, 1 / sum is relative to the largest logit at the entries and has its sign turned.  A row of weight 0,
+// which the forward call does not look at, has a factor that no other row has.
 __device__ __forceinline__ float4 passed_over() { return make_float4(0.f, 0.f, -INFINITY, 0.f); }
-__device__ __forceinline__ float4 stats_of(const Teacher &o, float inv, float ref, SoftStat rest, float outside, float c)
+__device__ __forceinline__ float4 stats_of(const Teacher &o, const RowSums &u)
 {
-    const float down = (weight_reference(rest.m) - ref) * c;
-    if (!o.remainder || rest.s == 0.f) return make_float4(ref, inv, outside, (float)o.shift);
-    if (down < -kFar) return make_float4(rest.m, -inv, outside, (float)o.shift);
-    return make_float4(ref, inv, inv - (float)o.r / (rest.s * __builtin_amdgcn_exp2f(down)), (float)o.shift);
+    return make_float4(u.out_ref, u.far ? -u.inv : u.inv, outside_of(o.remainder, (float)o.r, o.held, u), (float)o.shift);
 }
 
-// The row's loss, by one wavefront: total is the sum of the whole row relative to ref, rest that of its slots outside A relative to its own largest logit.
-__device__ __forceinline__ double loss_of(const DistillArgs &a, const Entries &t, const float (&zt)[kPerLane], const Teacher &o, float ref, float total,
-                                          SoftStat rest)
+// The row's loss, by one wavefront.
+__device__ __forceinline__ double loss_of(const DistillArgs &a, const Entries &t, const float (&zt)[kPerLane], const Teacher &o, const RowSums &u)
 {
-    const double log_total = log((double)total);
+    const double log_total = log((double)u.total);
     double loss = 0.;
 #pragma unroll
     for (int j = 0; j < kPerLane; ++j)
         if (o.p[j] != 0.f) {
-            const double log_s = total == 0.f ? -INFINITY : ((double)zt[j] - ref) * a.inv_t - log_total;
+            const double log_s = u.total == 0.f ? -INFINITY : ((double)zt[j] - u.ref) * a.inv_t - log_total;
             loss += o.p[j] * (o.log_t[j] - log_s);
         }
     loss = wave_sum(loss);
-    if (o.remainder && o.r != 0.) loss += rest.s == 0.f ? INFINITY : o.r * (log(o.r * total / rest.s) - ((double)rest.m - ref) * a.inv_t);
+    if (o.remainder && o.r != 0.) {
+        double log_ratio = log(o.r * u.total / u.rest);
+        if (u.far) log_ratio -= ((double)u.out_ref - u.ref) * a.inv_t;
+        loss += u.rest == 0.f ? INFINITY : o.r * log_ratio;
+    }
     return loss;
 }
 
@@ -293,12 +321,11 @@ __global__ __launch_bounds__(kWave) void distill_finish_kernel(DistillArgs a)
     SoftStat st{-INFINITY, 0.f};
     for (int p = lane_id(); p < a.parts; p += kWave) st = merge_at(st, a.part[row * a.parts + p], c);
     st = wave_merge_at(st, c);
-    const SoftStat at = REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f}, all = merge_at(st, at, c);
-    const float ref = weight_reference(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
-    const double loss = loss_of(a, t, zt, o, ref, all.s, st);
+    const RowSums u = sums_of(&st, 1, REST ? entry_stat(t, zt, c) : SoftStat{-INFINITY, 0.f}, c);
+    const double loss = loss_of(a, t, zt, o, u);
     if (threadIdx.x == 0) {
         a.loss[row] = (float)(w * loss);
-        a.stats[row] = stats_of(o, inv, ref, st, outside_of(o.remainder, (float)o.r, o.held, inv, ref, st, c), c);
+        a.stats[row] = stats_of(o, u);
     }
 }
 
@@ -448,16 +475,11 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
         if (lane_id() == 0) waves[tid / kWave] = st;
     }
     __syncthreads();   // (the logits at the entries have been read too: dz may be z)
-    SoftStat rest{-INFINITY, 0.f};
-    for (int k = 0; k < kWaves; ++k) rest.m = fmaxf(rest.m, waves[k].m);
-    const float rest_ref = weight_reference(rest.m);
-    for (int k = 0; k < kWaves; ++k) rest.s += waves[k].s == 0.f ? 0.f : waves[k].s * soft_term(weight_reference(waves[k].m), rest_ref, c);
-    const SoftStat all = REST ? merge_at(rest, entries, c) : rest;
-    const float ref = weight_reference(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
-    const float outside = outside_of(REST && kept.remainder, (float)kept.r, kept.held, inv, ref, rest, c), wt = w * a.inv_t;
+    const RowSums u = sums_of(waves, kWaves, REST ? entries : SoftStat{-INFINITY, 0.f}, c);
+    const float wt = w * a.inv_t;
     if (GRAD) {
-        const float scale = wt * outside;
-        const float own_scale = own_s == 0.f ? 0.f : scale * soft_term(own_ref, rest_ref, c);
+        const float scale = wt * outside_of(REST && kept.remainder, (float)kept.r, kept.held, u);
+        const float own_scale = own_s == 0.f ? 0.f : scale * soft_term(own_ref, u.out_ref, c);
         if (!follows) {
 #pragma unroll
             for (int j = 0; j < VECS; ++j)
@@ -467,7 +489,7 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
                         V::to(raw[j], v);
                     }
 #pragma unroll
-                    for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], rest_ref, c);
+                    for (int k = 0; k < V::kLen; ++k) v[k] = KEEP ? own_scale * e[j][k] : scale * soft_term(v[k], u.out_ref, c);
                     V::store_at((char *)dr + j * THREADS * 16, tid * 16, V::kLen, V::from(v));
                 }
             if (tid < behind) V::store1(dr, whole * V::kLen + tid, own_scale * e_last);
@@ -478,10 +500,10 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
     Teacher o;
     if (follows) {
         kept.get(t, zt, o);
-        const double loss = loss_of(a, t, zt, o, ref, all.s, rest);
+        const double loss = loss_of(a, t, zt, o, u);
         if (lane_id() == 0) {
             a.loss[row] = (float)(w * loss);
-            if (a.stats) a.stats[row] = stats_of(o, inv, ref, rest, outside, c);
+            if (a.stats) a.stats[row] = stats_of(o, u);
         }
     }
     if (!GRAD) return;
@@ -489,7 +511,7 @@ __global__ __launch_bounds__(THREADS + kWave) void distill_row_kernel(DistillArg
     if (follows) {
 #pragma unroll
         for (int j = 0; j < kPerLane; ++j)
-            if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], ref, c) * inv - o.p[j]));
+            if (t.slot[j] >= 0) V::store1(dr, t.slot[j], wt * (soft_term(zt[j], u.ref, c) * u.inv - o.p[j]));
     }
 }
 
@@ -595,16 +617,15 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
     if (!follows) return;
     SoftStat st = lane_id() < kWaves ? waves[lane_id()] : SoftStat{-INFINITY, 0.f};
     st = wave_merge_at(st, c);
-    const SoftStat all = merge_at(st, REST ? entries : SoftStat{-INFINITY, 0.f}, c);
-    const float ref = weight_reference(all.m), inv = all.s == 0.f ? 0.f : 1.f / all.s;
+    const RowSums u = sums_of(&st, 1, REST ? entries : SoftStat{-INFINITY, 0.f}, c);
     Entries t;
     float zt[kPerLane];
     Teacher o;
     kept.get(t, zt, o);
-    const double loss = loss_of(a, t, zt, o, ref, all.s, st);
+    const double loss = loss_of(a, t, zt, o, u);
     if (lane_id() == 0) {
         a.loss[row] = (float)(w * loss);
-        a.stats[row] = stats_of(o, inv, ref, st, outside_of(o.remainder, (float)o.r, o.held, inv, ref, st, c), c);
+        a.stats[row] = stats_of(o, u);
     }
 }
 
