@@ -630,7 +630,8 @@ __global__ __launch_bounds__(kLoopThreads + kWave) void distill_loop_kernel(Dist
 }
 
 // dz of a part of a row, whose logits lie in the registers; the entries as in distill_row_kernel.  Bound by HBM: 1024 bf16 rows of
-// 16384 (an eighth of weight 0) 8 us = 7.8 TB/s read and written, z out of the last-level cache, which holds it from the forward call.
+// 16384 (an eighth of weight 0) 8 to 9 us = 7 to 7.8 TB/s read and written.  The L2s fetch z anew (33 MB counted at their far side); the rate, above
+// the 6.0 to 6.4 of a copy, says that the last-level cache behind them still has it from the forward call.
 // A row of two references (stats_of) needs the logits of all its entries: over z itself they stand only until another workgroup writes its part, so
 // the first one goes over the whole of such a row.
 template <int KIND>
@@ -802,7 +803,8 @@ rdk_status_t launch_loss(const DistillArgs &a, int32_t B, hipStream_t st)
     // With the gradient only rows that no workgroup holds, which are then read again.
     if (a.n > (a.dz ? kRowSlots<KIND> : 448 * 9 * kLen)) return launch_loop<KIND, REST>(a, B, st);
     // As many threads and vectors to a thread as the row takes: two workgroups of eight wavefronts on a compute unit for the rows in between (2048 bf16
-    // rows of 32064: 448 threads of nine vectors 47.5 us, 512 of eight 62, one workgroup of 960 60), one for the longest.
+    // rows of 32064: 448 threads of nine vectors 47.5 us, 512 of eight 62, one workgroup of 960 60), one for the longest.  Beyond nine vectors the
+    // exponentials are formed twice: 2048 rows of 32064 and of 32768, all of them counted, 52 and 60 us.
     if (a.n <= 192 * 3 * kLen) return launch_row<KIND, 192, 3, REST>(a, B, st);
     if (a.n <= 192 * 9 * kLen) return launch_row<KIND, 192, 9, REST>(a, B, st);
     if (a.n <= 448 * 5 * kLen) return launch_row<KIND, 448, 5, REST>(a, B, st);

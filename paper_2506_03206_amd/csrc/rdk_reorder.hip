@@ -4,7 +4,7 @@
 // change before it writes any of them, so a reorder in place needs no scratch and no order between threads.  Units lie at any address
 // (the memory pipe takes them: five beams with rows of 8 pieces of 65934 bytes move at 4.3 TB/s, in units as small as the sizes' common
 // divisor at 1.4).  Bound by HBM: 5.8 to 6.2 TB/s of the bytes of rows that change and are needed, where a copy kernel reaches 6.0 to 6.4;
-// non-temporal accesses are worth an eighth (16 requests of 4 beams, 0.54 GB of caches: 137 us without, 131 stores alone, 119 both).
+// non-temporal accesses are worth an eighth (16 requests of 4 beams, 0.54 GB of caches: 137 us without, 131 stores alone, 119 to 122 both).
 #include "rdk_vec.hpp"
 
 namespace rdk {
@@ -52,7 +52,7 @@ struct Rows {
     {
         const int p = I < K ? parent[I] : -1;
         const bool moves = (unsigned)p < (unsigned)W && !(in_place && p == I);   // the same for the workgroup
-        T v{};   // (unset, the same code takes 2 to 8 % longer: 0.54 GB of caches 111 to 124 us, set 108 to 119)
+        T v{};   // (unset, four rows take 2 to 3 % longer, in turn on one card: 0.54 GB of caches 128.9 us, set 125.2; eight rows the same)
         if (moves) v = __builtin_nontemporal_load((const T *)(src + p * src_stride));
         Rows<U, I + 1, MOST>::move(src, dst, src_stride, dst_stride, parent, W, K, in_place);
         if (moves) __builtin_nontemporal_store(v, (T *)(dst + I * dst_stride));

@@ -174,9 +174,9 @@ __device__ __forceinline__ void write_row(int32_t *ids, float *values, float *ls
 // (values that rise along the row) the whole part is sifted; where more reaches the last bound than there is room for, by the bound to its last
 // bit; and where that is still more, it is the k-th largest value itself and met by many (what masks leave): those above it are
 // taken, and the first of those that equal it.
-// Only values that crowd in few lanes, and NaN, leave the search by halving.
-// Bound by HBM where rows are many and long: 1024 rows of 151936 fp32 logits, 64 kept, 100 us = 6.2 TB/s, bf16 58 us = 5.4 TB/s (twice the exponentials
-// a byte; without the noting and the end 50 us).  Few rows are a chain: 8 rows of 128256 bf16 logits in 32 parts each
+// Only values that crowd in few lanes, and NaN, are left to the search by halving.
+// Bound by HBM where rows are many and long: 1024 rows of 151936 fp32 logits, 64 kept, 100 us = 6.2 TB/s, weights 101 us, bf16 58 us = 5.4 TB/s (twice
+// the exponentials a byte; without the noting and the end 50 us).  Few rows are a chain: 8 rows of 128256 bf16 logits in 32 parts each
 // take 6.7 us, 2.5 of it until the loads are there and the bound stands, 1.3 for sifting, 0.7 for sorting, 0.5 for statistics and stores.
 template <int KIND>
 __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
