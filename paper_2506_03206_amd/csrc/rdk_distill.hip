@@ -640,16 +640,15 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(D
     typedef Vec<KIND> V;
     constexpr int kSlots = kDistillThreads * kGradVecs * V::kLen;
     const int64_t row = blockIdx.x / a.grad_parts;
-    const int part = blockIdx.x % a.grad_parts, begin = part * kSlots, tid = threadIdx.x;
+    const int part = blockIdx.x % a.grad_parts, begin = part * kSlots, here = min(a.n - begin, kSlots), tid = threadIdx.x;   // (n may be 2^31 - 1)
     const bool follows = tid >= kDistillThreads;
     const char *zr = (const char *)row_ptr<KIND>(a.z, a.ldz, row);
     char *dr = (char *)const_cast<void *>(row_ptr<KIND>(a.dz, a.ldd, row));
     const float w = a.weight ? a.weight[row] : 1.f;
     const float4 stats = a.stats[row];
     if (w == 0.f || stats.z == passed_over().z) {
-        const int end = min(a.n, begin + kSlots);
         const u32x4 zero{0, 0, 0, 0};
-        for (int i = begin + tid * V::kLen; i < end; i += (kDistillThreads + kWave) * V::kLen) V::store(dr, i, end, zero);
+        for (int i = tid * V::kLen; i < here; i += (kDistillThreads + kWave) * V::kLen) V::store(dr + (int64_t)begin * V::kSize, i, here, zero);
         return;
     }
     u32x4 raw[kGradVecs];
@@ -670,7 +669,7 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(D
     }
     const bool two = stats.y < 0.f, alone = two && a.in_place && a.grad_parts > 1;
     if (alone && part > 0) return;
-    const int end = alone ? a.n : min(a.n, begin + kSlots);
+    const int end = alone ? a.n : begin + here;
     const float c = a.inv_t * kLog2e, wt = w * a.inv_t, scale = stats.z * wt;
     if (a.in_place) __syncthreads();   // the logits at the entries have been read before anything is written
     if (!follows) {
@@ -687,8 +686,8 @@ __global__ __launch_bounds__(kDistillThreads + kWave) void distill_grad_kernel(D
                     V::store_at(dr + (int64_t)from * V::kSize + j * kDistillThreads * 16, tid * 16, left, V::from(v));
                 }
             }
+            if (end - from <= kSlots) break;
             from += kSlots;
-            if (from >= end) break;
             load_part(from);
         }
     }
