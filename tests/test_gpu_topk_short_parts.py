@@ -9,23 +9,26 @@ pytestmark = pytest.mark.gpu
 
 
 def part_time(B, N, k, kind):
+    """The least mean of three times twenty launches: one that is held up from outside does not count."""
     from paper_2506_03206_amd import rdk
     x, o = rows(B, N, kind, N), rdk.TopkOutputs(B, N, k, "cuda")
+    means = []
     for _ in range(3):
         rdk.rdk_topk(x, k, outputs=o)
-    torch.cuda.synchronize()
-    rdk.rdk_timing_read("topk_part_kernel")
-    rdk.rdk_timing_select("topk_part_kernel")
-    try:
-        for _ in range(20):
-            rdk.rdk_topk(x, k, outputs=o)
         torch.cuda.synchronize()
-    finally:
-        rdk.rdk_timing_select(None)
-    launches, ms = rdk.rdk_timing_read("topk_part_kernel")
-    assert launches == 20
+        rdk.rdk_timing_read("topk_part_kernel")
+        rdk.rdk_timing_select("topk_part_kernel")
+        try:
+            for _ in range(20):
+                rdk.rdk_topk(x, k, outputs=o)
+            torch.cuda.synchronize()
+        finally:
+            rdk.rdk_timing_select(None)
+        launches, ms = rdk.rdk_timing_read("topk_part_kernel")
+        assert launches == 20
+        means.append(ms / launches)
     verify(o, x, k, kind)
-    return ms / launches
+    return min(means)
 
 
 @pytest.mark.parametrize("kind,B,N,k,full", [
