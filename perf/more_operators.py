@@ -2,8 +2,8 @@
 
   score   log probabilities of given tokens of every row, their ranks, the row's entropy and its top alternatives: scoring a text, the
           log probabilities that a server returns, candidates held against redistributed rows
-  train   the same forward and then backward (two calls: what comes from above arrives in between): a drafter or a target trained on tokens,
-          with a gradient of the entropy where a policy is kept from collapsing
+  train   a drafter or a target trained on tokens, with a gradient of the entropy where a policy is kept from collapsing: forward and then
+          backward (two calls: what comes from above arrives in between), or both at once (weights known beforehand)
   embed   rows of an embedding table for a batch of tokens
   embed_grad  the table's gradient: rows of equal tokens summed
 
@@ -24,8 +24,8 @@ def _score(name, B, N, C, k=0, kind="bf16", temperature=1.0, masked=0.0, sigma=3
     return dict(c, name=name) if name else c
 
 
-def _train(name, B, N, n, C, kind="bf16", temperature=1.0, entropy=False, live=1.0, sigma=3.0):
-    c = {"op": "train", "B": B, "N": N, "n": n, "C": C, "k": 0, "kind": kind, "temperature": temperature, "masked": 0.0, "sigma": sigma,
+def _train(name, path, B, N, n, C, kind="bf16", temperature=1.0, entropy=False, live=1.0, sigma=3.0):
+    c = {"op": "train", "path": path, "B": B, "N": N, "n": n, "C": C, "k": 0, "kind": kind, "temperature": temperature, "masked": 0.0, "sigma": sigma,
          "entropy": entropy, "live": live}
     return dict(c, name=name) if name else c
 
@@ -52,17 +52,17 @@ def listed():
         # eight candidates a position held against redistributed rows (weights)
         _score("score_weights", 256, 32000, 8, kind="prob"),
         # the smallest training step: 4 sequences of 4 tokens over a toy vocabulary
-        _train("train_tiny", 16, 1024, 256, 1, kind="f32", sigma=2.0),
-        # a training batch of the pruned headline vocabulary: 2048 tokens, an eighth of them padding, with the entropy's gradient
-        _train("train_llama3", 2048, 128256, 32064, 1, entropy=True, live=0.875),
+        _train("train_step_tiny", "step", 16, 1024, 256, 1, kind="f32", sigma=2.0),
+        # forward and backward apart, as a framework's automatic differentiation calls them, with the entropy's gradient
+        _train("train_both_qwen", "both", 1024, 151936, 16384, 1, entropy=True, live=0.875),
+        # a training batch of the pruned headline vocabulary: 2048 tokens, an eighth of them padding, loss and gradient at once
+        _train("train_step_llama3", "step", 2048, 128256, 32064, 1, live=0.875),
         # one decoding step of eight beams: latency
         _embed("embed_decode", 8, 128256, 128256, 4096),
         # a prompt
         _embed("embed_prompt", 8192, 128256, 128256, 4096, scale=64.0),
-        # the smallest training step of a table
-        _embed_grad("embed_grad_tiny", 16, 1024, 1024, 64, "f32", "f32"),
-        # a pruned table of an odd width in 32 bits
-        _embed_grad("embed_grad_odd", 3001, 32003, 7999, 515, "f32", "f32", scale=0.5),
+        # a few sequences and a pruned table of an odd width in 32 bits
+        _embed_grad("embed_grad_odd", 301, 32003, 7999, 515, "f32", "f32", scale=0.5),
         # a training batch of 16384 tokens
         _embed_grad("embed_grad_batch", 16384, 128256, 128256, 2048),
     ]
@@ -86,7 +86,7 @@ def draw(rng):
         elif op == "train":
             kind = rng.choice(["bf16", "f32"])
             if B * n * (2 if kind == "bf16" else 4) <= 2048 * 32064 * 2:
-                return _train(None, B, N, n, rng.choice([1, 1, rng.randint(2, 16)]), kind, rng.choice([1.0, 1.0, 2.0]), rng.choice([False, True]),
+                return _train(None, rng.choice(["both", "step"]), B, N, n, rng.choice([1, 1, rng.randint(2, 16)]), kind, rng.choice([1.0, 1.0, 2.0]), rng.choice([False, True]),
                               rng.choice([1.0, 0.875]), sigma)
         else:
             d, table, rows = _log_int(rng, 16, 8192), rng.choice(["bf16", "f32"]), rng.choice(["bf16", "f32"])
@@ -151,8 +151,7 @@ def prepare(case, seed):
         st["rdk"], B, n = rdk, case["B"], case["n"]
         st["kernel"] = None if st["kept"] is None else rdk.rdk_build_kernel(case["N"], st["kept"], rdk.IDENTITY)   # the pruned vocabulary
         if case["op"] in ("score", "train"):
-            st["o"] = rdk.LogprobsOutputs(B, case["C"], case["k"], "cuda")
-            st["grad"] = torch.empty_like(st["x"]) if case["op"] == "train" else None
+            st["o"] = rdk.LogprobsOutputs(B, case["C"], case["k"], "cuda", grad=torch.empty_like(st["x"]) if case["op"] == "train" else None)
         elif case["op"] == "embed":
             st["out"] = torch.empty((B, case["d"]), dtype=_dtype(case["rows"]), device="cuda")
         else:
@@ -178,9 +177,13 @@ def _own_score(st, case):
 
 def _own_train(st, case):
     rdk, x, tokens = st["rdk"], st["x"], st["tokens"]
-    o = rdk.rdk_logprobs(x, tokens, kernel=st["kernel"], temperature=case["temperature"], ranks=False, outputs=st["o"])
-    rdk.rdk_logprobs_grad(x, tokens, o, st["above"], st["above_entropy"], kernel=st["kernel"], temperature=case["temperature"], grad=st["grad"])
-    return {"logprob": o.logprob, "entropy": o.entropy, "grad": st["grad"]}
+    args, above = {"kernel": st["kernel"], "temperature": case["temperature"]}, (st["above"], st["above_entropy"])
+    if case["path"] == "step":
+        o = rdk.rdk_logprobs_step(x, tokens, *above, outputs=st["o"], **args)
+    else:
+        o = rdk.rdk_logprobs(x, tokens, ranks=False, outputs=st["o"], **args)
+        rdk.rdk_logprobs_grad(x, tokens, o, *above, **args)
+    return {"logprob": o.logprob, "entropy": o.entropy, "grad": o.grad}
 
 
 def _own_embed(st, case):
@@ -272,7 +275,8 @@ def work(case):
         return {"bytes": B * (n * _size(case["kind"]) + 12 * case["C"] + 4 + 8 * case["k"]), "flops": (5.0 + case["C"]) * B * n}
     if case["op"] == "train":
         read_again = 1.0 - (1.0 - case["live"]) ** case["C"]            # rows of padding alone have no gradient that depends on them
-        return {"bytes": B * ((2 + read_again) * n * _size(case["kind"]) + 12 * case["C"] + 8), "flops": (12.0 if case["entropy"] else 9.0) * B * n}
+        reads = read_again + 1.0 if case["path"] == "both" else 1.0
+        return {"bytes": B * ((reads + 1.0) * n * _size(case["kind"]) + 12 * case["C"] + 8), "flops": (12.0 if case["entropy"] else 9.0) * B * n}
     d = case["d"]
     if case["op"] == "embed":
         p = 1.0 / np.arange(1, n + 1)
