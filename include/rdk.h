@@ -421,6 +421,71 @@ typedef struct {
 } rdk_state_t;
 rdk_status_t rdk_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *parent, const rdk_state_t *states, int32_t count, void *stream);
 
+/*
+ * Log probabilities of given tokens, with the row's entropy and its top alternatives, and the gradient of these: scoring a text, what a server returns
+ * beside its tokens, candidates held against redistributed rows, training on tokens.  Per row b of x [B, ldx] (logits, or weights such as redistributed
+ * rows) with y_j = x_j / temperature (weights: log x_j, temperature 1) and s = softmax(y):
+ *   logprob[b, c] = log s at tokens[b, c];  0 for a negative token (padding: nothing was asked); -inf for one that the row masks (a logit of -inf, a weight
+ *                   of 0) or does not hold (an id from N on; with `kernel` a pruned id).
+ *   rank[b, c]    = how many entries come before it in the order of rdk_topk (larger, or equal at a lower place); -1 beside a log probability of -inf
+ *                   or NaN and for a negative token.  May be NULL.
+ *   entropy[b]    = - sum_j s_j log s_j;  0 for a row that is masked altogether.  May be NULL.
+ *   top_ids, top_logprobs [B, k] = rdk_topk's entries with their log probabilities (-1, -inf where fewer are unmasked); not touched with k = 0.
+ *   stats [B, 4] fp32 = what the backward call reads (contents not part of the interface).  May be NULL.
+ * `kernel` (any format): the rows are over its n kept slots (N = n) and tokens, top_ids are target ids; NULL: ids are places in the row.
+ * A row with a NaN or a logit of +inf has log probabilities and an entropy of NaN (masked tokens -inf).  A row that is sure of an entry keeps the entropy and the
+ * log probability of that entry to their own last bits.  Tokens may repeat.  1 <= C <= 16, 0 <= k <= min(N, 128), N <= 2^30, B < 2^24.
+ *   rdk_logprobs_grad  dx [B, ldd] of x's type:  sum_c d_logprob[b, c] d logprob[b, c] / dx + d_entropy[b] d entropy[b] / dx
+ *       = 1 / T (sum_{c: token c at j} g_c - s_j (G + h (log s_j + entropy))),  g = d_logprob, h = d_entropy, G = sum of g over the tokens that the row holds;
+ *     tokens it does not hold add nothing, d_logprob or d_entropy may be NULL (0).  A row whose g (of tokens it holds) and h are all 0 has gradient 0 whatever its
+ *     logits hold (they are not read), and so has a row that is masked altogether.  No workspace.
+ *   rdk_logprobs_step  forward and backward at once, for d_logprob and d_entropy known beforehand; x is read once where a row fits the registers.
+ *     No ranks and no alternatives (k = 0).
+ * Gradients are of rows of logits only.  dx may be x itself (same stride), else they must not overlap.  Sums are held in fp32, a bf16 gradient is rounded once.
+ * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, N, C, k, strides, temperature, N other than the kernel's n, an overlap), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x, dx, stats,
+ * workspace), RDK_ERR_UNSUPPORTED (limits; weights with a temperature other than 1; gradients of weights; rdk_logprobs_step with k > 0), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ */
+typedef struct {
+    int32_t B, N, C, k;         /* rows, entries of a row, given tokens per row, alternatives per row */
+    float temperature;
+} rdk_logprobs_desc_t;
+rdk_status_t rdk_logprobs_workspace_bytes(const rdk_logprobs_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes);
+rdk_status_t rdk_logprobs(const rdk_logprobs_desc_t *desc, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t x_kind, int64_t ldx,
+                          const int32_t *tokens, float *logprob, int32_t *rank, float *entropy, int32_t *top_ids, float *top_logprobs, float *stats,
+                          void *workspace, size_t workspace_bytes, void *stream);
+rdk_status_t rdk_logprobs_grad(const rdk_logprobs_desc_t *desc, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t x_kind, int64_t ldx,
+                               const int32_t *tokens, const float *stats, const float *d_logprob, const float *d_entropy, void *dx, int64_t ldd,
+                               void *stream);
+rdk_status_t rdk_logprobs_step(const rdk_logprobs_desc_t *desc, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t x_kind, int64_t ldx,
+                               const int32_t *tokens, const float *d_logprob, const float *d_entropy, float *logprob, float *entropy, float *stats,
+                               void *dx, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows of an embedding table for a batch of tokens, and the table's gradient.  table [V, ldt], out [B, ldo], each fp32 or bf16:
+ *   rdk_embed       out[b, :] = scale * table[ids[b], :], rounded once; zeros for an id that the table does not hold (negative, from V on).
+ *   rdk_embed_grad  d_table[v, :] = scale * sum_{b: ids[b] = v} d_out[b, :]  (accumulate != 0: added to what d_table holds, and rows that no token names
+ *     are left as they are; accumulate = 0: these are set to 0), summed in fp32 and rounded once, in an order that depends on ids, B, V, d and types alone:
+ *     the same call gives the same bits.
+ * `kernel` (any format): the table has a row for each of its n kept slots (V = n) and ids are target ids, pruned ones are not held; NULL: ids are rows.
+ * Data of a row d elements wide; rows may lie at any stride.  Inputs and outputs must not overlap.  1 <= B < 2^24, 1 <= V <= 2^29, 1 <= d <= 2^24, scale finite.
+ * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, V, d, strides, scale, V other than the kernel's n, an overlap), RDK_ERR_DTYPE, RDK_ERR_ALIGN (table, out,
+ * d_table, d_out, workspace), RDK_ERR_UNSUPPORTED (limits), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ */
+typedef enum {
+    RDK_F32 = 1,
+    RDK_BF16 = 2
+} rdk_float_t;
+typedef struct {
+    int32_t B, V, d;            /* tokens, rows of the table, width */
+    float scale;
+} rdk_embed_desc_t;
+rdk_status_t rdk_embed(const rdk_embed_desc_t *desc, const rdk_kernel_t *kernel, const int32_t *ids, const void *table, rdk_float_t table_type,
+                       int64_t ldt, void *out, rdk_float_t out_type, int64_t ldo, void *stream);
+rdk_status_t rdk_embed_grad_workspace_bytes(const rdk_embed_desc_t *desc, size_t *bytes);
+rdk_status_t rdk_embed_grad(const rdk_embed_desc_t *desc, const rdk_kernel_t *kernel, const int32_t *ids, const void *d_out, rdk_float_t out_type,
+                            int64_t ldo, void *d_table, rdk_float_t table_type, int64_t ldt, int32_t accumulate, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
 /* The four Philox words of `count` consecutive positions, [count, 4] uint32 on the device (for
  * checking the random stream against an independent implementation). */
 rdk_status_t rdk_philox_words(uint64_t seed, uint64_t offset, int32_t count, uint32_t *words,
@@ -439,7 +504,10 @@ rdk_status_t rdk_philox_words(uint64_t seed, uint64_t offset, int32_t count, uin
  * tree_walk_kernel, verify_multi_kernel, verify_multi_round_kernel,
  * q_transpose_kernel, sparse_product_kernel, prep_a_split_kernel, exact_f32_split_kernel,
  * exact_reduce_kernel, prep_a_bf16_kernel, exact_bf16_kernel, topk_part_kernel, topk_merge_kernel, beam_merge_kernel, beam_reorder_kernel,
- * distill_row_kernel, distill_loop_kernel, distill_part_kernel, distill_finish_kernel, distill_grad_kernel.
+ * distill_row_kernel, distill_loop_kernel, distill_part_kernel, distill_finish_kernel, distill_grad_kernel,
+ * logprob_part_kernel, logprob_finish_kernel, logprob_grad_kernel, logprob_row_kernel,
+ * embed_kernel, embed_grad_few_kernel, embed_sort_kernel, embed_count_kernel, embed_scan_kernel, embed_place_kernel, embed_grad_sum_kernel,
+ * embed_grad_join_kernel.
  */
 rdk_status_t rdk_timing_select(const char *kernel_name);
 rdk_status_t rdk_timing_read(const char *kernel_name, int64_t *launches, double *total_ms);

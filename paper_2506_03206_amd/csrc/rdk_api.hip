@@ -840,6 +840,145 @@ rdk_status_t rdk_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *pa
     return launch_beam_reorder(G, W, K, parent, states, count, (hipStream_t)stream);
 }
 
+static rdk_status_t check_logprobs(const rdk_logprobs_desc_t *d, rdk_input_kind_t kind)
+{
+    if (!d) return RDK_ERR_NULL;
+    if (!kind_ok(kind)) return RDK_ERR_DTYPE;
+    if (d->B < 1 || d->N < 1 || d->C < 1 || d->k < 0 || d->k > d->N || !temperature_ok(d->temperature)) return RDK_ERR_SHAPE;
+    if (d->C > logprobs_max_tokens() || d->k > select_max_entries() || d->N > select_max_ids() || d->B > kMostRows) return RDK_ERR_UNSUPPORTED;
+    return kind == RDK_PROB_F32 && d->temperature != 1.f ? RDK_ERR_UNSUPPORTED : RDK_OK;
+}
+
+static rdk_status_t check_logprobs_call(const rdk_logprobs_desc_t *d, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t kind, int64_t ldx,
+                                        const int32_t *tokens)
+{
+    rdk_status_t rc = check_logprobs(d, kind);
+    if (rc != RDK_OK) return rc;
+    rc = check_rows(x, kind, ldx, d->N);
+    if (rc != RDK_OK) return rc;
+    if (!tokens) return RDK_ERR_NULL;
+    return kernel && kernel->h.n != d->N ? RDK_ERR_SHAPE : RDK_OK;
+}
+
+// Gradients: of logits, of a number of rows that a launch takes with all of their parts.
+static rdk_status_t check_logprobs_gradient(const rdk_logprobs_desc_t *d, rdk_input_kind_t kind, const void *x, int64_t ldx, const void *dx, int64_t ldd)
+{
+    if (kind == RDK_PROB_F32) return RDK_ERR_UNSUPPORTED;
+    const rdk_distill_desc_t as{d->B, d->N, 1, d->temperature};
+    return check_gradient(&as, kind, x, ldx, dx, ldd);
+}
+
+rdk_status_t rdk_logprobs_workspace_bytes(const rdk_logprobs_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes)
+{
+    if (!bytes) return RDK_ERR_NULL;
+    rdk_status_t rc = check_logprobs(desc, x_kind);
+    if (rc != RDK_OK) return rc;
+    *bytes = logprobs_workspace_bytes(*desc, x_kind) + 256;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_logprobs(const rdk_logprobs_desc_t *desc, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t x_kind, int64_t ldx,
+                          const int32_t *tokens, float *logprob, int32_t *rank, float *entropy, int32_t *top_ids, float *top_logprobs, float *stats,
+                          void *workspace, size_t workspace_bytes, void *stream)
+{
+    rdk_status_t rc = check_logprobs_call(desc, kernel, x, x_kind, ldx, tokens);
+    if (rc != RDK_OK) return rc;
+    if (!logprob || !workspace || (desc->k > 0 && (!top_ids || !top_logprobs))) return RDK_ERR_NULL;
+    if (!aligned16(workspace) || (stats && !aligned16(stats))) return RDK_ERR_ALIGN;
+    if (workspace_bytes < logprobs_workspace_bytes(*desc, x_kind)) return RDK_ERR_WORKSPACE;
+    return launch_logprobs(*desc, kernel ? &kernel->h : nullptr, RowInput{x, x_kind, ldx}, tokens, logprob, rank, entropy, top_ids, top_logprobs, stats,
+                           workspace, (hipStream_t)stream);
+}
+
+rdk_status_t rdk_logprobs_grad(const rdk_logprobs_desc_t *desc, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t x_kind, int64_t ldx,
+                               const int32_t *tokens, const float *stats, const float *d_logprob, const float *d_entropy, void *dx, int64_t ldd,
+                               void *stream)
+{
+    rdk_status_t rc = check_logprobs_call(desc, kernel, x, x_kind, ldx, tokens);
+    if (rc != RDK_OK) return rc;
+    if (!stats) return RDK_ERR_NULL;
+    if (!aligned16(stats)) return RDK_ERR_ALIGN;
+    rc = check_logprobs_gradient(desc, x_kind, x, ldx, dx, ldd);
+    if (rc != RDK_OK) return rc;
+    return launch_logprobs_grad(*desc, kernel ? &kernel->h : nullptr, RowInput{x, x_kind, ldx}, tokens, stats, d_logprob, d_entropy, dx, ldd,
+                                (hipStream_t)stream);
+}
+
+rdk_status_t rdk_logprobs_step(const rdk_logprobs_desc_t *desc, const rdk_kernel_t *kernel, const void *x, rdk_input_kind_t x_kind, int64_t ldx,
+                               const int32_t *tokens, const float *d_logprob, const float *d_entropy, float *logprob, float *entropy, float *stats,
+                               void *dx, int64_t ldd, void *workspace, size_t workspace_bytes, void *stream)
+{
+    rdk_status_t rc = check_logprobs_call(desc, kernel, x, x_kind, ldx, tokens);
+    if (rc != RDK_OK) return rc;
+    if (desc->k > 0) return RDK_ERR_UNSUPPORTED;
+    if (!logprob || !workspace) return RDK_ERR_NULL;
+    if (!aligned16(workspace) || (stats && !aligned16(stats))) return RDK_ERR_ALIGN;
+    rc = check_logprobs_gradient(desc, x_kind, x, ldx, dx, ldd);
+    if (rc != RDK_OK) return rc;
+    if (workspace_bytes < logprobs_workspace_bytes(*desc, x_kind)) return RDK_ERR_WORKSPACE;
+    return launch_logprobs_step(*desc, kernel ? &kernel->h : nullptr, RowInput{x, x_kind, ldx}, tokens, d_logprob, d_entropy, logprob, entropy, stats, dx,
+                                ldd, workspace, (hipStream_t)stream);
+}
+
+static rdk_status_t check_embed(const rdk_embed_desc_t *d, const rdk_kernel_t *kernel)
+{
+    if (!d) return RDK_ERR_NULL;
+    if (d->B < 1 || d->V < 1 || d->d < 1 || !(std::fabs(d->scale) <= FLT_MAX)) return RDK_ERR_SHAPE;
+    if (d->B > kMostRows || d->V > (1 << 29) || d->d > (1 << 24)) return RDK_ERR_UNSUPPORTED;
+    return kernel && kernel->h.n != d->V ? RDK_ERR_SHAPE : RDK_OK;
+}
+
+static bool float_ok(rdk_float_t t) { return t == RDK_F32 || t == RDK_BF16; }
+
+// What the table and the rows of the tokens have to be, whichever is written: `written` overlaps neither `read` nor the ids.
+static rdk_status_t check_embed_rows(const rdk_embed_desc_t &d, const int32_t *ids, const void *table, rdk_float_t table_type, int64_t ldt,
+                                     const void *rows, rdk_float_t rows_type, int64_t ldo, bool table_written)
+{
+    if (!float_ok(table_type) || !float_ok(rows_type)) return RDK_ERR_DTYPE;
+    if (!ids || !table || !rows) return RDK_ERR_NULL;
+    if (ldt < d.d || ldo < d.d || ldt > (int64_t)1 << 34 || ldo > (int64_t)1 << 34) return RDK_ERR_SHAPE;   // (extents stay inside 64 bits)
+    if (!aligned16(table) || !aligned16(rows)) return RDK_ERR_ALIGN;
+    const size_t table_bytes = ((size_t)(d.V - 1) * ldt + d.d) * (table_type == RDK_BF16 ? 2 : 4);
+    const size_t rows_bytes = ((size_t)(d.B - 1) * ldo + d.d) * (rows_type == RDK_BF16 ? 2 : 4);
+    if (overlap(table, table_bytes, rows, rows_bytes)) return RDK_ERR_SHAPE;
+    if (table_written ? overlap(table, table_bytes, ids, (size_t)d.B * 4) : overlap(rows, rows_bytes, ids, (size_t)d.B * 4)) return RDK_ERR_SHAPE;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_embed(const rdk_embed_desc_t *desc, const rdk_kernel_t *kernel, const int32_t *ids, const void *table, rdk_float_t table_type,
+                       int64_t ldt, void *out, rdk_float_t out_type, int64_t ldo, void *stream)
+{
+    rdk_status_t rc = check_embed(desc, kernel);
+    if (rc != RDK_OK) return rc;
+    rc = check_embed_rows(*desc, ids, table, table_type, ldt, out, out_type, ldo, false);
+    if (rc != RDK_OK) return rc;
+    return launch_embed(*desc, kernel ? &kernel->h : nullptr, ids, table, table_type, ldt, out, out_type, ldo, (hipStream_t)stream);
+}
+
+rdk_status_t rdk_embed_grad_workspace_bytes(const rdk_embed_desc_t *desc, size_t *bytes)
+{
+    if (!bytes) return RDK_ERR_NULL;
+    const rdk_status_t rc = check_embed(desc, nullptr);
+    if (rc != RDK_OK) return rc;
+    *bytes = embed_grad_workspace_bytes(*desc) + 256;
+    return RDK_OK;
+}
+
+rdk_status_t rdk_embed_grad(const rdk_embed_desc_t *desc, const rdk_kernel_t *kernel, const int32_t *ids, const void *d_out, rdk_float_t out_type,
+                            int64_t ldo, void *d_table, rdk_float_t table_type, int64_t ldt, int32_t accumulate, void *workspace,
+                            size_t workspace_bytes, void *stream)
+{
+    rdk_status_t rc = check_embed(desc, kernel);
+    if (rc != RDK_OK) return rc;
+    rc = check_embed_rows(*desc, ids, d_table, table_type, ldt, d_out, out_type, ldo, true);
+    if (rc != RDK_OK) return rc;
+    if (!workspace) return RDK_ERR_NULL;
+    if (!aligned16(workspace)) return RDK_ERR_ALIGN;
+    if (workspace_bytes < embed_grad_workspace_bytes(*desc)) return RDK_ERR_WORKSPACE;
+    return launch_embed_grad(*desc, kernel ? &kernel->h : nullptr, ids, d_out, out_type, ldo, d_table, table_type, ldt, accumulate != 0, workspace,
+                             (hipStream_t)stream);
+}
+
 rdk_status_t rdk_timing_select(const char *kernel_name)
 {
     std::lock_guard<std::mutex> lock(g_timing_mutex);

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -96,7 +97,8 @@ struct Rows {   // a [B, len] input
 
 struct Names {
     PyObject *h, *ws, *draft_ws, *fused_ws, *out_ws, *draft_ids, *accept, *alpha, *resid_mass, *resid_ids, *n_accepted, *out_tokens,
-        *cand_ids, *accepted, *token, *B, *N, *gamma, *ids, *values, *lse, *loss, *stats, *grad, *scores, *parent, *finished;
+        *cand_ids, *accepted, *token, *B, *N, *gamma, *ids, *values, *lse, *loss, *stats, *grad, *scores, *parent, *finished, *storage, *logprob, *rank,
+        *entropy, *top_ids, *top_logprobs;
 } g;
 
 struct Ref {   // an owned reference
@@ -637,11 +639,187 @@ PyObject *beam_reorder(PyObject *const *a)
     return status(rc);
 }
 
+// All tensors of a call lie on one device, the current one: a launch goes to that device's stream.
+void need_here(std::initializer_list<const at::Tensor *> all)
+{
+    for (const at::Tensor *t : all)
+        need(t->is_cuda() && t->device().index() == c10::hip::current_device(), "a tensor does not lie on the current device");
+}
+
+// A built kernel or None; its storage lies on the current device.
+const rdk_kernel_t *handle_or_none(PyObject *kernel)
+{
+    if (kernel == Py_None) return nullptr;
+    Ref a(PyObject_GetAttr(kernel, g.storage));
+    need_here({&tensor(a.o, "a kernel's storage is not a tensor")});
+    return handle(kernel);
+}
+
+// The tokens of rows x: int32 [B, C], or [B] for one each.
+const int32_t *tokens_of(PyObject *o, const at::Tensor &x, int32_t *C)
+{
+    const at::Tensor &t = tensor(o, "tokens is not a tensor");
+    need(t.scalar_type() == at::kInt && t.is_contiguous() && (t.dim() == 1 || t.dim() == 2) && t.size(0) == x.size(0),
+         "tokens: int32 [B, C] or [B] on the device, without gaps");
+    need(t.dim() == 1 || t.size(1) <= INT32_MAX, "too many tokens");
+    *C = t.dim() == 1 ? 1 : (int32_t)t.size(1);
+    need_here({&t});
+    return (const int32_t *)ptr(t);
+}
+
+rdk_logprobs_desc_t logprobs_desc(const at::Tensor &x, int32_t C, int32_t k, PyObject *temperature)
+{
+    rdk_logprobs_desc_t d;
+    d.B = extent(x, 0, "x is a [B, N] tensor");
+    d.N = extent(x, 1, "x is a [B, N] tensor");
+    d.C = C;
+    d.k = k;
+    d.temperature = real(temperature);
+    return d;
+}
+
+// kernel or None, x, tokens, x_kind, k, temperature, ranks, outputs
+PyObject *logprobs(PyObject *const *a)
+{
+    const rdk_kernel_t *kernel = handle_or_none(a[0]);
+    const at::Tensor &x = tensor(a[1], "x is not a tensor");
+    PyObject *o = a[7];
+    need(x.dim() == 2, "x is a [B, N] tensor");
+    int32_t C = 0;
+    const int32_t *tokens = tokens_of(a[2], x, &C);
+    const rdk_logprobs_desc_t d = logprobs_desc(x, C, int32_of(a[4]), a[5]);
+    const Rows xi(x, a[3]);
+    const bool ranks = PyObject_IsTrue(a[6]) == 1;
+    need_here({&x});
+    size_t bytes = 0;
+    const rdk_status_t rc = rdk_logprobs_workspace_bytes(&d, xi.kind, &bytes);
+    if (rc != RDK_OK) return status(rc);
+    const int64_t count = (int64_t)d.B * C, top = (int64_t)d.B * d.k;
+    const char *what = "the outputs were made for another batch shape";
+    const Output<float> lp = output<float>(o, g.logprob, at::kFloat, count, what), stats = output<float>(o, g.stats, at::kFloat, 4 * (int64_t)d.B, what),
+                        entropy = output<float>(o, g.entropy, at::kFloat, d.B, what), tl = output<float>(o, g.top_logprobs, at::kFloat, top, what);
+    const Output<int32_t> rank = output<int32_t>(o, g.rank, at::kInt, count, what), ti = output<int32_t>(o, g.top_ids, at::kInt, top, what);
+    need_here({&lp.t, &stats.t, &entropy.t, &tl.t, &rank.t, &ti.t});
+    const Scratch w = workspace(o, g.out_ws, bytes, x);
+    need_here({&w.t});
+    void *st = stream();
+    const rdk_status_t done = unlocked([&] {
+        return rdk_logprobs(&d, kernel, xi.p, xi.kind, xi.ld, tokens, lp.p, ranks ? rank.p : nullptr, entropy.p, ti.p, tl.p, stats.p, w.p, w.bytes, st);
+    });
+    if (done == RDK_OK && ranks) count_written(rank.t);
+    return status(done, {&lp.t, &stats.t, &entropy.t, &tl.t, &ti.t});
+}
+
+// kernel or None, x, tokens, temperature, d_logprob or None, d_entropy or None, outputs, step (0: the backward call, 1: forward and backward)
+PyObject *logprobs_grad(PyObject *const *a)
+{
+    const rdk_kernel_t *kernel = handle_or_none(a[0]);
+    const at::Tensor &x = tensor(a[1], "x is not a tensor");
+    PyObject *o = a[6];
+    const bool step = int32_of(a[7]) != 0;
+    need(x.dim() == 2, "x is a [B, N] tensor");
+    need(x.scalar_type() == at::kFloat || x.scalar_type() == at::kBFloat16, "logits are float32 or bfloat16");
+    const rdk_input_kind_t kind = x.scalar_type() == at::kBFloat16 ? RDK_LOGIT_BF16 : RDK_LOGIT_F32;
+    int32_t C = 0;
+    const int32_t *tokens = tokens_of(a[2], x, &C);
+    const rdk_logprobs_desc_t d = logprobs_desc(x, C, 0, a[3]);
+    const int64_t count = (int64_t)d.B * C, ldx = rows(x);
+    const float *gl = plain_or_none<float>(a[4], at::kFloat, count, "d_logprob: float32, of the shape of tokens, on the device, without gaps");
+    const float *ge = plain_or_none<float>(a[5], at::kFloat, d.B, "d_entropy: float32 [B] on the device, without gaps");
+    if (gl) need_here({&THPVariable_Unpack(a[4])});
+    if (ge) need_here({&THPVariable_Unpack(a[5])});
+    const char *what = "the outputs were made for another batch shape";
+    const Output<float> stats = output<float>(o, g.stats, at::kFloat, 4 * (int64_t)d.B, what);
+    Ref r(PyObject_GetAttr(o, g.grad));
+    const at::Tensor grad = tensor(r.o, "the outputs hold no gradient");
+    need(grad.scalar_type() == x.scalar_type() && grad.dim() == 2 && grad.size(0) == d.B && grad.size(1) == d.N, "the gradient has x's shape and type");
+    const int64_t ldd = rows(grad);
+    need_here({&x, &stats.t, &grad});
+    void *xp = ptr(x), *dx = ptr(grad), *st = stream();
+    if (!step)
+        return status(unlocked([&] { return rdk_logprobs_grad(&d, kernel, xp, kind, ldx, tokens, stats.p, gl, ge, dx, ldd, st); }), {&grad});
+    const Output<float> lp = output<float>(o, g.logprob, at::kFloat, count, what), entropy = output<float>(o, g.entropy, at::kFloat, d.B, what);
+    need_here({&lp.t, &entropy.t});
+    size_t bytes = 0;
+    const rdk_status_t rc = rdk_logprobs_workspace_bytes(&d, kind, &bytes);
+    if (rc != RDK_OK) return status(rc);
+    const Scratch w = workspace(o, g.out_ws, bytes, x);
+    need_here({&w.t});
+    return status(unlocked([&] {
+        return rdk_logprobs_step(&d, kernel, xp, kind, ldx, tokens, gl, ge, lp.p, entropy.p, stats.p, dx, ldd, w.p, w.bytes, st);
+    }), {&lp.t, &entropy.t, &stats.t, &grad});
+}
+
+rdk_float_t float_of(const at::Tensor &t)
+{
+    need(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16, "rows are float32 or bfloat16");
+    return t.scalar_type() == at::kBFloat16 ? RDK_BF16 : RDK_F32;
+}
+
+// The ids of a batch: int32 of any shape, without gaps; `rows` holds a row for each.
+const int32_t *ids_of(PyObject *o, const at::Tensor &rows, int32_t *B)
+{
+    const at::Tensor &t = tensor(o, "ids is not a tensor");
+    need(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() <= INT32_MAX, "ids: int32 on the device, without gaps");
+    need(rows.dim() == 2 && rows.size(0) == t.numel(), "a row for each of the ids");
+    *B = (int32_t)t.numel();
+    need_here({&t});
+    return (const int32_t *)ptr(t);
+}
+
+// kernel or None, ids, table, scale, out
+PyObject *embed(PyObject *const *a)
+{
+    const rdk_kernel_t *kernel = handle_or_none(a[0]);
+    const at::Tensor &table = tensor(a[2], "table is not a tensor");
+    const at::Tensor out = tensor(a[4], "out is not a tensor");
+    rdk_embed_desc_t d;
+    const int32_t *ids = ids_of(a[1], out, &d.B);
+    d.V = extent(table, 0, "table is a [V, d] tensor");
+    d.d = extent(table, 1, "table is a [V, d] tensor");
+    d.scale = real(a[3]);
+    need(out.size(1) == d.d, "out has the width of the table");
+    const int64_t ldt = rows(table), ldo = rows(out);
+    const rdk_float_t tt = float_of(table), ot = float_of(out);
+    need_here({&table, &out});
+    void *tp = ptr(table), *op = ptr(out), *st = stream();
+    return status(unlocked([&] { return rdk_embed(&d, kernel, ids, tp, tt, ldt, op, ot, ldo, st); }), {&out});
+}
+
+// kernel or None, ids, d_out, scale, accumulate, outputs
+PyObject *embed_grad(PyObject *const *a)
+{
+    const rdk_kernel_t *kernel = handle_or_none(a[0]);
+    const at::Tensor &d_out = tensor(a[2], "d_out is not a tensor");
+    PyObject *o = a[5];
+    rdk_embed_desc_t d;
+    const int32_t *ids = ids_of(a[1], d_out, &d.B);
+    Ref r(PyObject_GetAttr(o, g.grad));
+    const at::Tensor grad = tensor(r.o, "the outputs hold no gradient");
+    d.V = extent(grad, 0, "the gradient is a [V, d] tensor");
+    d.d = extent(grad, 1, "the gradient is a [V, d] tensor");
+    d.scale = real(a[3]);
+    const int32_t accumulate = PyObject_IsTrue(a[4]) == 1;
+    need(d_out.size(1) == d.d, "d_out has the width of the gradient");
+    const int64_t ldt = rows(grad), ldo = rows(d_out);
+    const rdk_float_t tt = float_of(grad), ot = float_of(d_out);
+    need_here({&d_out, &grad});
+    size_t bytes = 0;
+    const rdk_status_t rc = rdk_embed_grad_workspace_bytes(&d, &bytes);
+    if (rc != RDK_OK) return status(rc);
+    const Scratch w = workspace(o, g.out_ws, bytes, d_out);
+    need_here({&w.t});
+    void *gp = ptr(grad), *op = ptr(d_out), *st = stream();
+    return status(unlocked([&] { return rdk_embed_grad(&d, kernel, ids, op, ot, ldo, gp, tt, ldt, accumulate, w.p, w.bytes, st); }), {&grad});
+}
+
 #define RDK_METHOD(NAME, COUNT) {#NAME, (PyCFunction)(void (*)(void))(&guarded<NAME, COUNT>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RDK_METHOD(redistribute_verify, 12), RDK_METHOD(verify_sample, 9),  RDK_METHOD(redistribute_exact, 4),
                          RDK_METHOD(redistribute_linear, 7),  RDK_METHOD(sample_draft, 8),   RDK_METHOD(verify_multi, 8),
                          RDK_METHOD(tree_walk, 3),            RDK_METHOD(topk, 5),           RDK_METHOD(distill, 9),
-                         RDK_METHOD(beam_select, 7),          RDK_METHOD(beam_reorder, 4),   {nullptr, nullptr, 0, nullptr}};
+                         RDK_METHOD(beam_select, 7),          RDK_METHOD(beam_reorder, 4),
+                         RDK_METHOD(logprobs, 8),             RDK_METHOD(logprobs_grad, 8),  RDK_METHOD(embed, 5),
+                         RDK_METHOD(embed_grad, 6),           {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rdk_binding", "Per-step calls of the RDK library on torch tensors.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
@@ -652,10 +830,12 @@ PyMODINIT_FUNC PyInit__rdk_binding(void)
 {
     PyObject **slot[] = {&g.h, &g.ws, &g.draft_ws, &g.fused_ws, &g.out_ws, &g.draft_ids, &g.accept, &g.alpha, &g.resid_mass,
                          &g.resid_ids, &g.n_accepted, &g.out_tokens, &g.cand_ids, &g.accepted, &g.token, &g.B, &g.N, &g.gamma,
-                         &g.ids, &g.values, &g.lse, &g.loss, &g.stats, &g.grad, &g.scores, &g.parent, &g.finished};
+                         &g.ids, &g.values, &g.lse, &g.loss, &g.stats, &g.grad, &g.scores, &g.parent, &g.finished, &g.storage, &g.logprob,
+                         &g.rank, &g.entropy, &g.top_ids, &g.top_logprobs};
     const char *name[] = {"_h", "_ws", "_draft_ws", "fused_ws", "ws", "draft_ids", "accept", "alpha", "resid_mass",
                           "resid_ids", "n_accepted", "out_tokens", "cand_ids", "accepted", "token", "B", "N", "gamma",
-                          "ids", "values", "lse", "loss", "stats", "grad", "scores", "parent", "finished"};
+                          "ids", "values", "lse", "loss", "stats", "grad", "scores", "parent", "finished", "storage", "logprob",
+                          "rank", "entropy", "top_ids", "top_logprobs"};
     for (size_t i = 0; i < sizeof(slot) / sizeof(slot[0]); ++i) {
         *slot[i] = PyUnicode_InternFromString(name[i]);
         if (!*slot[i]) return nullptr;

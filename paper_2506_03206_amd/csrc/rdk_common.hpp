@@ -227,6 +227,24 @@ rdk_status_t launch_distill_loss(const rdk_distill_desc_t &d, const KernelHandle
 rdk_status_t launch_distill_grad(const rdk_distill_desc_t &d, const KernelHandle *h, RowInput z, const int32_t *top_ids, const float *top_logits,
                                  const float *stats, const float *weight, void *dz, int64_t ldd, hipStream_t st);
 
+// rdk_logprob.hip  (h: the rows' vocabulary, or NULL; above, above_entropy: what comes from above, either may be NULL)
+int logprobs_max_tokens();
+size_t logprobs_workspace_bytes(const rdk_logprobs_desc_t &d, rdk_input_kind_t kind);
+rdk_status_t launch_logprobs(const rdk_logprobs_desc_t &d, const KernelHandle *h, RowInput x, const int32_t *tokens, float *logprob, int32_t *rank,
+                             float *entropy, int32_t *top_ids, float *top_logprobs, float *stats, void *ws, hipStream_t st);
+rdk_status_t launch_logprobs_grad(const rdk_logprobs_desc_t &d, const KernelHandle *h, RowInput x, const int32_t *tokens, const float *stats,
+                                  const float *above, const float *above_entropy, void *dx, int64_t ldd, hipStream_t st);
+rdk_status_t launch_logprobs_step(const rdk_logprobs_desc_t &d, const KernelHandle *h, RowInput x, const int32_t *tokens, const float *above,
+                                  const float *above_entropy, float *logprob, float *entropy, float *stats, void *dx, int64_t ldd, void *ws,
+                                  hipStream_t st);
+
+// rdk_embed.hip  (h: the table's vocabulary, or NULL)
+rdk_status_t launch_embed(const rdk_embed_desc_t &d, const KernelHandle *h, const int32_t *ids, const void *table, rdk_float_t table_type, int64_t ldt,
+                          void *out, rdk_float_t out_type, int64_t ldo, hipStream_t st);
+size_t embed_grad_workspace_bytes(const rdk_embed_desc_t &d);
+rdk_status_t launch_embed_grad(const rdk_embed_desc_t &d, const KernelHandle *h, const int32_t *ids, const void *d_out, rdk_float_t out_type,
+                               int64_t ldo, void *d_table, rdk_float_t table_type, int64_t ldt, bool accumulate, void *ws, hipStream_t st);
+
 // rdk_verify.hip
 // What a call cannot do without, and what it asks for: with room for the records of the per-sequence scan the scan runs inside
 // the finish, with less it is a launch of its own.

@@ -19,6 +19,7 @@ OK = 0
 DENSE_F32, DENSE_BF16, SPARSE_TOPK, IDENTITY = 0, 1, 2, 3
 PROB_F32, LOGIT_F32, LOGIT_BF16 = 0, 1, 2
 LINEAR_TAYLOR, LINEAR_SPARSE = 0, 1
+F32, BF16 = 1, 2
 
 EXPORTS = [
     "rdk_status_string", "rdk_last_hip_error", "rdk_kernel_storage_bytes", "rdk_build_kernel", "rdk_destroy_kernel",
@@ -29,6 +30,8 @@ EXPORTS = [
     "rdk_verify_multi_workspace_bytes", "rdk_verify_multi", "rdk_tree_walk", "rdk_verify_sample_static",
     "rdk_topk_workspace_bytes", "rdk_topk", "rdk_distill_workspace_bytes", "rdk_distill_loss", "rdk_distill_grad",
     "rdk_distill_loss_grad", "rdk_beam_select_workspace_bytes", "rdk_beam_select", "rdk_beam_reorder",
+    "rdk_logprobs_workspace_bytes", "rdk_logprobs", "rdk_logprobs_grad", "rdk_logprobs_step", "rdk_embed", "rdk_embed_grad_workspace_bytes",
+    "rdk_embed_grad",
 ]
 
 
@@ -65,6 +68,14 @@ class State(ctypes.Structure):
     _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("src_stride", ctypes.c_int64), ("dst_stride", ctypes.c_int64),
                 ("segments", ctypes.c_int64), ("segment_bytes", ctypes.c_int64), ("src_pitch", ctypes.c_int64),
                 ("dst_pitch", ctypes.c_int64)]
+
+
+class LogprobsDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("N", ctypes.c_int32), ("C", ctypes.c_int32), ("k", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+
+class EmbedDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("V", ctypes.c_int32), ("d", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
 class RdkError(RuntimeError):
@@ -139,6 +150,13 @@ def lib():
         L.rdk_beam_select_workspace_bytes.argtypes = [ctypes.POINTER(BeamDesc), kind, psz]
         L.rdk_beam_select.argtypes = [ctypes.POINTER(BeamDesc), vp, kind, i64, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.rdk_beam_reorder.argtypes = [i32, i32, i32, vp, ctypes.POINTER(State), i32, vp]
+        L.rdk_logprobs_workspace_bytes.argtypes = [ctypes.POINTER(LogprobsDesc), kind, psz]
+        L.rdk_logprobs.argtypes = [ctypes.POINTER(LogprobsDesc), vp, vp, kind, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.rdk_logprobs_grad.argtypes = [ctypes.POINTER(LogprobsDesc), vp, vp, kind, i64, vp, vp, vp, vp, vp, i64, vp]
+        L.rdk_logprobs_step.argtypes = [ctypes.POINTER(LogprobsDesc), vp, vp, kind, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp]
+        L.rdk_embed.argtypes = [ctypes.POINTER(EmbedDesc), vp, vp, vp, kind, i64, vp, kind, i64, vp]
+        L.rdk_embed_grad_workspace_bytes.argtypes = [ctypes.POINTER(EmbedDesc), psz]
+        L.rdk_embed_grad.argtypes = [ctypes.POINTER(EmbedDesc), vp, vp, vp, kind, i64, vp, kind, i64, i32, vp, sz, vp]
         L.rdk_timing_select.argtypes = [ctypes.c_char_p]
         L.rdk_timing_read.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_double)]
         for name in EXPORTS:
@@ -469,6 +487,125 @@ def rdk_beam_reorder(states, parent, W=None, out=None):
     [G*W, ...] whose rows have at most one gap (a cache of which a part is filled) in the order of their memory.  Returns the reordered states."""
     _check((_native or native()).beam_reorder(states, parent, parent.shape[1] if W is None else W, out), "rdk_beam_reorder")
     return list(states) if out is None else list(out)
+
+
+class LogprobsOutputs:
+    """Outputs (and scratch) of the rdk_logprobs calls for a fixed batch shape: logprob, rank [B,C], entropy [B], top_ids, top_logprobs [B,k], stats [B,4]
+    (what the backward call reads), grad: the tensor that a gradient goes to, x itself included (None: made by the first call that has one)."""
+
+    def __init__(self, B, C, k, device, grad=None):
+        self.logprob = torch.empty((B, C), dtype=torch.float32, device=device)
+        self.rank = torch.empty((B, C), dtype=torch.int32, device=device)
+        self.entropy = torch.empty(B, dtype=torch.float32, device=device)
+        self.top_ids = torch.empty((B, k), dtype=torch.int32, device=device)
+        self.top_logprobs = torch.empty((B, k), dtype=torch.float32, device=device)
+        self.stats = torch.empty((B, 4), dtype=torch.float32, device=device)
+        self.grad = grad
+        self.ws = None
+
+
+def _tokens_per_row(tokens):
+    return 1 if tokens.dim() == 1 else tokens.shape[1]
+
+
+def rdk_logprobs(x, tokens, x_kind="logit", k=0, kernel=None, temperature=1.0, ranks=True, outputs=None):
+    """Log probabilities of tokens [B,C] (or [B]) under the rows x [B,N], their ranks, the rows' entropy, and the k top entries with their log probabilities.
+    kernel: the vocabulary of the rows (None: ids are places in the row); ranks=False leaves outputs.rank as it is."""
+    o = outputs or LogprobsOutputs(x.shape[0], _tokens_per_row(tokens), k, x.device)
+    _check((_native or native()).logprobs(kernel, x, tokens, x_kind, k, temperature, ranks, o), "rdk_logprobs")
+    return o
+
+
+def rdk_logprobs_grad(x, tokens, outputs, d_logprob=None, d_entropy=None, kernel=None, temperature=1.0):
+    """Gradient of sum(d_logprob * logprob) + sum(d_entropy * entropy) into outputs.grad, from the statistics that rdk_logprobs left in outputs."""
+    if outputs.grad is None:
+        outputs.grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check((_native or native()).logprobs_grad(kernel, x, tokens, temperature, d_logprob, d_entropy, outputs, 0), "rdk_logprobs_grad")
+    return outputs
+
+
+def rdk_logprobs_step(x, tokens, d_logprob=None, d_entropy=None, kernel=None, temperature=1.0, outputs=None):
+    """rdk_logprobs (without ranks and top entries) and rdk_logprobs_grad in one call, for what comes from above known beforehand."""
+    o = outputs or LogprobsOutputs(x.shape[0], _tokens_per_row(tokens), 0, x.device)
+    if o.grad is None:
+        o.grad = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check((_native or native()).logprobs_grad(kernel, x, tokens, temperature, d_logprob, d_entropy, o, 1), "rdk_logprobs_step")
+    return o
+
+
+class _TokenLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, tokens, kernel, temperature):
+        o = rdk_logprobs(x, tokens, kernel=kernel, temperature=temperature, ranks=False)
+        ctx.save_for_backward(x, tokens, o.stats)
+        ctx.kernel, ctx.temperature = kernel, temperature
+        ctx.set_materialize_grads(False)
+        return o.logprob.view(tokens.shape), o.entropy
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, above, above_entropy):
+        if above is None and above_entropy is None:
+            return None, None, None, None
+        x, tokens, stats = ctx.saved_tensors
+        o = LogprobsOutputs(x.shape[0], 0, 0, x.device)
+        o.stats = stats
+        rdk_logprobs_grad(x, tokens, o, None if above is None else above.contiguous(), None if above_entropy is None else above_entropy.contiguous(),
+                          ctx.kernel, ctx.temperature)
+        return o.grad, None, None, None
+
+
+def rdk_token_logprobs(x, tokens, kernel=None, temperature=1.0):
+    """rdk_logprobs of logits under torch's automatic differentiation: (log probabilities of the shape of tokens, entropy [B]), whose gradients reach x.  x
+    and tokens are kept for the backward pass, which raises torch's error where a call has written over them meanwhile."""
+    return _TokenLogprobs.apply(x, tokens, kernel, temperature)
+
+
+def rdk_embed(ids, table, scale=1.0, kernel=None, out=None, dtype=None):
+    """scale * table[ids] (zeros for ids that the table does not hold), of the table's type or `dtype`, or into out [ids.numel(), d].  kernel: the table has
+    a row for each of its kept slots, and ids are target ids."""
+    given = out
+    if out is None:
+        out = torch.empty((ids.numel(), table.shape[1]), dtype=dtype or table.dtype, device=table.device)
+    _check((_native or native()).embed(kernel, ids, table, scale, out), "rdk_embed")
+    return out.view(ids.shape + (table.shape[1],)) if given is None else out
+
+
+class EmbedGradOutputs:
+    """Output (and scratch) of rdk_embed_grad: grad [V,d] (a tensor that is given, or a new one)."""
+
+    def __init__(self, V, d, dtype, device, grad=None):
+        self.grad = torch.empty((V, d), dtype=dtype, device=device) if grad is None else grad
+        self.ws = None
+
+
+def rdk_embed_grad(ids, d_out, outputs, scale=1.0, kernel=None, accumulate=False):
+    """The gradient of the table of rdk_embed from that of its rows d_out [ids.numel(), d], into outputs.grad (accumulate: added to what it holds)."""
+    _check((_native or native()).embed_grad(kernel, ids, d_out, scale, accumulate, outputs), "rdk_embed_grad")
+    return outputs
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, ids, scale, kernel):
+        ctx.save_for_backward(ids)
+        ctx.args = scale, kernel, table.shape, table.dtype
+        return rdk_embed(ids, table, scale, kernel)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, above):
+        (ids,), (scale, kernel, shape, dtype) = ctx.saved_tensors, ctx.args
+        above = above.reshape(ids.numel(), shape[1]).contiguous()
+        if above.data_ptr() % 16:
+            above = above.clone()
+        o = EmbedGradOutputs(shape[0], shape[1], dtype, above.device)
+        return rdk_embed_grad(ids, above, o, scale, kernel).grad, None, None, None
+
+
+def rdk_embedding(ids, table, scale=1.0, kernel=None):
+    """rdk_embed under torch's automatic differentiation: rows [*ids.shape, d], whose gradient reaches the table (all of its rows)."""
+    return _Embedding.apply(table, ids, scale, kernel)
 
 
 def rdk_philox_words(seed, offset, count, device="cuda"):
