@@ -96,6 +96,19 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a)
 
 // ---- gradient
 
+constexpr int kShares = 256;      // of the tokens that are sorted, a workgroup each
+
+// What stands for a row among 0 .. V (V: a token that the table does not hold, behind all others) when rows are sorted; bits: of V.
+struct SortOrder {
+    int high;                 // bits above the lowest eight
+    uint32_t V;
+    __host__ __device__ __forceinline__ uint32_t of(uint32_t row) const
+    {
+        return row >= V ? (uint32_t)kShares << high : (row & (kShares - 1)) << high | row >> 8;
+    }
+    __device__ __forceinline__ uint32_t row(uint32_t key) const { return key >> high >= (uint32_t)kShares ? V : (key & ((1u << high) - 1)) << 8 | key >> high; }
+};
+
 struct EmbedGradArgs {
     Rows rows;
     const int32_t *ids;
@@ -107,7 +120,8 @@ struct EmbedGradArgs {
     int blocks, shift;        // workgroups along a row; 2^shift threads side by side on a row
     int fill_rows, fills;     // rows of the table that a workgroup sets to 0 where no token names them, and workgroups that do
     // sorted: tokens by row
-    const uint32_t *key;      // [B] the row, V for tokens that the table does not hold
+    SortOrder order;
+    const uint32_t *key;      // [B] what stands for the row
     const int32_t *at;        // [B] the token
     int piece, pieces;        // tokens of a piece
     float *partial;           // [pieces, 2, d]: sums of a row that begins before the piece; of one that begins in it and goes on behind it
@@ -129,17 +143,21 @@ __device__ __forceinline__ void write_sum(const EmbedGradArgs &a, int row, int c
     Cols<TABLE>::store(to, col, left, v);
 }
 
-// Sets rows first .. first + 63 of the table to 0 where `named` has no bit, by the threads of a workgroup.
+// Sets rows first .. first + count - 1 (at most 64) of the table to 0 where `named` has no bit, by the threads of a workgroup.
 template <int TABLE>
 __device__ __forceinline__ void clear_rows(const EmbedGradArgs &a, int first, int count, uint64_t named)
 {
-    const int units = (a.d - 1) / kCols + 1;
     const float zero[kCols] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    const int across = 1 << a.shift, down = kThreads >> a.shift;
-    for (int r = (int)threadIdx.x >> a.shift; r < count; r += down) {
-        if (named >> r & 1) continue;
-        void *to = const_cast<void *>(row_ptr<TABLE>(a.d_table, a.ldt, first + r));
-        for (int u = (int)threadIdx.x & (across - 1); u < units; u += across) Cols<TABLE>::store(to, u * kCols, a.d - u * kCols, zero);
+    const int units = (a.d - 1) / kCols + 1;
+    int r = 0, u = threadIdx.x;
+    while (true) {   // all units of the rows one behind the other
+        while (u >= units && r < count) {
+            u -= units;
+            ++r;
+        }
+        if (r >= count) break;
+        if (!(named >> r & 1)) Cols<TABLE>::store(const_cast<void *>(row_ptr<TABLE>(a.d_table, a.ldt, first + r)), u * kCols, a.d - u * kCols, zero);
+        u += kThreads;
     }
 }
 
@@ -236,28 +254,32 @@ __global__ __launch_bounds__(kThreads) void embed_grad_few_kernel(EmbedGradArgs 
     }
 }
 
-// ---- tokens sorted by row: least significant digits first, each pass stable
+// ---- tokens sorted by row, each row's in the order of the batch
+//
+// Rows are ordered by their lowest eight bits first (SortOrder), whatever order the table has: where frequent tokens have neighbouring ids, as
+// tokenizers give them, the workgroups that sort by these bits have shares of one size.
 
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / kWave;
-constexpr int kSortRounds = 16;                       // tokens of a thread
+constexpr int kSortRounds = 20;                       // tokens of a thread
 constexpr int kSortTokens = kSortThreads * kSortRounds;
-
-// How many tokens before it in its wavefront's round and in earlier rounds have its digit; counts[digit] grows by those of the round.
-__device__ __forceinline__ int rank_of(uint32_t digit, volatile uint32_t *counts)
+// The place of a token: places[digit] is that of the wavefront's next token of a digit, and grows by those of the round.
+__device__ __forceinline__ uint32_t place_next(uint32_t digit, volatile uint32_t *places)
 {
-    uint64_t like = ~(uint64_t)0;
+    uint32_t lo = ~0u, hi = ~0u;
 #pragma unroll
     for (int b = 0; b < kDigitBits; ++b) {
         const uint64_t on = __ballot(digit >> b & 1);
-        like &= digit >> b & 1 ? on : ~on;
+        const uint32_t other = (uint32_t)__builtin_amdgcn_sbfe((int)~digit, b, 1);   // all ones where the lane's bit is 0
+        lo &= (uint32_t)on ^ other;
+        hi &= (uint32_t)(on >> 32) ^ other;
     }
-    const uint32_t have = counts[digit];
-    const int rank = __popcll(like & (((uint64_t)1 << lane_id()) - 1));
+    const uint64_t like = (uint64_t)hi << 32 | lo;
+    const uint32_t first = places[digit], before = (uint32_t)__popcll(like & (((uint64_t)1 << lane_id()) - 1));
     __builtin_amdgcn_wave_barrier();
-    if (rank == 0) counts[digit] = have + (uint32_t)__popcll(like);   // one lane of those alike
+    if (before == 0) places[digit] = first + (uint32_t)__popcll(like);   // one lane of those alike
     __builtin_amdgcn_wave_barrier();
-    return (int)have + rank;
+    return first + before;
 }
 
 __device__ __forceinline__ uint32_t wave_scan(uint32_t v)   // inclusive
@@ -270,42 +292,47 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t v)   // inclusive
     return v;
 }
 
-// counts[w][digit] of the wavefronts become the places where their tokens of that digit begin: `base` of the digit (NULL: after all of
-// the lower digits) and the wavefronts before.  All threads call it.
+// counts[w][digit] of the wavefronts become the places where their tokens of that digit begin: behind `base` (the digit's; NULL: all tokens of the
+// lower digits) and the wavefronts before.  All threads call it.
 template <int WAVES>
 __device__ __forceinline__ void place_counts(uint32_t (*counts)[kDigits], uint32_t *totals, const uint32_t *base, int base_stride)
 {
     const int tid = threadIdx.x;
     constexpr int kT = WAVES * kWave;
-    static_assert(kT >= kDigits / 2 && kDigits == 8 * kWave, "two digits to a thread, eight to a lane");
+    static_assert(kDigits == 8 * kWave, "eight digits to a lane");
+    if (!base) {
+        for (int g = tid; g < kDigits; g += kT) {
+            uint32_t sum = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) sum += counts[w][g];
+            totals[g] = sum;
+        }
+        __syncthreads();
+        if (tid < kWave) {   // eight digits a lane
+            uint32_t own[8], sum = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                own[e] = totals[tid * 8 + e];
+                sum += own[e];
+            }
+            uint32_t before = wave_scan(sum) - sum;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                totals[tid * 8 + e] = before;
+                before += own[e];
+            }
+        }
+        __syncthreads();
+    }
     for (int g = tid; g < kDigits; g += kT) {
-        uint32_t sum = 0;
+        uint32_t own[WAVES], at = base ? base[(int64_t)g * base_stride] : totals[g];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) own[w] = counts[w][g];
+#pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-            const uint32_t c = counts[w][g];
-            counts[w][g] = sum;
-            sum += c;
+            counts[w][g] = at;
+            at += own[w];
         }
-        totals[g] = sum;
-    }
-    __syncthreads();
-    if (!base && tid < kWave) {   // eight digits a lane
-        uint32_t own[8], sum = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            own[e] = totals[tid * 8 + e];
-            sum += own[e];
-        }
-        uint32_t before = wave_scan(sum) - sum;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            totals[tid * 8 + e] = before;
-            before += own[e];
-        }
-    }
-    __syncthreads();
-    for (int g = tid; g < kDigits; g += kT) {
-        const uint32_t first = base ? base[(int64_t)g * base_stride] : totals[g];
-        for (int w = 0; w < WAVES; ++w) counts[w][g] += first;
     }
     __syncthreads();
 }
@@ -313,10 +340,11 @@ __device__ __forceinline__ void place_counts(uint32_t (*counts)[kDigits], uint32
 struct SortArgs {
     Rows rows;
     const int32_t *ids;
-    int B, V, passes;
+    int B, passes;
+    SortOrder order;
     uint32_t *key;
     int32_t *at;
-    // of more tokens than one workgroup sorts
+    // of more tokens than one workgroup holds
     const uint32_t *key_in;   // NULL: from ids
     const int32_t *at_in;
     int shift, tiles;
@@ -326,7 +354,7 @@ struct SortArgs {
 __device__ __forceinline__ uint32_t key_of(const SortArgs &a, int b)
 {
     const int row = a.rows.of(a.ids[b]);
-    return row < 0 ? (uint32_t)a.V : (uint32_t)row;
+    return a.order.of(row < 0 ? a.order.V : (uint32_t)row);
 }
 
 struct SortShared {
@@ -334,53 +362,98 @@ struct SortShared {
     uint16_t at[kSortTokens];
     uint32_t counts[kSortWaves][kDigits];
     uint32_t totals[kDigits];
+    uint32_t waves[kSortWaves][2];
 };
 
-// Up to 16384 tokens by one workgroup: they lie in registers, and go through LDS to their new places in every pass.
+// Up to 20480 tokens in one launch.  Every workgroup reads the keys of all, takes those of its share (the highest bits of the key) in their order, counts those
+// of lower shares, which come before them, and sorts its own by the bits that are left: a pass of nine bits for tables of up to 2^17 rows.  Tokens that the
+// table does not hold are a share of their own, in order already.
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
 {
     extern __shared__ __align__(16) char lds[];
     SortShared &sh = *(SortShared *)lds;
     const int tid = threadIdx.x, wid = tid / kWave, rounds = (a.B - 1) / kSortThreads + 1;
     const int first = wid * rounds * kWave + lane_id();   // a wavefront's tokens stand together
+    const uint32_t share = blockIdx.x;
     uint32_t key[kSortRounds];
-    int at[kSortRounds], rank[kSortRounds];
+    uint32_t mine = 0, lower = 0;
 #pragma unroll
     for (int r = 0; r < kSortRounds; ++r)
         if (r < rounds) {
-            at[r] = first + r * kWave;
-            key[r] = at[r] < a.B ? key_of(a, at[r]) : 0x7FFFFFFFu;   // behind all others
+            const int b = first + r * kWave;
+            key[r] = b < a.B ? key_of(a, b) : 0xFFFFFFFFu;
         }
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+        if (r < rounds) {
+            mine += key[r] >> a.order.high == share;
+            lower += key[r] >> a.order.high < share;
+        }
+    mine = (uint32_t)wave_sum((float)mine);   // (at most 1280 a wavefront: exact)
+    lower = (uint32_t)wave_sum((float)lower);
+    if (lane_id() == 0) {
+        sh.waves[wid][0] = mine;
+        sh.waves[wid][1] = lower;
+    }
+    __syncthreads();
+    uint32_t before = 0, n = 0, base = 0;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+        if (w < wid) before += sh.waves[w][0];
+        n += sh.waves[w][0];
+        base += sh.waves[w][1];
+    }
+    if (n == 0) return;
+#pragma unroll
+    for (int r = 0; r < kSortRounds; ++r)
+        if (r < rounds) {
+            const uint64_t who = __ballot(key[r] >> a.order.high == share);
+            if (who >> lane_id() & 1) {
+                const uint32_t to = before + __popcll(who & (((uint64_t)1 << lane_id()) - 1));
+                sh.key[to] = key[r];
+                sh.at[to] = (uint16_t)(first + r * kWave);
+            }
+            before += __popcll(who);
+        }
+    __syncthreads();
+    if (share >= (uint32_t)kShares || a.passes == 0) {
+        for (int i = tid; i < (int)n; i += kSortThreads) {
+            a.key[base + i] = sh.key[i];
+            a.at[base + i] = sh.at[i];
+        }
+        return;
+    }
+    const int own_rounds = ((int)n - 1) / kSortThreads + 1, own_first = wid * own_rounds * kWave + lane_id();
 #pragma unroll 1
     for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * kDigitBits;
+        const int shift = pass * kDigitBits, bits = min(a.order.high - shift, kDigitBits);
+        const uint32_t mask = (1u << bits) - 1;
         for (int i = tid; i < kSortWaves * kDigits; i += kSortThreads) (&sh.counts[0][0])[i] = 0;
         __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
-            if (r < rounds) rank[r] = rank_of(key[r] >> shift & (kDigits - 1), sh.counts[wid]);
+#pragma unroll 1
+        for (int r = 0; r < own_rounds; ++r) {
+            const int i = own_first + r * kWave;
+            if (i < (int)n) atomicAdd(&sh.counts[wid][sh.key[i] >> shift & mask], 1u);
+        }
         __syncthreads();
         place_counts<kSortWaves>(sh.counts, sh.totals, nullptr, 0);
-#pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
-            if (r < rounds) {
-                const uint32_t to = sh.counts[wid][key[r] >> shift & (kDigits - 1)] + rank[r];
-                sh.key[to] = key[r];
-                sh.at[to] = (uint16_t)at[r];
+#pragma unroll 1
+        for (int r = 0; r < own_rounds; ++r) {
+            const int i = own_first + r * kWave;
+            const uint32_t k = i < (int)n ? sh.key[i] : 0xFFFFFFFFu;
+            const uint32_t to = base + place_next(k >> shift & mask, sh.counts[wid]);   // (those behind the last token come last, and are not written)
+            if (i < (int)n) {
+                a.key[to] = k;
+                a.at[to] = sh.at[i];
             }
+        }
         __syncthreads();
-        if (pass + 1 == a.passes) break;
-#pragma unroll
-        for (int r = 0; r < kSortRounds; ++r)
-            if (r < rounds) {
-                key[r] = sh.key[first + r * kWave];
-                at[r] = sh.at[first + r * kWave];
-            }
+        if (pass + 1 == a.passes) return;
+        for (int i = tid; i < (int)n; i += kSortThreads) {   // (what this workgroup wrote)
+            sh.key[i] = a.key[base + i];
+            sh.at[i] = (uint16_t)a.at[base + i];
+        }
         __syncthreads();
-    }
-    for (int i = tid; i < a.B; i += kSortThreads) {
-        a.key[i] = sh.key[i];
-        a.at[i] = sh.at[i];
     }
 }
 
@@ -432,21 +505,19 @@ __global__ __launch_bounds__(kThreads) void embed_place_kernel(SortArgs a)
     for (int i = threadIdx.x; i < kWaves * kDigits; i += kThreads) (&counts[0][0])[i] = 0;
     __syncthreads();
     uint32_t key[kTileRounds];
-    int rank[kTileRounds];
 #pragma unroll
     for (int r = 0; r < kTileRounds; ++r) {
         const int b = first + r * kWave;
-        key[r] = b >= a.B ? 0x7FFFFFFFu : a.key_in ? a.key_in[b] : key_of(a, b);
+        key[r] = b >= a.B ? 0xFFFFFFFFu : a.key_in ? a.key_in[b] : key_of(a, b);
+        if (b < a.B) atomicAdd(&counts[wid][key[r] >> a.shift & (kDigits - 1)], 1u);
     }
-#pragma unroll
-    for (int r = 0; r < kTileRounds; ++r) rank[r] = rank_of(key[r] >> a.shift & (kDigits - 1), counts[wid]);   // (those behind the last token come last)
     __syncthreads();
     place_counts<kWaves>(counts, totals, a.table + tile, a.tiles);
 #pragma unroll
     for (int r = 0; r < kTileRounds; ++r) {
         const int b = first + r * kWave;
+        const uint32_t to = place_next(key[r] >> a.shift & (kDigits - 1), counts[wid]);   // (those behind the last token come last, and are not written)
         if (b < a.B) {
-            const uint32_t to = counts[wid][key[r] >> a.shift & (kDigits - 1)] + rank[r];
             a.key[to] = key[r];
             a.at[to] = a.at_in ? a.at_in[b] : b;
         }
@@ -467,13 +538,14 @@ __global__ __launch_bounds__(kThreads) void embed_grad_sum_kernel(EmbedGradArgs 
         if (tid < kWave) {
             bool is = false;
             if (tid < count) {   // the first token that is not below the row
+                const uint32_t key = a.order.of((uint32_t)(first + tid));
                 int lo = 0, hi = a.B;
                 while (lo < hi) {
                     const int mid = (lo + hi) >> 1;
-                    if (a.key[mid] < (uint32_t)(first + tid)) lo = mid + 1;
+                    if (a.key[mid] < key) lo = mid + 1;
                     else hi = mid;
                 }
-                is = lo < a.B && a.key[lo] == (uint32_t)(first + tid);
+                is = lo < a.B && a.key[lo] == key;
             }
             const uint64_t who = __ballot(is);
             if (tid == 0) named = who;
@@ -486,7 +558,7 @@ __global__ __launch_bounds__(kThreads) void embed_grad_sum_kernel(EmbedGradArgs 
     const int col = ((int)blockIdx.x % a.blocks * across + (tid & (across - 1))) * kCols, left = a.d - col;
     if (piece >= a.pieces || left <= 0) return;
     const int begin = piece * a.piece, end = min(begin + a.piece, a.B);
-    const uint32_t none = (uint32_t)a.V;
+    const uint32_t none = a.order.of(a.order.V);
     uint32_t run = a.key[begin];
     if (run >= none) return;
     bool head = begin > 0 && a.key[begin - 1] == run;   // the run at hand began before the piece
@@ -511,7 +583,7 @@ __global__ __launch_bounds__(kThreads) void embed_grad_sum_kernel(EmbedGradArgs 
             if (i + j >= end || run >= none) break;
             if (key[j] != run) {   // the run ends within the piece
                 if (head) keep(0);
-                else write_sum<TABLE>(a, (int)run, col, left, acc);
+                else write_sum<TABLE>(a, (int)a.order.row(run), col, left, acc);
                 head = false;
                 run = key[j];
 #pragma unroll
@@ -527,7 +599,7 @@ __global__ __launch_bounds__(kThreads) void embed_grad_sum_kernel(EmbedGradArgs 
     if (run >= none) return;
     if (head) keep(0);
     else if (end < a.B && a.key[end] == run) keep(1);
-    else write_sum<TABLE>(a, (int)run, col, left, acc);
+    else write_sum<TABLE>(a, (int)a.order.row(run), col, left, acc);
 }
 
 // The sums of a row that goes over the end of a piece, brought together by a workgroup to the piece where it begins: threads side by side on
@@ -539,7 +611,7 @@ __global__ __launch_bounds__(kThreads) void embed_grad_join_kernel(EmbedGradArgs
     const int piece = (int)blockIdx.x / a.blocks, begin = piece * a.piece, end = begin + a.piece, tid = threadIdx.x;
     if (end >= a.B) return;
     const uint32_t run = a.key[end - 1];
-    if (run >= (uint32_t)a.V || a.key[end] != run) return;
+    if (run >= a.order.of(a.order.V) || a.key[end] != run) return;
     if (a.key[begin] == run && begin > 0 && a.key[begin - 1] == run) return;   // it begins before this piece
     const int across = 1 << a.shift, down = kThreads >> a.shift, x = tid & (across - 1), y = tid >> a.shift;
     const int col = ((int)blockIdx.x % a.blocks * across + x) * kCols, left = a.d - col;
@@ -581,7 +653,7 @@ __global__ __launch_bounds__(kThreads) void embed_grad_join_kernel(EmbedGradArgs
 #pragma unroll
                 for (int e = 0; e < kCols; ++e) acc[e] += sums[w * across + x][e];
     }
-    if (y == 0 && left > 0) write_sum<TABLE>(a, (int)run, col, left, acc);
+    if (y == 0 && left > 0) write_sum<TABLE>(a, (int)a.order.row(run), col, left, acc);
 }
 
 // ---- host
@@ -599,6 +671,7 @@ struct GradPlan {
     bool few;
     int shift, blocks;
     int piece, pieces;
+    SortOrder order;
     int tiles, passes;
     size_t key, at, key2, at2, table, partial, bytes;   // places in the workspace
 };
@@ -618,9 +691,11 @@ GradPlan plan_of(const rdk_embed_desc_t &d)
     p.piece = 32;
     while (p.piece > 4 && waves / p.piece < 4096) p.piece >>= 1;
     p.pieces = (d.B - 1) / p.piece + 1;
-    int bits = 0;
-    while (bits < 31 && (d.V >> bits) != 0) ++bits;                      // keys are 0 .. V
-    p.passes = (bits - 1) / kDigitBits + 1;
+    int bits = 8;
+    while (((d.V - 1) >> bits) != 0) ++bits;                             // of rows
+    p.order = SortOrder{bits - 8, (uint32_t)d.V};
+    // all bits of the keys over tiles, or those that a share is sorted by
+    p.passes = d.B > kSortTokens ? bits / kDigitBits + 1 : (bits - 8 + kDigitBits - 1) / kDigitBits;
     p.tiles = d.B > kSortTokens ? (d.B - 1) / kTile + 1 : 0;
     size_t at = 0;
     auto room = [&](size_t bytes) {
@@ -656,7 +731,7 @@ rdk_status_t launch_sort(SortArgs s, const GradPlan &p, char *ws, hipStream_t st
     if (!p.tiles) {
         const rdk_status_t rc = sort_grant((const void *)embed_sort_kernel, sizeof(SortShared));
         if (rc != RDK_OK) return rc;
-        RDK_TIMED_LAUNCH("embed_sort_kernel", embed_sort_kernel, dim3(1), dim3(kSortThreads), sizeof(SortShared), st, s);
+        RDK_TIMED_LAUNCH("embed_sort_kernel", embed_sort_kernel, dim3(kShares + 1), dim3(kSortThreads), sizeof(SortShared), st, s);
         RDK_LAUNCH_CHECK("embed_sort_kernel");
         return RDK_OK;
     }
@@ -724,10 +799,10 @@ rdk_status_t launch_embed_grad(const rdk_embed_desc_t &d, const KernelHandle *h,
     if (!p.few) {
         SortArgs s{};
         s.rows = a.rows;
-        s.ids = ids; s.B = d.B; s.V = d.V; s.passes = p.passes;
+        s.ids = ids; s.B = d.B; s.order = p.order; s.passes = p.passes;
         s.key = (uint32_t *)(w + p.key);
         s.at = (int32_t *)(w + p.at);
-        a.key = s.key; a.at = s.at;
+        a.order = p.order; a.key = s.key; a.at = s.at;
         a.partial = (float *)(w + p.partial);
         const rdk_status_t rc = launch_sort(s, p, w, st);
         if (rc != RDK_OK) return rc;

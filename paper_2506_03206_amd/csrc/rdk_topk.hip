@@ -1,7 +1,7 @@
 // The k largest entries of rows over a vocabulary with the logarithm of their normaliser, and beam search's selection over beams and
-// vocabulary, which takes the K largest entries of every live beam and merges them per request.
-#include "rdk_select.hpp"
-#include "rdk_vec.hpp"
+// vocabulary, which takes the K largest entries of every live beam and merges them per request.  The log probabilities of given tokens with the row's top
+// entries beside them come from the same pass.
+#include "rdk_tokens.hpp"
 
 namespace rdk {
 
@@ -33,6 +33,8 @@ struct TopArgs {
     float *values, *lse;
 };
 
+struct NoTokens {};
+
 struct TopShared {
     SelectShared slow;
     uint64_t found[kFound];
@@ -41,6 +43,14 @@ struct TopShared {
     float wave_m[kTopWaves], wave_s[kTopWaves], bound[kTopWaves];
     int count;
 };
+
+// What a pass over tokens keeps in LDS, of the kernels that make one.
+template <bool TOKENS>
+__device__ __forceinline__ TokenShared<kTopThreads> &token_shared()
+{
+    __shared__ TokenShared<kTopThreads> sh;
+    return sh;
+}
 
 // The nth largest of the keys of 64 lanes, to their highest BITS bits, by halving.  (Rolled up: code that runs once is fetched while it runs.)
 template <int BITS>
@@ -152,6 +162,19 @@ __device__ __forceinline__ int take_equal(const void *xr, int begin, int whole, 
     return min(have, k);
 }
 
+// The top entries of a row with their log probabilities; of a row over kept slots with their target ids.
+template <int KIND>
+__device__ __forceinline__ void write_top(const TokenArgs &t, int32_t *ids, float *values, int k, int64_t row, const uint64_t *sorted, int n, RowSum r)
+{
+    if ((int)threadIdx.x < k) {
+        const bool in = (int)threadIdx.x < n;
+        const uint64_t e = in ? sorted[threadIdx.x] : 0;
+        const int32_t at = in ? (int32_t)entry_id(e) : -1;
+        ids[row * k + threadIdx.x] = in && t.kept_ids ? t.kept_ids[at] : at;
+        values[row * k + threadIdx.x] = in ? log_share<KIND>(key_value(entry_key(e)), r.m, log1pf(r.rest), t.inv_t) : -INFINITY;
+    }
+}
+
 template <int KIND>
 __device__ __forceinline__ void write_row(int32_t *ids, float *values, float *lse, int k, float inv_t, int64_t row, const uint64_t *sorted, int n,
                                           SoftStat st)
@@ -178,9 +201,11 @@ __device__ __forceinline__ void write_row(int32_t *ids, float *values, float *ls
 // Bound by HBM where rows are many and long: 1024 rows of 151936 fp32 logits, 64 kept, 100 us = 6.2 TB/s, weights 101 us, bf16 58 us = 5.4 TB/s (twice
 // the exponentials a byte; without the noting and the end 50 us).  Few rows are a chain: 8 rows of 128256 bf16 logits in 32 parts each
 // take 6.7 us, 2.5 of it until the loads are there and the bound stands, 1.3 for sifting, 0.7 for sorting, 0.5 for statistics and stores.
-template <int KIND>
-__global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
+// TOKENS: the sums are those of TokenPass, which also counts the ranks of the row's tokens.
+template <int KIND, bool TOKENS>
+__global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a, std::conditional_t<TOKENS, TokenArgs, NoTokens> t)
 {
+    static_assert(kRoundVecs == kTokenRoundVecs, "one pass for both");
     typedef Vec<KIND> V;
     constexpr int kRound = kTopThreads * kRoundVecs;    // vectors
     __shared__ TopShared sh;
@@ -219,7 +244,17 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         return b;
     };
     if (tid == 0) sh.count = 0;
-    if (tid < behind) {
+    [[maybe_unused]] TokenPass<KIND, kTopThreads> pass;
+    [[maybe_unused]] RowSum row_sum{none, 0.f, 0.f};
+    auto begin_tokens = [&]() __attribute__((always_inline)) {
+        if constexpr (TOKENS) {
+            pass.begin(t, row, xr, begin, begin + whole * V::kLen, a.N);
+            if (tid < behind) last = load1<KIND>(from, whole * V::kLen + tid);
+            if (behind > 0 && wid == 0) pass.single(t, last, begin + whole * V::kLen + tid);
+            m = pass.s.m;
+        }
+    };
+    if (!TOKENS && tid < behind) {
         last = load1<KIND>(from, whole * V::kLen + tid);
         m = fmaxf(m, last);
         if (KIND == RDK_PROB_F32) {
@@ -249,6 +284,10 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         float vm[kRoundVecs];
 #pragma unroll
         for (int j = 0; j < kRoundVecs; ++j) {
+            if constexpr (TOKENS) {
+                vm[j] = pass.vector(t, now[j]);
+                continue;
+            }
             float v[V::kLen], sum = 0.f;
             V::to(now[j], v);
             vm[j] = V::largest(v, none);
@@ -263,6 +302,8 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
             s += sum;
         }
         m = max3(m, max3(vm[0], vm[1], vm[2]), vm[3]);
+        if constexpr (TOKENS)
+            if (t.rank) pass.ranks(t, now, max3(max3(vm[0], vm[1], vm[2]), vm[3], none), base);
         if (round == next_bound) {
             next_bound = round + 1 + round / 2;
             publish(std::integral_constant<int, 16>());
@@ -287,6 +328,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     if (whole > 0) {
         u32x4 raw[kRoundVecs], ahead[kRoundVecs];   // in turn: the round at hand, and the next one on its way
         load_round(raw, 0, std::true_type());
+        begin_tokens();
 #pragma unroll 1
         for (int base = 0;; base += 2 * kRound) {
             load_round(ahead, base + kRound, std::false_type());
@@ -297,9 +339,14 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
             if (base + 2 * kRound >= whole) break;
         }
     }
+    if (whole == 0) begin_tokens();
     // statistics of the part, and its last bound
+    if constexpr (TOKENS) {
+        pass.s.m = m;
+        row_sum = pass.finish(t, from, whole, behind, token_shared<TOKENS>());
+    }
     const float wave_m = wave_max(m);
-    if constexpr (KIND != RDK_PROB_F32) {
+    if constexpr (!TOKENS && KIND != RDK_PROB_F32) {
         const float to = fminf(fmaxf(wave_m, -a.limit), a.limit) * a.c;
         s = s == 0.f ? 0.f : s * __builtin_amdgcn_exp2f(ref - to);
     }
@@ -315,7 +362,9 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
     SoftStat stat{none, 0.f};
 #pragma unroll
     for (int w = 0; w < kTopWaves; ++w) stat.m = fmaxf(stat.m, sh.wave_m[w]);
-    if constexpr (KIND == RDK_PROB_F32) {
+    if constexpr (TOKENS) {
+        stat.s = row_sum.rest;   // (looked at for NaN)
+    } else if constexpr (KIND == RDK_PROB_F32) {
 #pragma unroll
         for (int w = 0; w < kTopWaves; ++w) stat.s += sh.wave_s[w];
     } else {
@@ -402,7 +451,16 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a)
         // the best of every part and beam first, then the second best of every one, ...
         const uint32_t group = (uint32_t)row / (uint32_t)a.W, beam = (uint32_t)row % (uint32_t)a.W;
         if (tid < a.k) a.entries[(((int64_t)group * a.k + tid) * a.parts + part) * a.W + beam] = tid < n ? sh.slow.sorted[tid] : 0;
-        if (tid == 0) a.stat[row * a.parts + part] = stat;
+        if constexpr (TOKENS) {
+            if (wid == 0) pass.write_part(t, row, part, a.parts, row_sum, token_shared<TOKENS>());
+        } else if (tid == 0) {
+            a.stat[row * a.parts + part] = stat;
+        }
+        return;
+    }
+    if constexpr (TOKENS) {
+        if (wid == 0) write_tokens<KIND>(t, row, row_sum, pass.place, pass.value, pass.counted(t, token_shared<TOKENS>()));
+        write_top<KIND>(t, a.ids, a.values, a.k, row, sh.slow.sorted, n, row_sum);
         return;
     }
     write_row<KIND>(a.ids, a.values, a.lse, a.k, a.inv_t, row, sh.slow.sorted, n, stat);
@@ -500,6 +558,8 @@ __device__ __forceinline__ int select_entries(const uint64_t (&own)[EACH], int c
 }
 
 struct TopMergeArgs {
+    const void *x;        // TOKENS: the rows
+    int64_t ldx;
     const uint64_t *entries;
     const SoftStat *stat;
     int k, parts;
@@ -510,8 +570,8 @@ struct TopMergeArgs {
 
 // The parts of a row brought together.  A chain of reads of the caches, a search of a step a bit and a sort: 4.0 us with its launch for 8 rows of 32
 // parts and 16 kept (512 entries a row; bf16 keys have 16 bits that matter, others are searched to 24: with 32 4.5 us).
-template <int KIND, int EACH>
-__global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a)
+template <int KIND, int EACH, bool TOKENS>
+__global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a, std::conditional_t<TOKENS, TokenArgs, NoTokens> t)
 {
     __shared__ MergeShared<kTopThreads> sh;
     const int64_t row = blockIdx.x;
@@ -521,6 +581,16 @@ __global__ __launch_bounds__(kTopThreads) void topk_merge_kernel(TopMergeArgs a)
     for (int i = 0; i < EACH; ++i) {
         const int at = i * kTopThreads + (int)threadIdx.x;
         own[i] = at < count ? a.entries[row * count + at] : 0;
+    }
+    if constexpr (TOKENS) {
+        __shared__ RowSum row_sum;
+        if (threadIdx.x < kWave) {
+            const RowSum r = merge_tokens<KIND>(t, row, row_ptr<KIND>(a.x, a.ldx, row), a.parts);
+            if (threadIdx.x == 0) row_sum = r;
+        }
+        const int n = select_entries<kTopThreads, EACH, KIND == RDK_LOGIT_BF16 ? 16 : 24>(own, count, a.k, sh);
+        write_top<KIND>(t, a.ids, a.values, a.k, row, sh.slow.sorted, n, row_sum);
+        return;
     }
     SoftStat stat{0.f, 0.f};
     if (threadIdx.x < kWave) stat = merge_stats<KIND>(first_stat<KIND>(a.stat + row * a.parts, a.parts), a.stat + row * a.parts, a.parts, a.c);
@@ -699,14 +769,63 @@ rdk_status_t launch_topk(const rdk_topk_desc_t &d, RowInput x, int32_t *ids, flo
         a.stat = w.stat;
     }
     with_kind(x.kind, [&](auto kind) {
-        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<decltype(kind)::value>), dim3((unsigned)d.B * parts), dim3(kTopThreads), 0, st, a);
+        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<decltype(kind)::value, false>), dim3((unsigned)d.B * parts), dim3(kTopThreads), 0, st, a,
+                         NoTokens{});
         if (parts > 1) {
             constexpr int KIND = decltype(kind)::value;
-            const TopMergeArgs m{a.entries, a.stat, d.k, parts, a.inv_t, a.c, ids, values, lse};
+            const TopMergeArgs m{nullptr, 0, a.entries, a.stat, d.k, parts, a.inv_t, a.c, ids, values, lse};
             if (parts * d.k <= 4 * kTopThreads)
-                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 4>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m);
+                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 4, false>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m, NoTokens{});
             else
-                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 16>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m);
+                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 16, false>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m, NoTokens{});
+        }
+    });
+    RDK_LAUNCH_CHECK("topk_part_kernel");
+    return RDK_OK;
+}
+
+static Parts logprobs_top_parts(const rdk_logprobs_desc_t &d, rdk_input_kind_t kind)
+{
+    const int most = kMergeEntries / d.k;
+    return parts_of(d.B, d.N, kind, most < kWave ? most : kWave, false);   // (the tokens' merge has a lane to a part)
+}
+
+static size_t carve_tokens(const rdk_logprobs_desc_t &d, int parts, TokenArgs &t, TopWs &w, void *ws)
+{
+    size_t bytes = 0;
+    w = carve(d.B, parts, d.k, ws, &bytes);
+    return bytes + token_places(t, (char *)ws + bytes, d.B, parts);
+}
+
+size_t logprobs_top_workspace_bytes(const rdk_logprobs_desc_t &d, rdk_input_kind_t kind)
+{
+    const int parts = logprobs_top_parts(d, kind).count;
+    TokenArgs t{};
+    TopWs w;
+    t.C = d.C;
+    return parts > 1 ? carve_tokens(d, parts, t, w, nullptr) : 0;
+}
+
+rdk_status_t launch_logprobs_top(const rdk_logprobs_desc_t &d, RowInput x, TokenArgs t, int32_t *top_ids, float *top_logprobs, void *ws, hipStream_t st)
+{
+    const Parts split = logprobs_top_parts(d, x.kind);
+    const int parts = split.count;
+    TopArgs a = part_args(x, d.N, d.k, split, d.temperature);
+    a.ids = top_ids; a.values = top_logprobs;
+    TopWs w{};
+    if (parts > 1) {
+        carve_tokens(d, parts, t, w, ws);
+        a.entries = w.entries;
+    }
+    with_kind(x.kind, [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<KIND, true>), dim3((unsigned)d.B * parts), dim3(kTopThreads), 0, st, a, t);
+        if (parts > 1) {
+            const TopMergeArgs m{x.ptr, x.ld, a.entries, nullptr, d.k, parts, a.inv_t, a.c, top_ids, top_logprobs, nullptr};
+            if (parts * d.k <= 4 * kTopThreads)
+                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 4, true>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m, t);
+            else
+                RDK_TIMED_LAUNCH("topk_merge_kernel", (topk_merge_kernel<KIND, 16, true>), dim3((unsigned)d.B), dim3(kTopThreads), 0, st, m, t);
         }
     });
     RDK_LAUNCH_CHECK("topk_part_kernel");
@@ -739,7 +858,8 @@ rdk_status_t launch_beam_select(const rdk_beam_desc_t &d, RowInput x, const floa
     b.scores_out = scores_out; b.parent = parent; b.token = token; b.finished_out = finished_out;
     with_kind(x.kind, [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<KIND>), dim3((unsigned)(d.G * d.W) * parts), dim3(kTopThreads), 0, st, a);
+        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<KIND, false>), dim3((unsigned)(d.G * d.W) * parts), dim3(kTopThreads), 0, st, a,
+                         NoTokens{});
         const int count = d.W * parts * k;
         if (count <= 4 * 256)
             RDK_TIMED_LAUNCH("beam_merge_kernel", (beam_merge_kernel<KIND, 256, 4>), dim3((unsigned)d.G), dim3(256), 0, st, b);
