@@ -18,7 +18,7 @@ struct LogprobArgs {
 };
 
 // One pass over a part of a row.
-template <int KIND, int THREADS>
+template <int KIND, int THREADS, bool RANKS>
 __global__ __launch_bounds__(THREADS) void logprob_part_kernel(LogprobArgs a)
 {
     typedef Vec<KIND> V;
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(THREADS) void logprob_part_kernel(LogprobArgs a)
     const void *xr = row_ptr<KIND>(a.x, a.ldx, row);
     const char *from = (const char *)xr + (int64_t)begin * V::kSize;
     const int whole = (end - begin) / V::kLen, behind = (end - begin) % V::kLen;
-    TokenPass<KIND, THREADS> pass;
+    TokenPass<KIND, THREADS, RANKS> pass;
     // Always as many loads, of the last vector where the round has none of its own: the compiler counts loads in flight, and would wait for all of
     // them behind a branch that has some of its own.
     auto load_round = [&](u32x4 (&raw)[kRoundVecs], int base) __attribute__((always_inline)) {
@@ -50,7 +50,7 @@ __global__ __launch_bounds__(THREADS) void logprob_part_kernel(LogprobArgs a)
         static_assert(kRoundVecs == 4, "the largest of a round is formed of four");
         const float most = max3(max3(vm[0], vm[1], vm[2]), vm[3], no_value<KIND>());
         pass.s.m = fmaxf(pass.s.m, most);
-        if (a.t.rank) pass.ranks(a.t, now, most, base);
+        if constexpr (RANKS) pass.ranks(a.t, now, most, base);
     };
     u32x4 raw[kRoundVecs], ahead[kRoundVecs];   // in turn: the round at hand, and the next one on its way
     if (whole > 0) load_round(raw, 0);
@@ -211,11 +211,11 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a)
 // Forward and backward of a row that lies in the registers of one workgroup: read once.  With eight vectors a thread the exponentials are kept for the
 // gradient, with more they are formed again.
 template <int KIND, int THREADS, int VECS>
-__global__ __launch_bounds__(THREADS, 4) void logprob_row_kernel(LogprobArgs a, GradArgs b)
+__global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel(LogprobArgs a, GradArgs b)
 {
     typedef Vec<KIND> V;
     constexpr int kW = THREADS / kWave;
-    constexpr bool kKeep = VECS <= 8;
+    constexpr bool kKeep = VECS <= 2;
     __shared__ float wave_m[kW], wave_rest[kW], wave_pull[kW];
     __shared__ int wave_ties[kW];
     const int64_t row = blockIdx.x;
@@ -249,6 +249,7 @@ __global__ __launch_bounds__(THREADS, 4) void logprob_row_kernel(LogprobArgs a, 
         V::to(raw[j], v);
         m = V::largest(v, m);
         V::again(raw[j]);
+        __builtin_amdgcn_sched_barrier(0);
     }
     const float own = wave_max(m);
     if (lane_id() == 0) wave_m[wid] = own;
@@ -295,6 +296,7 @@ __global__ __launch_bounds__(THREADS, 4) void logprob_row_kernel(LogprobArgs a, 
         }
         rest += s;
         pull += p;
+        __builtin_amdgcn_sched_barrier(0);   // (one vector after the other, or registers hold fewer workgroups)
     }
     rest = wave_sum(rest);
     pull = wave_sum(pull);
@@ -336,6 +338,7 @@ __global__ __launch_bounds__(THREADS, 4) void logprob_row_kernel(LogprobArgs a, 
         if constexpr (kKeep) y = grad.template vector<KIND>(raw[j], terms[j], at * V::kLen, C, place, g);
         else y = grad.template vector<KIND>(raw[j], at * V::kLen, C, place, g);
         if (at < whole) V::store_at(to, (uint32_t)at * 16u, V::kLen, y);
+        __builtin_amdgcn_sched_barrier(0);
     }
     if (behind > 0 && wid == last_tid / kWave) {
         const u32x4 y = grad.template vector<KIND>(last, whole * V::kLen - (last_tid - tid) * V::kLen, C, place, g);
@@ -386,13 +389,19 @@ GradArgs grad_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, Row
     return a;
 }
 
+template <int KIND, int THREADS>
+void launch_parts(const LogprobArgs &a, int32_t B, hipStream_t st)
+{
+    const dim3 grid((unsigned)B * a.parts), block(THREADS);
+    if (a.t.rank) RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, true>), grid, block, 0, st, a);
+    else RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, false>), grid, block, 0, st, a);
+}
+
 template <int KIND>
 rdk_status_t launch_rows(const LogprobArgs &a, int32_t B, hipStream_t st)
 {
-    if (a.threads == kThreads)
-        RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, kThreads>), dim3((unsigned)B * a.parts), dim3(kThreads), 0, st, a);
-    else
-        RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, 1024>), dim3((unsigned)B * a.parts), dim3(1024), 0, st, a);
+    if (a.threads == kThreads) launch_parts<KIND, kThreads>(a, B, st);
+    else launch_parts<KIND, 1024>(a, B, st);
     if (a.parts > 1) RDK_TIMED_LAUNCH("logprob_finish_kernel", (logprob_finish_kernel<KIND>), dim3((unsigned)B), dim3(kWave), 0, st, a);
     RDK_LAUNCH_CHECK("logprob_part_kernel");
     return RDK_OK;
@@ -419,6 +428,12 @@ template <int KIND>
 rdk_status_t launch_step(const LogprobArgs &a, const GradArgs &b, int32_t B, hipStream_t st)
 {
     constexpr int kLen = Vec<KIND>::kLen;
+    // Few long rows: several workgroups to a row, in two launches more (bf16: 16 rows of 128256 20.3 -> 15.9 us, 128 of 32064 8.4 in one launch, 512 of
+    // 128256 62 in one and 73 in three).
+    if (a.parts > 1 && B <= 128 && a.n > 512 * 8 * kLen) {
+        const rdk_status_t rc = launch_rows<KIND>(a, B, st);
+        return rc == RDK_OK ? launch_grad<KIND>(b, B, st) : rc;
+    }
     if (a.n <= 256 * 2 * kLen) return launch_row<KIND, 256, 2>(a, b, B, st);
     if (a.n <= 256 * 8 * kLen) return launch_row<KIND, 256, 8>(a, b, B, st);
     if (a.n <= 512 * 8 * kLen) return launch_row<KIND, 512, 8>(a, b, B, st);

@@ -196,7 +196,7 @@ __device__ __forceinline__ u16x2 u16x2_of(uint32_t w) { return __builtin_bit_cas
 // with the largest of all has that entry's 1 in its sum, in whose rounding its other entries may be lost: where that matters (all others
 // together come to less than it) this lane's vectors are read again, out of the cache, a vector to a thread, and summed without it.  Entries before a token in the
 // order of rdk_topk are those above its value, and those that equal it at a lower place: in vectors before its own the bound is the next number below.
-template <int KIND, int THREADS>
+template <int KIND, int THREADS, bool RANKS>
 struct TokenPass {
     typedef Vec<KIND> V;
     typedef TokenShared<THREADS> Shared;
@@ -222,7 +222,7 @@ struct TokenPass {
             value = v[0];
 #pragma unroll
             for (int e = 1; e < V::kLen; ++e) value = place - own == e ? v[e] : value;
-            if (a.rank && threadIdx.x < kWave && here >= 0 && own + V::kLen <= last)
+            if (RANKS && threadIdx.x < kWave && here >= 0 && own + V::kLen <= last)
 #pragma unroll
                 for (int e = 0; e < V::kLen - 1; ++e) count += (own + e < place) & (v[e] == value);
         }
@@ -234,7 +234,7 @@ struct TokenPass {
         s.m = fmaxf(s.m, x);
         if (x > s.high) s.raise(x, a.c, a.margin);
         s.add({x}, a.c);
-        if (a.rank)
+        if (RANKS)
             for (int c = 0; c < a.C; ++c) {
                 const int to = lane_value(place, c);
                 const float v = lane_value(value, c);
@@ -317,7 +317,7 @@ struct TokenPass {
             sh.wave[wid].sum_besides = sum_b;
             sh.wave[wid].pull_besides = pull_b;
         }
-        if (lane_id() < a.C) sh.rank[wid][lane_id()] = count;
+        if (RANKS && lane_id() < a.C) sh.rank[wid][lane_id()] = count;
         __syncthreads();
         float m = sh.wave[0].m;
         int holds = 0;   // the first wavefront that has the largest value
@@ -406,7 +406,7 @@ struct TokenPass {
     __device__ __forceinline__ int counted(const TokenArgs &a, const Shared &sh) const
     {
         int all = count;
-        if (lane_id() < a.C)
+        if (RANKS && lane_id() < a.C)
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) all += sh.rank[w][lane_id()];
         return all;
@@ -417,7 +417,7 @@ struct TokenPass {
     {
         const int all = counted(a, sh);
         if (lane_id() == 0) a.part_sum[row * parts + part] = make_float4(r.m, r.rest, r.pull, 0.f);
-        if (a.rank && lane_id() < a.C) a.part_rank[(row * a.C + lane_id()) * parts + part] = all;
+        if (RANKS && lane_id() < a.C) a.part_rank[(row * a.C + lane_id()) * parts + part] = all;
     }
 };
 

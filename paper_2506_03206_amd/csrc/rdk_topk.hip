@@ -244,7 +244,7 @@ __global__ __launch_bounds__(kTopThreads) void topk_part_kernel(TopArgs a, std::
         return b;
     };
     if (tid == 0) sh.count = 0;
-    [[maybe_unused]] TokenPass<KIND, kTopThreads> pass;
+    [[maybe_unused]] TokenPass<KIND, kTopThreads, true> pass;
     [[maybe_unused]] RowSum row_sum{none, 0.f, 0.f};
     auto begin_tokens = [&]() __attribute__((always_inline)) {
         if constexpr (TOKENS) {

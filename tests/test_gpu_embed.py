@@ -88,7 +88,7 @@ def check_gradient(ids, d_out, V, dtype, scale, accumulate, ld=0, kernel=None, s
 
 
 @pytest.mark.parametrize("how", ["uniform", "zipf", "one", "none", "ends"])
-@pytest.mark.parametrize("B", [1, 2, 63, 300, 1023, 1024, 1025, 2049, 5000, 16384, 16385, 40000])
+@pytest.mark.parametrize("B", [1, 2, 63, 300, 1023, 1024, 1025, 2049, 5000, 16384, 20480, 20481, 40000])
 def test_gradient(how, B):
     i = 0
     for V, d in ((1, 5), (513, 64), (8000, 24), (300000, 8)):
