@@ -441,7 +441,7 @@ rdk_status_t rdk_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *pa
  *     logits hold (they are not read), and so has a row that is masked altogether.  No workspace.
  *   rdk_logprobs_step  forward and backward at once, for d_logprob and d_entropy known beforehand; x is read once where a row fits the registers.
  *     No ranks and no alternatives (k = 0).
- * Gradients are of rows of logits only.  dx may be x itself (same stride), else they must not overlap.  Sums are held in fp32, a bf16 gradient is rounded once.
+ * Gradients are of rows of logits only, B < 2^22 and B ceil(N / 16384) < 2^24 (fp32: N / 8192).  dx may be x itself (same stride), else they must not overlap.  Sums are held in fp32, a bf16 gradient is rounded once.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, N, C, k, strides, temperature, N other than the kernel's n, an overlap), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x, dx, stats,
  * workspace), RDK_ERR_UNSUPPORTED (limits; weights with a temperature other than 1; gradients of weights; rdk_logprobs_step with k > 0), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */
@@ -467,7 +467,7 @@ rdk_status_t rdk_logprobs_step(const rdk_logprobs_desc_t *desc, const rdk_kernel
  *     are left as they are; accumulate = 0: these are set to 0), summed in fp32 and rounded once, in an order that depends on ids, B, V, d and types alone:
  *     the same call gives the same bits.
  * `kernel` (any format): the table has a row for each of its n kept slots (V = n) and ids are target ids, pruned ones are not held; NULL: ids are rows.
- * Data of a row d elements wide; rows may lie at any stride.  Inputs and outputs must not overlap.  1 <= B < 2^24, 1 <= V <= 2^29, 1 <= d <= 2^24, scale finite.
+ * Data of a row d elements wide; rows may lie at any stride.  Inputs and outputs must not overlap.  1 <= B < 2^24, 1 <= V <= 2^29, 1 <= d <= 2^20, scale finite.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, V, d, strides, scale, V other than the kernel's n, an overlap), RDK_ERR_DTYPE, RDK_ERR_ALIGN (table, out,
  * d_table, d_out, workspace), RDK_ERR_UNSUPPORTED (limits), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */

@@ -865,7 +865,9 @@ static rdk_status_t check_logprobs_gradient(const rdk_logprobs_desc_t *d, rdk_in
 {
     if (kind == RDK_PROB_F32) return RDK_ERR_UNSUPPORTED;
     const rdk_distill_desc_t as{d->B, d->N, 1, d->temperature};
-    return check_gradient(&as, kind, x, ldx, dx, ldd);
+    const rdk_status_t rc = check_gradient(&as, kind, x, ldx, dx, ldd);
+    if (rc != RDK_OK) return rc;
+    return (int64_t)d->B * logprobs_grad_parts(d->N, kind) > kMostRows || d->B >= (1 << 22) ? RDK_ERR_UNSUPPORTED : RDK_OK;
 }
 
 rdk_status_t rdk_logprobs_workspace_bytes(const rdk_logprobs_desc_t *desc, rdk_input_kind_t x_kind, size_t *bytes)
@@ -924,7 +926,7 @@ static rdk_status_t check_embed(const rdk_embed_desc_t *d, const rdk_kernel_t *k
 {
     if (!d) return RDK_ERR_NULL;
     if (d->B < 1 || d->V < 1 || d->d < 1 || !(std::fabs(d->scale) <= FLT_MAX)) return RDK_ERR_SHAPE;
-    if (d->B > kMostRows || d->V > (1 << 29) || d->d > (1 << 24)) return RDK_ERR_UNSUPPORTED;
+    if (d->B > kMostRows || d->V > (1 << 29) || d->d > (1 << 20)) return RDK_ERR_UNSUPPORTED;
     return kernel && kernel->h.n != d->V ? RDK_ERR_SHAPE : RDK_OK;
 }
 

@@ -229,6 +229,7 @@ rdk_status_t launch_distill_grad(const rdk_distill_desc_t &d, const KernelHandle
 
 // rdk_logprob.hip  (h: the rows' vocabulary, or NULL; above, above_entropy: what comes from above, either may be NULL)
 int logprobs_max_tokens();
+int logprobs_grad_parts(int32_t N, rdk_input_kind_t kind);   // workgroups of a row of the backward call
 size_t logprobs_workspace_bytes(const rdk_logprobs_desc_t &d, rdk_input_kind_t kind);
 rdk_status_t launch_logprobs(const rdk_logprobs_desc_t &d, const KernelHandle *h, RowInput x, const int32_t *tokens, float *logprob, int32_t *rank,
                              float *entropy, int32_t *top_ids, float *top_logprobs, float *stats, void *ws, hipStream_t st);

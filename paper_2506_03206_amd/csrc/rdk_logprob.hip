@@ -410,7 +410,7 @@ rdk_status_t launch_rows(const LogprobArgs &a, int32_t B, hipStream_t st)
 template <int KIND>
 rdk_status_t launch_grad(GradArgs a, int32_t B, hipStream_t st)
 {
-    a.parts = (a.n - 1) / (kThreads * kGradVecs * Vec<KIND>::kLen) + 1;
+    a.parts = logprobs_grad_parts(a.n, (rdk_input_kind_t)KIND);
     RDK_TIMED_LAUNCH("logprob_grad_kernel", (logprob_grad_kernel<KIND, kGradVecs>), dim3((unsigned)B * a.parts), dim3(kThreads), 0, st, a);
     RDK_LAUNCH_CHECK("logprob_grad_kernel");
     return RDK_OK;
@@ -430,7 +430,7 @@ rdk_status_t launch_step(const LogprobArgs &a, const GradArgs &b, int32_t B, hip
     constexpr int kLen = Vec<KIND>::kLen;
     // Few long rows: several workgroups to a row, in two launches more (bf16: 16 rows of 128256 20.3 -> 15.9 us, 128 of 32064 8.4 in one launch, 512 of
     // 128256 62 in one and 73 in three).
-    if (a.parts > 1 && B <= 128 && a.n > 512 * 8 * kLen) {
+    if (a.parts > 1 && B < 128 && a.n > 512 * 8 * kLen) {
         const rdk_status_t rc = launch_rows<KIND>(a, B, st);
         return rc == RDK_OK ? launch_grad<KIND>(b, B, st) : rc;
     }
@@ -446,6 +446,11 @@ rdk_status_t launch_step(const LogprobArgs &a, const GradArgs &b, int32_t B, hip
 }  // namespace
 
 int logprobs_max_tokens() { return kMaxTokens; }
+
+int logprobs_grad_parts(int32_t N, rdk_input_kind_t kind)
+{
+    return (N - 1) / (kThreads * kGradVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4)) + 1;
+}
 
 TokenArgs token_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, const int32_t *tokens, float *logprob, int32_t *rank, float *entropy,
                           float4 *stats)

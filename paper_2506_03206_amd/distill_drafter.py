@@ -1,11 +1,15 @@
 #!/usr/bin/env python3
-"""A pruned drafter distilled from its target's top logits, and beam search with the target and with the trained drafter.
+"""A pruned drafter distilled from its target's top logits, another trained on its target's tokens, and beam search with the target and with the trained drafter.
 
 The target is a small recurrent model with random weights: a state s, s' = tanh(s A + E[token]), and logits s U on a Zipf rank bias over N ids.
 The drafter sees the same state and has a trainable head V over the n most frequent ids.
 
   training   the target's rows of a batch of states -> rdk_topk keeps K logits and the normaliser of each (all that is stored of a teacher)
              -> rdk_distill_loss_grad gives the loss and its gradient with respect to the drafter's logits -> the head's weights by one product
+  tokens     a drafter that reads one state less and the token that followed, by an embedding over its own vocabulary (rdk_embed), trained on the
+             tokens that the target drew: rdk_logprobs_step gives their log probabilities and the gradient with respect to the logits, rdk_embed_grad that of the
+             embedding
+  scoring    the target's own text under its rows: log probabilities, ranks, entropy and the top alternatives (rdk_logprobs)
   check      the acceptance rate alpha of the drafter under redistribution (Eq. 3), before and after, by rdk_redistribute_verify
   decoding   beam search over the target's rows and over the drafter's redistributed rows: rdk_beam_select picks the beams, rdk_beam_reorder moves
              their recurrent states and token histories
@@ -34,7 +38,7 @@ class Target:
         self.N, self.d, self.gen = N, d, g
 
     def step(self, state, token):
-        return torch.tanh(state @ self.A + self.E[token])
+        return torch.tanh(state @ self.A + rdk.rdk_embed(token.to(torch.int32).contiguous(), self.E))
 
     def rows(self, state, dtype=torch.bfloat16):
         return (state @ self.U + self.bias).to(dtype)
@@ -47,6 +51,10 @@ class Target:
             s = self.step(s, torch.multinomial(p, 1, generator=self.gen)[:, 0])
         return s
 
+    def draw(self, state):
+        """A token of every row."""
+        return torch.multinomial(torch.softmax(self.rows(state).float(), 1), 1, generator=self.gen)[:, 0].to(torch.int32)
+
 
 class Drafter:
     """A head over the kept ids on the target's state."""
@@ -58,6 +66,25 @@ class Drafter:
 
     def rows(self, state):
         return torch.addmm(self.V[-1], state, self.V[:-1]).to(torch.bfloat16)
+
+
+class TokenDrafter(Drafter):
+    """A head on the state before the last token and an embedding of that token over the kept ids (zero for others)."""
+
+    def __init__(self, target, n):
+        super().__init__(target, n)
+        self.E = torch.zeros((n, target.d), device=self.kept.device)
+
+    def step(self, state, token, following, weight, entropy_weight=None):
+        """Log probabilities of the following tokens [B], entropies, and the gradients of sum(weight * logprob) + sum(entropy_weight * entropy) with respect to
+        the head and the embedding.  Tokens that the vocabulary does not hold have a log probability of -inf and no gradient."""
+        h = state + rdk.rdk_embed(token, self.E, kernel=self.kernel)
+        o = rdk.rdk_logprobs_step(self.rows(h), following, weight, entropy_weight, kernel=self.kernel)
+        dz = o.grad.float()
+        head = torch.cat([h.t() @ dz, dz.sum(0, keepdim=True)])
+        table = rdk.EmbedGradOutputs(self.E.shape[0], self.E.shape[1], torch.float32, self.E.device)
+        rdk.rdk_embed_grad(token, dz @ self.V[:-1].t(), table, kernel=self.kernel)
+        return o.logprob[:, 0], o.entropy, head, table.grad
 
 
 def train(target, drafter, steps, B, K, temperature, rate, remainder=True):
@@ -78,6 +105,33 @@ def train(target, drafter, steps, B, K, temperature, rate, remainder=True):
         second.mul_(0.99).addcmul_(grad, grad, value=0.01)
         drafter.V -= rate * (first / (1 - 0.9 ** t)) / ((second / (1 - 0.99 ** t)).sqrt() + 1e-8)
     return torch.stack(losses).tolist()
+
+
+def train_on_tokens(target, drafter, steps, B, rate, entropy=0.0):
+    """Mean losses of the tokens that the drafter's vocabulary holds, one a step.  Adam on its head and its embedding; entropy: weight of the mean entropy, which is
+    held up by it."""
+    params = [drafter.V, drafter.E]
+    first, second, losses = [torch.zeros_like(p) for p in params], [torch.zeros_like(p) for p in params], []
+    weight = torch.full((B,), -1.0 / B, device=drafter.V.device)
+    for t in range(1, steps + 1):
+        s = target.states(B)
+        token = target.draw(s)
+        following = target.draw(target.step(s, token))
+        logprob, _, *grads = drafter.step(s, token, following, weight, weight * entropy if entropy else None)
+        held = logprob > -float("inf")
+        losses.append(-torch.where(held, logprob, 0.0).sum() / held.sum().clamp(min=1))
+        for p, m, v, g in zip(params, first, second, grads):
+            m.mul_(0.9).add_(g, alpha=0.1)
+            v.mul_(0.99).addcmul_(g, g, value=0.01)
+            p -= rate * (m / (1 - 0.9 ** t)) / ((v / (1 - 0.99 ** t)).sqrt() + 1e-8)
+    return torch.stack(losses).tolist()
+
+
+def score(target, B, top):
+    """The target's own next tokens under its rows: mean log probability, mean entropy, the share of them that is among the top entries."""
+    s = target.states(B)
+    o = rdk.rdk_logprobs(target.rows(s), target.draw(s), k=top)
+    return float(o.logprob.mean()), float(o.entropy.mean()), float((o.rank < top).float().mean())
 
 
 def acceptance(target, drafter, B=512):
@@ -130,9 +184,14 @@ def main():
     eos = int(target.by_frequency[0])
     history, scores, _ = beam_search(target, 4, 4, 12, eos)
     draft_history, draft_scores, _ = beam_search(target, 4, 4, 12, eos, drafter)
+    by_tokens = TokenDrafter(target, a.n)
+    token_losses = train_on_tokens(target, by_tokens, a.steps, a.batch, a.rate)
+    logprob, entropy, among_top = score(target, a.batch, 5)
     print(json.dumps({"N": a.N, "n": a.n, "loss_first": losses[0], "loss_last": losses[-1], "alpha_before": before, "alpha_after": after,
                       "best_scores": scores[:, 0].tolist(), "best_tokens": history[:, 0].tolist(),
-                      "drafter_best_scores": draft_scores[:, 0].tolist(), "drafter_best_tokens": draft_history[:, 0].tolist()}))
+                      "drafter_best_scores": draft_scores[:, 0].tolist(), "drafter_best_tokens": draft_history[:, 0].tolist(),
+                      "token_loss_first": token_losses[0], "token_loss_last": token_losses[-1], "text_logprob": logprob, "text_entropy": entropy,
+                      "text_among_top": among_top}))
 
 
 if __name__ == "__main__":

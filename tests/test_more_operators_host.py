@@ -58,6 +58,8 @@ def test_logprobs_refusals(rdk, which):
         assert call(dx=0) == NULL and call(ldd=999) == SHAPE and call(dx=0x900004) == ALIGN
         assert call(dx=0x100000, ldd=1008) == SHAPE                     # x itself, but other strides
         assert call(dx=0x100010) == SHAPE                               # overlaps x
+        assert call(B=1 << 22, dx=1 << 50) == UNSUPPORTED               # more workgroups than a launch has
+        assert call(B=1 << 20, N=1 << 18, ldx=1 << 18, ldd=1 << 18, dx=1 << 50) == UNSUPPORTED
     if which == "grad":
         assert call(stats=0) == NULL
 
@@ -71,7 +73,7 @@ def test_logprobs_workspace(rdk):
     assert L.rdk_logprobs_workspace_bytes(None, 2, ctypes.byref(need)) == NULL
     assert L.rdk_logprobs_workspace_bytes(ctypes.byref(d), 5, ctypes.byref(need)) == DTYPE
     for B in (1, 8, 1000, (1 << 24) - 1):                               # no size overflows
-        big = rdk.LogprobsDesc(B=B, N=1 << 30, C=16, k=128, temperature=1.0)
+        big = rdk.LogprobsDesc(B=B, N=1 << 30, C=16, k=0, temperature=1.0)
         assert L.rdk_logprobs_workspace_bytes(ctypes.byref(big), 2, ctypes.byref(need)) == 0 and need.value >= 16 * B
 
 
@@ -92,7 +94,7 @@ def test_embed_refusals(rdk, which):
     for kw in ({"B": 0}, {"V": 0}, {"d": 0}, {"d": -1}, {"scale": float("inf")}, {"scale": float("nan")}, {"ldt": 63}, {"ldo": 63}, {"ldt": 1 << 40},
                {"table": 0x300000 - 64}, {"rows": 0x200010}):
         assert call(**kw) == SHAPE, kw
-    assert call(B=1 << 24) == UNSUPPORTED and call(V=(1 << 29) + 1) == UNSUPPORTED and call(d=(1 << 24) + 1) == UNSUPPORTED
+    assert call(B=1 << 24) == UNSUPPORTED and call(V=(1 << 29) + 1) == UNSUPPORTED and call(d=(1 << 20) + 1, ldt=1 << 21, ldo=1 << 21) == UNSUPPORTED
     for kw in ({"tt": 0}, {"tt": 3}, {"rt": 0}, {"rt": -1}):
         assert call(**kw) == DTYPE, kw
     for name in ("ids", "table", "rows") + (("ws",) if which == "grad" else ()):
