@@ -152,7 +152,11 @@ struct TokenShared {
 template <int KIND>
 __device__ __forceinline__ float log_share(float x, float m, float log_all, float inv_t)
 {
-    if (KIND == RDK_PROB_F32) return x > 0.f ? logf(x / m) - log_all : x == 0.f ? -INFINITY : x;
+    if (KIND == RDK_PROB_F32) {
+        if (!(x > 0.f)) return x == 0.f ? -INFINITY : x;
+        // (the ratio of weights that far apart may be no normal number, which has fewer bits)
+        return (x < m * 0x1p-100f ? logf(x * 0x1p64f) - (logf(m) + 64.f * kLn2) : logf(x / m)) - log_all;
+    }
     return x == -INFINITY ? -INFINITY : (x - m) * inv_t - log_all;
 }
 

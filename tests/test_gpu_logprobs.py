@@ -4,11 +4,15 @@ Tolerances.  With d = (x - M) / T, Z' = sum of exp(d) over all but the largest, 
 1 / T and log2(e) / T, and in their product: 2^-22 |d| in all; the exponential itself and d in U add 2^-22.  Terms that lie 20 below the largest of the others come to
 nothing beside it, so Z' and U are off by the relative D = 2^-22 (D1 + 20) + A 2^-24, D1 the distance of the second largest entry (0 for ties), A the
 additions that a term goes through: at most one for each of 8 entries, vectors of a lane (n / 2048 of bf16, n / 1024 of fp32) and 20 to bring lanes and parts together.
+The distances in U are first taken to a reference that a lane's largest value, in units of log 2, lies at most 8.5 above, and are brought to the largest value after
+the sums: |d| <= (distance) + 8.5 log 2, so that U is off by D (|U| + 6 Z') (where nearly all entries tie, U comes to much less than Z').
   log probability:  2^-22 |d| (its own distance) + D Z' / (1 + Z') + 2^-23 of it
-  entropy:          D (Z' / (1 + Z') + 2 |U| / (1 + Z')) + 2^-23 of it
+  entropy:          D (7 Z' / (1 + Z') + 2 |U| / (1 + Z')) + 2^-23 of it
   s:                the relative S = 2^-22 (|d| + 1) + D Z' / (1 + Z')
-  gradient:         1/T (s S (|G| + |h| (|d| + |u|)) + s |h| (2^-22 |d| + D |u|) + 2^-20 sum |g| at the tokens), u = U / (1 + Z'), 2^-22 of it, and where it is
-                    rounded to bf16 half a step, 2^-8 of it.  At a token that is the largest entry, alone: |g| Z' / (1 + Z') D in the place of 2^-20 |g|."""
+  gradient:         1/T (s S (|G| + |h| (|d| + |u|)) + s |h| (2^-22 |d| + D (|u| + 6 Z' / (1 + Z'))) + s 2^-20 sum |g| + 2^-20 sum |g| at the tokens), u = U / (1 + Z'), 2^-22 of it,
+                    and where it is rounded to bf16 half a step, 2^-8 of it.  (G is a sum of up to 16 numbers, off by 16 2^-24 sum |g|, however small it is.
+                    The exponential of the hardware gives 0 where the result is below 2^-126: s there is off by that, in units of 1 / (1 + Z'), Z' by n 2^-126, and U by 104 times that: beyond a
+                    distance of 104 it is less than 2^-149 of anything.)  At a token that is the largest entry, alone: |g| Z' / (1 + Z') D in the place of 2^-20 |g|."""
 import math
 
 import pytest
@@ -54,8 +58,8 @@ def reference(x, tokens, kind, T=1.0, slots=None, g=None, h=None):
     lp = torch.where(masked[:, None], torch.full_like(dt, -INF), dt - torch.log1p(rest)[:, None])
     lp = torch.where(tokens == -2, torch.zeros_like(lp), torch.where(tokens == -1, torch.full_like(lp, -INF), lp))
     dfin = lambda a: torch.where(torch.isfinite(a), a, torch.zeros_like(a)).abs()  # noqa: E731
-    tol_lp = 2.0 ** -22 * dfin(dt) + (D * share)[:, None] + 2.0 ** -23 * dfin(lp) + 1e-38
-    tol_h = D * (share + 2 * u.abs()) + 2.0 ** -23 * entropy.abs() + 1e-38
+    tol_lp = 2.0 ** -22 * dfin(dt) + (D * share)[:, None] + 2.0 ** -23 * dfin(lp) + n * 2.0 ** -126
+    tol_h = D * (7 * share + 2 * u.abs()) + 2.0 ** -23 * entropy.abs() + 105 * n * 2.0 ** -126
     v = torch.gather(x64, 1, at)
     place = torch.arange(n, device=x.device)
     ranks = torch.stack([(x64 > v[:, c:c + 1]).sum(1) + ((x64 == v[:, c:c + 1]) & (place < at[:, c:c + 1])).sum(1) for c in range(tokens.shape[1])], 1)
@@ -72,15 +76,19 @@ def reference(x, tokens, kind, T=1.0, slots=None, g=None, h=None):
     factor = G + h64[:, None] * (dd - u[:, None])
     dx = -s * factor
     S = 2.0 ** -22 * (dd.abs() + 1) + (D * share)[:, None]
-    tol = s * S * (G.abs() + h64[:, None].abs() * (dd.abs() + u[:, None].abs())) + s * h64[:, None].abs() * (2.0 ** -22 * dd.abs() + (D * u.abs())[:, None])
+    tol = s * S * (G.abs() + h64[:, None].abs() * (dd.abs() + u[:, None].abs())) + s * h64[:, None].abs() * (2.0 ** -22 * dd.abs() + (D * (u.abs() + 6 * share))[:, None])
     # at the tokens; of a sure row 1 - s = Z' / (1 + Z') is formed without a difference, here too
     add = torch.zeros_like(dx).scatter_add_(1, at, g64)
     met = torch.zeros_like(dx).scatter_add_(1, at, (tokens >= 0).double()) > 0
     largest = met & (d == 0)
     dx = torch.where(largest, (add - G) + (G * share[:, None] + h64[:, None] * u[:, None] / all_[:, None]), dx + add)
     total = g64.abs().sum(1, keepdim=True)
+    tol = tol + s * 2.0 ** -20 * total
+    far = torch.where(torch.isfinite(d), d, 0.0).abs().clamp(max=200.0)
+    tol = tol + 2.0 ** -126 / all_[:, None] * (G.abs() + h64[:, None].abs() * (far + u[:, None].abs()))
     alone = largest & (add == G) & (g64.ne(0).sum(1, keepdim=True) == 1)
-    tol = torch.where(alone, (D * share)[:, None] * total + h64[:, None].abs() * (D * u.abs())[:, None] * 3 / all_[:, None], tol + met * 2.0 ** -20 * total)
+    tol = torch.where(alone, (D * share)[:, None] * total + h64[:, None].abs() * (D * (u.abs() * 3 + 6 * share))[:, None] / all_[:, None], tol + met * 2.0 ** -20 * total)
+    tol = tol + n * 2.0 ** -126 * (G.abs() + 105 * h64[:, None].abs())       # of Z' and U
     dx, tol = dx / T, tol / T
     tol = tol + dx.abs() * (2.0 ** -22 + (2.0 ** -8 if x.dtype == torch.bfloat16 else 0.0)) + 1e-38
     out["dx"], out["tol_dx"] = torch.where(live[:, None], dx, torch.zeros_like(dx)), torch.where(live[:, None], tol, torch.zeros_like(tol))
@@ -481,3 +489,27 @@ def test_far_rows():
     near(o.logprob[-3:], ref["logprob"], ref["tol_lp"], "logprob")
     near(x[-3:], ref["dx"], ref["tol_dx"], "gradient")
     assert (o.logprob[:-3] + math.log(N)).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("sigma", [40.0, 80.0])
+def test_weights_far_apart(sigma):
+    """Weights that are next to nothing beside the largest, whose ratios to it are no normal numbers."""
+    for B, N in ((3, 1000), (2, 50001)):
+        x, gen = rows("prob", B, N, N, None, sigma)
+        tokens = torch.randint(0, N, (B, 16), generator=gen, device="cuda", dtype=torch.int32)
+        tokens[:, 0] = torch.where(x >= 2.0 ** -126, x, 2.0).argmin(1).to(torch.int32)
+        check_forward(x, tokens, "prob", 1.0, min(N, 128))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_rows_of_ties(kind):
+    """Few values, far from 0, that many entries have: of entropy gradients alone and with others."""
+    for B, N, step in ((33, 33703, 16.0), (5, 513, 0.25)):
+        x, gen = rows(kind, B, N, N, None, 10.0)
+        x.copy_((x / step).round() * step + 3008.0)
+        tokens = some_tokens(B, N, 1, gen)
+        tokens[::2, 0] = x[::2].float().argmax(1).to(torch.int32)
+        g, h = torch.randn((B, 1), generator=gen, device="cuda"), torch.randn(B, generator=gen, device="cuda")
+        g[::4] = 0
+        check_forward(x, tokens, kind, 0.3)
+        check_gradients(x, tokens, kind, 0.3, g, h)
