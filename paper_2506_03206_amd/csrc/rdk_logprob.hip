@@ -390,18 +390,23 @@ GradArgs grad_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, Row
 }
 
 template <int KIND, int THREADS>
-void launch_parts(const LogprobArgs &a, int32_t B, hipStream_t st)
+rdk_status_t launch_parts(const LogprobArgs &a, int32_t B, hipStream_t st)
 {
     const dim3 grid((unsigned)B * a.parts), block(THREADS);
-    if (a.t.rank) RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, true>), grid, block, 0, st, a);
+    if (a.t.rank && THREADS * kMaxTokens * 4 >= 65536) {
+        static LdsGrant grant;
+        if (const rdk_status_t rc = grant((const void *)logprob_part_kernel<KIND, THREADS, true>, THREADS * kMaxTokens * 4)) return rc;
+    }
+    if (a.t.rank) RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, true>), grid, block, before_tokens_bytes(a.t, THREADS), st, a);
     else RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, false>), grid, block, 0, st, a);
+    return RDK_OK;
 }
 
 template <int KIND>
 rdk_status_t launch_rows(const LogprobArgs &a, int32_t B, hipStream_t st)
 {
-    if (a.threads == kThreads) launch_parts<KIND, kThreads>(a, B, st);
-    else launch_parts<KIND, 1024>(a, B, st);
+    const rdk_status_t rc = a.threads == kThreads ? launch_parts<KIND, kThreads>(a, B, st) : launch_parts<KIND, 1024>(a, B, st);
+    if (rc) return rc;
     if (a.parts > 1) RDK_TIMED_LAUNCH("logprob_finish_kernel", (logprob_finish_kernel<KIND>), dim3((unsigned)B), dim3(kWave), 0, st, a);
     RDK_LAUNCH_CHECK("logprob_part_kernel");
     return RDK_OK;

@@ -148,6 +148,16 @@ struct TokenShared {
     int rank[kWaves][kMaxTokens];
 };
 
+// Entries before a token of a thread's own vectors, [token][thread]: a word that only this thread reads and writes.  Of as many tokens as there are, so that
+// workgroups of few tokens lie beside each other (16 always: four fused passes a unit become three, 1024 rows of 151936 bf16 logits 72 -> 77 us).
+template <int THREADS>
+__device__ __forceinline__ uint32_t &before_token(int c)
+{
+    extern __shared__ uint32_t before[];
+    return before[c * THREADS + (int)threadIdx.x];
+}
+inline uint32_t before_tokens_bytes(const TokenArgs &a, int threads) { return a.rank ? (uint32_t)(a.C * threads * 4) : 0; }
+
 // log probability of an entry x of a row with the largest value m, log_all = log(1 + rest)
 template <int KIND>
 __device__ __forceinline__ float log_share(float x, float m, float log_all, float inv_t)
@@ -215,7 +225,9 @@ struct TokenPass {
         s.clear();
         place = kNoToken;
         here = count = 0;
-        value = no_value<KIND>();
+        value = NAN;   // (nothing is before none)
+        if (RANKS && a.rank)
+            for (int c = 0; c < a.C; ++c) before_token<THREADS>(c) = 0;
         if (lane_id() < a.C) place = place_of(a.tokens[row * a.C + lane_id()], a.slot_of, a.ids);
         if (place >= 0) {
             here = place - first;
@@ -261,45 +273,61 @@ struct TokenPass {
 
     // Entries of a round before the tokens; its vectors begin with `base` of the part, most is the lane's largest value of the round.  In vectors before a
     // token's own the entries that equal it count too.  Nothing waits for the mask of a comparison: pairs of bf16 values are taken as signed whole numbers,
-    // of which those below 0 have their order turned round with all others (`turn`), and counted in 16 bits each; fp32 values by the sign of a difference.
+    // of which those below 0 have their order turned round with all others (`turn`), and counted in 16 bits each; of fp32 values the signs of differences are
+    // gathered.  A thread's counts are its own until the end.  Bounds are a wavefront's in all rounds but the one that the token lies in.
     __device__ __forceinline__ void ranks(const TokenArgs &a, u32x4 (&now)[kTokenRoundVecs], float most, int base)
     {
-        const int own = base + (int)threadIdx.x;
 #pragma unroll 1
         for (int c = 0; c < a.C; ++c) {
-            const int first = lane_value(here, c) >> (V::kLen == 8 ? 3 : 2);   // (-1 or less: it lies before the part)
             const float v = lane_value(value, c);
-            if (lane_value(place, c) < 0 || __ballot(most >= v) == 0) continue;
+            if (__ballot(most >= v) == 0) continue;
+            const int first = lane_value(here, c) >> (V::kLen == 8 ? 3 : 2);   // (-1 or less: it lies before the part)
 #pragma unroll
             for (int j = 0; j < kTokenRoundVecs; ++j) V::again(now[j]);   // (or what is made of them for every token alike would be kept beside them)
+            const bool all_before = first >= base + kTokenRoundVecs * THREADS, none_before = first <= base;
             uint32_t n = 0;
             if constexpr (KIND == RDK_LOGIT_BF16) {
                 // above v: turned if v < 0;  at least v: turned if v <= 0, as -0 is the next below 0 in that order and equals it
                 const uint32_t half = __float_as_uint(v + 0.f) >> 16;
-                const uint32_t turn_above = v < 0.f ? 0x7FFFu : 0u, turn_least = v <= 0.f ? 0x7FFFu : 0u;
-                const uint32_t above = half ^ turn_above, least = v == 0.f ? 0xFFFEu : ((half ^ turn_least) - 1u) & 0xFFFFu;
+                const uint32_t turn_above = v < 0.f ? 0x7FFF7FFFu : 0u, turn_least = v <= 0.f ? 0x7FFF7FFFu : 0u;
+                const uint32_t above = (half ^ (turn_above & 0xFFFFu)) * 0x10001u;
+                const uint32_t least = (v == 0.f ? 0xFFFEu : ((half ^ (turn_least & 0xFFFFu)) - 1u) & 0xFFFFu) * 0x10001u;
                 s16x2 counts = {0, 0};
+                auto take = [&](u32x4 x, uint32_t bound, uint32_t turn) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < kTokenRoundVecs; ++j) {
-                    const bool before = own + j * THREADS < first;
-                    const s16x2 bound = s16x2_of(before ? least * 0x10001u : above * 0x10001u);
-                    const uint32_t turn = before ? turn_least * 0x10001u : turn_above * 0x10001u;
+                    for (int i = 0; i < 4; ++i) counts -= __builtin_elementwise_sub_sat(s16x2_of(bound), s16x2_of(x[i] ^ turn)) >> 15;
+                };
+                if (all_before || none_before) {
+                    const uint32_t bound = all_before ? least : above, turn = all_before ? turn_least : turn_above;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) counts -= __builtin_elementwise_sub_sat(bound, s16x2_of(now[j][i] ^ turn)) >> 15;
+                    for (int j = 0; j < kTokenRoundVecs; ++j) take(now[j], bound, turn);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kTokenRoundVecs; ++j) {
+                        const bool before = base + j * THREADS + (int)threadIdx.x < first;
+                        take(now[j], before ? least : above, before ? turn_least : turn_above);
+                    }
                 }
                 n = __builtin_bit_cast(uint32_t, counts);
                 n = (n & 0xFFFFu) + (n >> 16);
             } else {
                 const float above = v + 0.f, least = lane_value(below(value), c);   // (0 - 0 has no sign, -0 - 0 has)
+                auto take = [&](u32x4 x, float bound) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < kTokenRoundVecs; ++j) {
-                    const float bound = own + j * THREADS < first ? least : above;
+                    for (int i = 0; i < 4; ++i) n = __builtin_amdgcn_alignbit(n, __float_as_uint(bound - __uint_as_float(x[i])), 31);
+                };
+                static_assert(V::kLen * kTokenRoundVecs <= 32, "a bit each");
+                if (all_before || none_before) {
+                    const float bound = all_before ? least : above;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) n += __float_as_uint(bound - __uint_as_float(now[j][i])) >> 31;
+                    for (int j = 0; j < kTokenRoundVecs; ++j) take(now[j], bound);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kTokenRoundVecs; ++j) take(now[j], base + j * THREADS + (int)threadIdx.x < first ? least : above);
                 }
+                n = __popc(n);
             }
-            const int all = wave_count((int)n);
-            if (lane_id() == c) count += all;
+            __hip_atomic_fetch_add(&before_token<THREADS>(c), n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
         }
     }
 
@@ -321,7 +349,19 @@ struct TokenPass {
             sh.wave[wid].sum_besides = sum_b;
             sh.wave[wid].pull_besides = pull_b;
         }
-        if (RANKS && lane_id() < a.C) sh.rank[wid][lane_id()] = count;
+        if (RANKS) {
+            for (int c = 0; a.rank && c < a.C; c += 4) {   // four at a time on their way
+                int own[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) own[i] = (int)before_token<THREADS>(min(c + i, a.C - 1));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int all = wave_count(own[i]);
+                    if (lane_id() == c + i) count += all;
+                }
+            }
+            if (lane_id() < a.C) sh.rank[wid][lane_id()] = count;
+        }
         __syncthreads();
         float m = sh.wave[0].m;
         int holds = 0;   // the first wavefront that has the largest value

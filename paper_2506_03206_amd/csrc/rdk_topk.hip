@@ -819,7 +819,8 @@ rdk_status_t launch_logprobs_top(const rdk_logprobs_desc_t &d, RowInput x, Token
     }
     with_kind(x.kind, [&](auto kind) {
         constexpr int KIND = decltype(kind)::value;
-        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<KIND, true>), dim3((unsigned)d.B * parts), dim3(kTopThreads), 0, st, a, t);
+        RDK_TIMED_LAUNCH("topk_part_kernel", (topk_part_kernel<KIND, true>), dim3((unsigned)d.B * parts), dim3(kTopThreads),
+                         before_tokens_bytes(t, kTopThreads), st, a, t);
         if (parts > 1) {
             const TopMergeArgs m{x.ptr, x.ld, a.entries, nullptr, d.k, parts, a.inv_t, a.c, top_ids, top_logprobs, nullptr};
             if (parts * d.k <= 4 * kTopThreads)

@@ -513,3 +513,17 @@ def test_rows_of_ties(kind):
         g[::4] = 0
         check_forward(x, tokens, kind, 0.3)
         check_gradients(x, tokens, kind, 0.3, g, h)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32", "prob"])
+def test_many_tokens_of_many_rows(kind):
+    """Sixteen tokens of rows that one large workgroup reads each, the same token among them, tokens that lie side by side and at both ends."""
+    for B, N in ((200, 20003), (130, 8193)):
+        x, gen = rows(kind, B, N, N)
+        tokens = some_tokens(B, N, 16, gen)
+        tokens[:, 1] = 0
+        tokens[:, 2] = N - 1
+        tokens[:, 3] = (tokens[:, 0] + 1).clamp(max=N - 1)
+        tokens[::3, 5] = -1
+        tokens[1::3, 6] = N
+        check_forward(x, tokens, kind)
