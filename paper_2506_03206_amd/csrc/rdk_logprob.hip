@@ -13,36 +13,39 @@ constexpr float kLog2e = 1.44269504088896341f;
 struct LogprobArgs {
     const void *x;
     int64_t ldx;
-    int n, parts, part_len, threads;
+    int n, parts, part_len;
     TokenArgs t;
 };
 
-// One pass over a part of a row.
-template <int KIND, int THREADS, bool RANKS>
-__global__ __launch_bounds__(THREADS) void logprob_part_kernel(LogprobArgs a)
+// One pass over a part of a row; what it sums and counts, and why in that form, stands at TokenPass.  Two rounds of four vectors a thread in turn, one at work
+// and one on its way.  Without tokens' ranks it is bound by HBM and by the vector unit in about equal parts (an entry takes some 8 lane operations, an exponential
+// of a quarter rate among them): 1024 bf16 rows of 151936 58.5 us = 5.3 TB/s, 2048 fp32 rows of 32064 48 us = 5.5 TB/s; with a token's rank 62.5 and 50.5, and every
+// further token 11.5 us (bf16, 155 million entries).  Rows that are all on the chip at once are a chain: loads, sums, two meetings of the wavefronts.
+template <int KIND, bool RANKS>
+__global__ __launch_bounds__(kThreads) void logprob_part_kernel(LogprobArgs a)
 {
     typedef Vec<KIND> V;
-    constexpr int kRoundVecs = kTokenRoundVecs, kRound = THREADS * kRoundVecs;   // vectors
-    __shared__ TokenShared<THREADS> sh;
+    constexpr int kRoundVecs = kTokenRoundVecs, kRound = kThreads * kRoundVecs;   // vectors
+    __shared__ TokenShared<kThreads> sh;
     const int64_t row = blockIdx.x / a.parts;
     const int part = blockIdx.x % a.parts, begin = part * a.part_len, end = max(begin, min(a.n, begin + a.part_len));
     const int tid = threadIdx.x, wid = tid / kWave;
     const void *xr = row_ptr<KIND>(a.x, a.ldx, row);
     const char *from = (const char *)xr + (int64_t)begin * V::kSize;
     const int whole = (end - begin) / V::kLen, behind = (end - begin) % V::kLen;
-    TokenPass<KIND, THREADS, RANKS> pass;
+    TokenPass<KIND, kThreads, RANKS> pass;
     // Always as many loads, of the last vector where the round has none of its own: the compiler counts loads in flight, and would wait for all of
     // them behind a branch that has some of its own.
     auto load_round = [&](u32x4 (&raw)[kRoundVecs], int base) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < kRoundVecs; ++j)
-            raw[j] = *(const u32x4_any *)(from + (uint64_t)(uint32_t)min(base + j * THREADS + tid, whole - 1) * 16);
+            raw[j] = *(const u32x4_any *)(from + (uint64_t)(uint32_t)min(base + j * kThreads + tid, whole - 1) * 16);
     };
     auto take_round = [&](u32x4 (&now)[kRoundVecs], int base) __attribute__((always_inline)) {
         if (base + kRound > whole) {
 #pragma unroll
             for (int j = 0; j < kRoundVecs; ++j)
-                if (base + j * THREADS + tid >= whole) now[j] = V::fill();
+                if (base + j * kThreads + tid >= whole) now[j] = V::fill();
         }
         float vm[kRoundVecs];
 #pragma unroll
@@ -165,7 +168,9 @@ struct RowGrad {
     }
 };
 
-// The gradient of a part of a row, from the statistics that the forward call left.
+// The gradient of a part of a row, from the statistics that the forward call left.  One exponential and two or three products an entry, nothing to meet for: HBM
+// (2048 fp32 rows of 32064 95 us = 5.5 TB/s read and written), or the last-level cache where the logits still lie there (1024 bf16 rows of 16384 9.6-11.7 us = 5.7 TB/s
+// and above).  Rows of which nothing is asked are set to 0 without being read.
 template <int KIND, int VECS>
 __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a)
 {
@@ -208,16 +213,18 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a)
     }
 }
 
-// Forward and backward of a row that lies in the registers of one workgroup: read once.  With eight vectors a thread the exponentials are kept for the
-// gradient, with more they are formed again.
-template <int KIND, int THREADS, int VECS>
+// Forward and backward of a row that lies in the registers of one workgroup, or forward alone (GRAD, RANKS: which): read once.  The largest value is known before the first exponential, so sums need no
+// second reference and what the largest leaves out is left out at once.  With two vectors a thread the exponentials are kept for the gradient; with more they are formed
+// again, because registers decide how many rows lie beside each other (2048 bf16 rows of 32064, 512 threads of eight vectors: 55 us with 5 wavefronts a SIMD unit, 60 with
+// 6, which spill, 67 with exponentials kept).  HBM: 2048 rows of 32064 52.5 us = 5.0 TB/s read and written, fp32 97 us = 5.4 TB/s.
+template <int KIND, int THREADS, int VECS, bool GRAD, bool RANKS>
 __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel(LogprobArgs a, GradArgs b)
 {
     typedef Vec<KIND> V;
     constexpr int kW = THREADS / kWave;
-    constexpr bool kKeep = VECS <= 2;
+    constexpr bool kKeep = GRAD && VECS <= 2;
     __shared__ float wave_m[kW], wave_rest[kW], wave_pull[kW];
-    __shared__ int wave_ties[kW];
+    __shared__ int wave_ties[kW], wave_rank[RANKS ? kW : 1][kMaxTokens];
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, wid = tid / kWave;
     const char *from = (const char *)row_ptr<KIND>(a.x, a.ldx, row);
@@ -229,20 +236,27 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         for (int j = 0; j < VECS; ++j) raw[j] = *(const u32x4_any *)(from + (uint32_t)min(j * THREADS + tid, whole - 1) * 16u);
     }
     if (behind > 0 && tid == last_tid) last = V::load_at(from, (uint32_t)whole * 16u, behind);
-    const float h = b.above_entropy ? b.above_entropy[row] : 0.f;
-    int place = kNoToken;
-    float g = 0.f, value = -INFINITY;
-    if (lane_id() < b.C) {
-        place = place_of(b.tokens[row * b.C + lane_id()], b.slot_of, b.ids);
+    const float h = GRAD && b.above_entropy ? b.above_entropy[row] : 0.f;
+    int place = kNoToken, count = 0;
+    float g = 0.f, value = RANKS ? NAN : -INFINITY;   // (nothing is before none)
+    if (lane_id() < a.t.C) {
+        place = place_of(a.t.tokens[row * a.t.C + lane_id()], a.t.slot_of, a.t.ids);
         if (place >= 0) {
             value = load1<KIND>(from, place);
-            if (b.above) g = b.above[row * b.C + lane_id()];
+            if (GRAD && b.above) g = b.above[row * a.t.C + lane_id()];
+            if (RANKS && wid == 0) {   // entries of its own vector that equal it and lie before it
+                const int own = place & ~(V::kLen - 1);
+                float v[V::kLen];
+                V::to(V::load(from, own, a.n), v);
+#pragma unroll
+                for (int e = 0; e < V::kLen - 1; ++e) count += (own + e < place) & (v[e] == value);
+            }
         }
     }
 #pragma unroll
     for (int j = 0; j < VECS; ++j)
         if (j * THREADS + tid >= whole) raw[j] = j == last_vec ? last : V::fill();   // (fill but for one thread)
-    float m = -INFINITY;
+    float m = no_value<KIND>();
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
         float v[V::kLen];
@@ -253,15 +267,28 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
     }
     const float own = wave_max(m);
     if (lane_id() == 0) wave_m[wid] = own;
-    asm volatile("" ::"v"(value));   // it is there before another wavefront writes over it (dx may be x)
+    if (GRAD) asm volatile("" ::"v"(value));   // it is there before another wavefront writes over it (dx may be x)
     __syncthreads();
     m = wave_m[0];
 #pragma unroll
     for (int w = 1; w < kW; ++w) m = fmaxf(m, wave_m[w]);
     const float ref = weight_reference(m);
+    // of weights: a power of two that keeps them from overflowing and from having few bits, and the largest's reciprocal beside it
+    const float scale = KIND == RDK_PROB_F32 ? power_of_two(-weight_exponent(m)) : 1.f, inv = KIND == RDK_PROB_F32 ? m > 0.f ? 1.f / (m * scale) : 0.f : 1.f;
+    // an entry relative to the largest value, and its distance from it: over T, in units of log 2 for weights
+    auto term = [&](float v, float &d) __attribute__((always_inline)) {
+        if constexpr (KIND == RDK_PROB_F32) {
+            const float x = v * scale * inv;
+            d = __builtin_amdgcn_logf(fmaxf(x, 0x1p-126f));
+            return x;
+        } else {
+            d = v - ref;
+            return __builtin_amdgcn_exp2f(d * a.t.c);
+        }
+    };
     float rest = 0.f, pull = 0.f, terms[kKeep ? VECS : 1][V::kLen];
     int ties = 0;
-    const bool holds = own == m && m > -INFINITY;   // a wavefront that holds the largest value: that is left out
+    const bool holds = own == m && m > no_value<KIND>();   // a wavefront that holds the largest value: that is left out
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
         float v[V::kLen], s = 0.f, p = 0.f;
@@ -269,28 +296,33 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         V::again(raw[j]);
 #pragma unroll
         for (int e = 0; e < V::kLen; ++e) {
-            const float d = v[e] - ref, x = __builtin_amdgcn_exp2f(d * b.c);
+            float d;
+            const float x = term(v[e], d);
             if constexpr (kKeep) terms[j][e] = x;
             s += x;
             p = fmaf(x, d, p);
         }
-        if (p != p) {   // 0 times the distance of a masked entry: such distances are held finite.  (NaN is in the sum.)
+        if (KIND != RDK_PROB_F32 && p != p) {   // 0 times the distance of a masked entry: such distances are held finite.  (NaN is in the sum.)
             p = 0.f;
 #pragma unroll
             for (int e = 0; e < V::kLen; ++e) {
-                const float d = v[e] - ref;
-                p = fmaf(__builtin_amdgcn_exp2f(d * b.c), fmaxf(d, -0x1p126f), p);
+                float d;
+                const float x = term(v[e], d);
+                p = fmaf(x, fmaxf(d, -0x1p126f), p);
             }
         }
         if (holds) {
-            float most = V::largest(v, -INFINITY);
-            if (__ballot(most == m)) {
+            float most = V::largest(v, no_value<KIND>());
+            if (__ballot(most == m)) {   // (of a logit the distance is 0; of a weight a product that may be rounded, so it is left out of both)
                 s = 0.f;
+                if (KIND == RDK_PROB_F32) p = 0.f;
 #pragma unroll
                 for (int e = 0; e < V::kLen; ++e) {
-                    const float x = __builtin_amdgcn_exp2f((v[e] - ref) * b.c);
+                    float d;
+                    const float x = term(v[e], d);
                     ties += __popcll(__ballot(v[e] == m));
                     s += v[e] == m ? 0.f : x;
+                    if (KIND == RDK_PROB_F32) p = v[e] == m ? p : fmaf(x, d, p);
                 }
             }
         }
@@ -305,6 +337,16 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         wave_pull[wid] = pull;
         wave_ties[wid] = ties;
     }
+    if constexpr (RANKS) {
+#pragma unroll 1
+        for (int c = 0; c < a.t.C; ++c) {
+            const float v = lane_value(value, c);
+            if (!(own >= v)) continue;   // (alike for the wavefront)
+            const int all = wave_count((int)entries_before<KIND, THREADS>(raw, 0, lane_value(place, c) / V::kLen, v));
+            if (lane_id() == c) count += all;
+        }
+        if (lane_id() < a.t.C) wave_rank[wid][lane_id()] = count;
+    }
     __syncthreads();
     rest = pull = 0.f;
     ties = 0;
@@ -314,11 +356,17 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         pull += wave_pull[w];
         ties += wave_ties[w];
     }
-    const bool some = m > -INFINITY && m < INFINITY;
+    const bool some = m > no_value<KIND>() && m < INFINITY;
     rest = some ? rest + (float)(ties - 1) : m > 0.f ? NAN : rest - rest;   // (an infinity; NaN where there is one, 0 where all is masked)
-    pull = some ? pull * b.inv_t : 0.f;
+    pull = some ? pull * (KIND == RDK_PROB_F32 ? kLn2 : a.t.inv_t) : 0.f;
     const float4 st = make_float4(m, rest, pull / (1.f + rest), 0.f);
-    if (wid == 0) write_tokens<KIND>(a.t, row, RowSum{m, rest, pull}, place, value, 0);
+    if (wid == 0) {
+        if (RANKS && lane_id() < a.t.C)
+#pragma unroll
+            for (int w = 1; w < kW; ++w) count += wave_rank[w][lane_id()];
+        write_tokens<KIND>(a.t, row, RowSum{m, rest, pull}, place, value, count);
+    }
+    if constexpr (GRAD) {
     char *to = (char *)const_cast<void *>(row_ptr<KIND>(b.dx, b.ldd, row));
     const bool masked = m == -INFINITY && rest == 0.f;
     if (masked || (h == 0.f && __ballot(g != 0.f) == 0)) {
@@ -344,21 +392,22 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         const u32x4 y = grad.template vector<KIND>(last, whole * V::kLen - (last_tid - tid) * V::kLen, C, place, g);
         if (tid == last_tid) V::store_at(to, (uint32_t)whole * 16u, behind, y);
     }
+    }
 }
 
+// Parts of a row: as many workgroups as fill the chip four times, each of a whole round at least.
 struct Parts {
-    int count, len, threads;
+    int count, len;
 };
 Parts parts_of(int64_t rows, int n, rdk_input_kind_t kind)
 {
-    if (rows >= 128 && rows < 512 && n > 4096) return Parts{1, (int)align_up((size_t)n, 64), 1024};
     const int round = kThreads * kTokenRoundVecs * (kind == RDK_LOGIT_BF16 ? 8 : 4);
     int want = (int)(1024 / rows);
     if (want > kMaxParts) want = kMaxParts;
-    if (want <= 1 || n <= 2 * round) return Parts{1, (int)align_up((size_t)n, 64), kThreads};
+    if (want <= 1 || n <= 2 * round) return Parts{1, (int)align_up((size_t)n, 64)};
     int64_t len = ((int64_t)n - 1) / want + 1;
     len = (int64_t)align_up((size_t)len, (size_t)(len > round ? round : round / 4));
-    return Parts{(int)((n - 1) / len) + 1, (int)len, kThreads};
+    return Parts{(int)((n - 1) / len) + 1, (int)len};
 }
 
 LogprobArgs arguments(const rdk_logprobs_desc_t &d, RowInput x, const TokenArgs &t, char *ws)
@@ -366,7 +415,7 @@ LogprobArgs arguments(const rdk_logprobs_desc_t &d, RowInput x, const TokenArgs 
     const Parts split = parts_of(d.B, d.N, x.kind);
     LogprobArgs a{};
     a.x = x.ptr; a.ldx = x.ld;
-    a.n = d.N; a.parts = split.count; a.part_len = split.len; a.threads = split.threads;
+    a.n = d.N; a.parts = split.count; a.part_len = split.len;
     a.t = t;
     token_places(a.t, ws, d.B, split.count);
     return a;
@@ -389,24 +438,12 @@ GradArgs grad_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, Row
     return a;
 }
 
-template <int KIND, int THREADS>
-rdk_status_t launch_parts(const LogprobArgs &a, int32_t B, hipStream_t st)
-{
-    const dim3 grid((unsigned)B * a.parts), block(THREADS);
-    if (a.t.rank && THREADS * kMaxTokens * 4 >= 65536) {
-        static LdsGrant grant;
-        if (const rdk_status_t rc = grant((const void *)logprob_part_kernel<KIND, THREADS, true>, THREADS * kMaxTokens * 4)) return rc;
-    }
-    if (a.t.rank) RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, true>), grid, block, before_tokens_bytes(a.t, THREADS), st, a);
-    else RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, THREADS, false>), grid, block, 0, st, a);
-    return RDK_OK;
-}
-
 template <int KIND>
 rdk_status_t launch_rows(const LogprobArgs &a, int32_t B, hipStream_t st)
 {
-    const rdk_status_t rc = a.threads == kThreads ? launch_parts<KIND, kThreads>(a, B, st) : launch_parts<KIND, 1024>(a, B, st);
-    if (rc) return rc;
+    const dim3 grid((unsigned)B * a.parts), block(kThreads);
+    if (a.t.rank) RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, true>), grid, block, before_tokens_bytes(a.t, kThreads), st, a);
+    else RDK_TIMED_LAUNCH("logprob_part_kernel", (logprob_part_kernel<KIND, false>), grid, block, 0, st, a);
     if (a.parts > 1) RDK_TIMED_LAUNCH("logprob_finish_kernel", (logprob_finish_kernel<KIND>), dim3((unsigned)B), dim3(kWave), 0, st, a);
     RDK_LAUNCH_CHECK("logprob_part_kernel");
     return RDK_OK;
@@ -416,27 +453,55 @@ template <int KIND>
 rdk_status_t launch_grad(GradArgs a, int32_t B, hipStream_t st)
 {
     a.parts = logprobs_grad_parts(a.n, (rdk_input_kind_t)KIND);
-    RDK_TIMED_LAUNCH("logprob_grad_kernel", (logprob_grad_kernel<KIND, kGradVecs>), dim3((unsigned)B * a.parts), dim3(kThreads), 0, st, a);
+    // (a thread asks for no more vectors than short rows have: 8192 bf16 rows of 4096 33.2 -> 21.8 us)
+    if (a.n <= kThreads * 2 * Vec<KIND>::kLen)
+        RDK_TIMED_LAUNCH("logprob_grad_kernel", (logprob_grad_kernel<KIND, 2>), dim3((unsigned)B), dim3(kThreads), 0, st, a);
+    else
+        RDK_TIMED_LAUNCH("logprob_grad_kernel", (logprob_grad_kernel<KIND, kGradVecs>), dim3((unsigned)B * a.parts), dim3(kThreads), 0, st, a);
     RDK_LAUNCH_CHECK("logprob_grad_kernel");
     return RDK_OK;
 }
 
-template <int KIND, int THREADS, int VECS>
+template <int KIND, int THREADS, int VECS, bool GRAD = true>
 rdk_status_t launch_row(const LogprobArgs &a, const GradArgs &b, int32_t B, hipStream_t st)
 {
-    RDK_TIMED_LAUNCH("logprob_row_kernel", (logprob_row_kernel<KIND, THREADS, VECS>), dim3((unsigned)B), dim3(THREADS), 0, st, a, b);
+    const dim3 grid((unsigned)B), block(THREADS);
+    if constexpr (GRAD) {
+        RDK_TIMED_LAUNCH("logprob_row_kernel", (logprob_row_kernel<KIND, THREADS, VECS, true, false>), grid, block, 0, st, a, b);
+    } else {
+        if (a.t.rank) RDK_TIMED_LAUNCH("logprob_row_kernel", (logprob_row_kernel<KIND, THREADS, VECS, false, true>), grid, block, 0, st, a, b);
+        else RDK_TIMED_LAUNCH("logprob_row_kernel", (logprob_row_kernel<KIND, THREADS, VECS, false, false>), grid, block, 0, st, a, b);
+    }
     RDK_LAUNCH_CHECK("logprob_row_kernel");
     return RDK_OK;
+}
+
+// The forward call.  Rows that the registers of a workgroup hold take one launch and one look at their largest value, which is known before the first exponential (with a
+// token's rank, in rounds or parts -> this way: 8192 bf16 rows of 4096 42.8 -> 21.0 us, 2048 of 1000 13.4 -> 7.1, 1024 of 16384 13.5 -> 12.7, 2048 of 32064 32.3 -> 30.9, 64 of
+// 32064 12.5 -> 6.5, 8192 fp32 rows of 2048 33.6 -> 16.2).  Weights take more registers: 512 rows of 16384 14.2 -> 10.2, 1024 16.2 -> 17.3 and so not.  1024 threads where a
+// row has a compute unit for itself (256 bf16 rows of 65536 16.0 -> 12.9, 512 21.2 -> 23.3; 256 rows of 32000 weights, 8 tokens 19.6 -> 14.8); a few rows of many tokens
+// are spread over more units instead, whose wavefronts have fewer ranks to count (one row of 65536, 8 tokens 11.8 us, 17.5 this way).
+template <int KIND>
+rdk_status_t launch_forward(const LogprobArgs &a, int32_t B, hipStream_t st)
+{
+    constexpr int kLen = Vec<KIND>::kLen;
+    const GradArgs none{};
+    if (a.n <= 256 * 2 * kLen) return launch_row<KIND, 256, 2, false>(a, none, B, st);
+    if (a.n <= 256 * 4 * kLen) return launch_row<KIND, 256, 4, false>(a, none, B, st);
+    if (a.n <= 256 * 8 * kLen) return launch_row<KIND, 256, 8, false>(a, none, B, st);
+    if (a.n <= 512 * 8 * kLen && (KIND != RDK_PROB_F32 || B <= 512)) return launch_row<KIND, 512, 8, false>(a, none, B, st);
+    if (a.n <= 1024 * 8 * kLen && B <= 256 && (B >= 32 || a.t.C <= 2)) return launch_row<KIND, 1024, 8, false>(a, none, B, st);
+    return launch_rows<KIND>(a, B, st);
 }
 
 template <int KIND>
 rdk_status_t launch_step(const LogprobArgs &a, const GradArgs &b, int32_t B, hipStream_t st)
 {
     constexpr int kLen = Vec<KIND>::kLen;
-    // Few long rows: several workgroups to a row, in two launches more (bf16: 16 rows of 128256 20.3 -> 15.9 us, 128 of 32064 8.4 in one launch, 512 of
+    // Few long rows: several workgroups to a row, in one launch or two more (bf16: 16 rows of 128256 20.3 -> 15.9 us, 128 of 32064 8.4 in one launch, 512 of
     // 128256 62 in one and 73 in three).
     if (a.parts > 1 && B < 128 && a.n > 512 * 8 * kLen) {
-        const rdk_status_t rc = launch_rows<KIND>(a, B, st);
+        const rdk_status_t rc = launch_forward<KIND>(a, B, st);
         return rc == RDK_OK ? launch_grad<KIND>(b, B, st) : rc;
     }
     if (a.n <= 256 * 2 * kLen) return launch_row<KIND, 256, 2>(a, b, B, st);
@@ -496,8 +561,8 @@ rdk_status_t launch_logprobs(const rdk_logprobs_desc_t &d, const KernelHandle *h
     const TokenArgs t = token_arguments(d, h, tokens, logprob, rank, entropy, (float4 *)stats);
     if (d.k > 0) return launch_logprobs_top(d, x, t, top_ids, top_logprobs, ws, st);
     const LogprobArgs a = arguments(d, x, t, (char *)ws);
-    if (x.kind == RDK_PROB_F32) return launch_rows<RDK_PROB_F32>(a, d.B, st);
-    return x.kind == RDK_LOGIT_F32 ? launch_rows<RDK_LOGIT_F32>(a, d.B, st) : launch_rows<RDK_LOGIT_BF16>(a, d.B, st);
+    if (x.kind == RDK_PROB_F32) return launch_forward<RDK_PROB_F32>(a, d.B, st);
+    return x.kind == RDK_LOGIT_F32 ? launch_forward<RDK_LOGIT_F32>(a, d.B, st) : launch_forward<RDK_LOGIT_BF16>(a, d.B, st);
 }
 
 rdk_status_t launch_logprobs_grad(const rdk_logprobs_desc_t &d, const KernelHandle *h, RowInput x, const int32_t *tokens, const float *stats,

@@ -47,13 +47,6 @@ __device__ __forceinline__ int place_of(int id, const int32_t *slot_of, int ids)
     return slot_of ? max(slot_of[id], kUnknown) : id;
 }
 
-// The largest number below x.  (Of -inf, of which nothing is asked, a NaN.)
-__device__ __forceinline__ float below(float x)
-{
-    const uint32_t b = __float_as_uint(x);
-    return __uint_as_float(x == 0.f ? 0x80000001u : b + (b >> 31 ? 1u : 0xFFFFFFFFu));
-}
-
 // A power of two by which weights up to m come to lie below 4, and its logarithm.  (Weights below 2^-126 stay below 1.)
 __device__ __forceinline__ int weight_exponent(float m) { return min(max((int)(__float_as_uint(m) >> 23) & 0xFF, 1) - 127, 126); }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
@@ -206,6 +199,68 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ s16x2 s16x2_of(uint32_t w) { return __builtin_bit_cast(s16x2, w); }
 __device__ __forceinline__ u16x2 u16x2_of(uint32_t w) { return __builtin_bit_cast(u16x2, w); }
 
+// Entries of a thread's vectors before a token of the value v that lies in the vector `first`; they begin with `base` and stand THREADS apart.  In vectors before a
+// token's own the entries that equal it count too.  Nothing waits for the mask of a comparison: pairs of bf16 values are taken as signed whole numbers, of which those
+// below 0 have their order turned round with all others (`turn`), and counted in 16 bits each; of fp32 values the signs of differences are gathered.  Bounds are a
+// wavefront's but where the token lies among the vectors.
+template <int KIND, int THREADS, int VECS>
+__device__ __forceinline__ uint32_t entries_before(u32x4 (&now)[VECS], int base, int first, float v)
+{
+    typedef Vec<KIND> V;
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) V::again(now[j]);   // (or what is made of them for every token alike would be kept beside them)
+    const bool all_before = first >= base + VECS * THREADS, none_before = first <= base;
+    uint32_t n = 0;
+    if constexpr (KIND == RDK_LOGIT_BF16) {
+        // above v: turned if v < 0;  at least v: turned if v <= 0, as -0 is the next below 0 in that order and equals it
+        const uint32_t half = __float_as_uint(v + 0.f) >> 16;
+        const uint32_t turn_above = v < 0.f ? 0x7FFF7FFFu : 0u, turn_least = v <= 0.f ? 0x7FFF7FFFu : 0u;
+        const uint32_t above = (half ^ (turn_above & 0xFFFFu)) * 0x10001u;
+        const uint32_t least = (v == 0.f ? 0xFFFEu : ((half ^ (turn_least & 0xFFFFu)) - 1u) & 0xFFFFu) * 0x10001u;
+        s16x2 counts = {0, 0};
+        auto take = [&](u32x4 x, uint32_t bound, uint32_t turn) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) counts -= __builtin_elementwise_sub_sat(s16x2_of(bound), s16x2_of(x[i] ^ turn)) >> 15;
+        };
+        if (all_before || none_before) {
+            const uint32_t bound = all_before ? least : above, turn = all_before ? turn_least : turn_above;
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) take(now[j], bound, turn);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) {
+                const bool before = base + j * THREADS + (int)threadIdx.x < first;
+                take(now[j], before ? least : above, before ? turn_least : turn_above);
+            }
+        }
+        n = __builtin_bit_cast(uint32_t, counts);
+        n = (n & 0xFFFFu) + (n >> 16);
+    } else {
+        // above v: v - x < 0;  at least v: not x - v < 0.  (No bound beside v, which below the lowest finite value would be -inf, and -inf - -inf no number.)
+        static_assert(V::kLen * VECS <= 32, "a bit each");
+        const float above = v + 0.f, least = 0.f - v;   // (0 - 0 has no sign, -0 - 0 has)
+        auto take = [&](u32x4 x, float factor, float bound, uint32_t turn) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n = __builtin_amdgcn_alignbit(n, __float_as_uint(fmaf(__uint_as_float(x[i]), factor, bound)), 31);
+            n ^= turn;
+        };
+        if (all_before || none_before) {
+            const float factor = all_before ? 1.f : -1.f, bound = all_before ? least : above;
+            const uint32_t turn = all_before ? 15u : 0u;
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) take(now[j], factor, bound, turn);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VECS; ++j) {
+                const bool before = base + j * THREADS + (int)threadIdx.x < first;
+                take(now[j], before ? 1.f : -1.f, before ? least : above, before ? 15u : 0u);
+            }
+        }
+        n = __popc(n);
+    }
+    return n;
+}
+
 // A part of a row read by a workgroup in rounds of four vectors a thread.  A lane's sums are relative to a value that it has seen; the lane that ends
 // with the largest of all has that entry's 1 in its sum, in whose rounding its other entries may be lost: where that matters (all others
 // together come to less than it) this lane's vectors are read again, out of the cache, a vector to a thread, and summed without it.  Entries before a token in the
@@ -271,10 +326,8 @@ struct TokenPass {
         return most;
     }
 
-    // Entries of a round before the tokens; its vectors begin with `base` of the part, most is the lane's largest value of the round.  In vectors before a
-    // token's own the entries that equal it count too.  Nothing waits for the mask of a comparison: pairs of bf16 values are taken as signed whole numbers,
-    // of which those below 0 have their order turned round with all others (`turn`), and counted in 16 bits each; of fp32 values the signs of differences are
-    // gathered.  A thread's counts are its own until the end.  Bounds are a wavefront's in all rounds but the one that the token lies in.
+    // Entries of a round before the tokens; its vectors begin with `base` of the part, most is the lane's largest value of the round.  A thread's counts are
+    // its own until the end.
     __device__ __forceinline__ void ranks(const TokenArgs &a, u32x4 (&now)[kTokenRoundVecs], float most, int base)
     {
 #pragma unroll 1
@@ -282,52 +335,8 @@ struct TokenPass {
             const float v = lane_value(value, c);
             if (__ballot(most >= v) == 0) continue;
             const int first = lane_value(here, c) >> (V::kLen == 8 ? 3 : 2);   // (-1 or less: it lies before the part)
-#pragma unroll
-            for (int j = 0; j < kTokenRoundVecs; ++j) V::again(now[j]);   // (or what is made of them for every token alike would be kept beside them)
-            const bool all_before = first >= base + kTokenRoundVecs * THREADS, none_before = first <= base;
-            uint32_t n = 0;
-            if constexpr (KIND == RDK_LOGIT_BF16) {
-                // above v: turned if v < 0;  at least v: turned if v <= 0, as -0 is the next below 0 in that order and equals it
-                const uint32_t half = __float_as_uint(v + 0.f) >> 16;
-                const uint32_t turn_above = v < 0.f ? 0x7FFF7FFFu : 0u, turn_least = v <= 0.f ? 0x7FFF7FFFu : 0u;
-                const uint32_t above = (half ^ (turn_above & 0xFFFFu)) * 0x10001u;
-                const uint32_t least = (v == 0.f ? 0xFFFEu : ((half ^ (turn_least & 0xFFFFu)) - 1u) & 0xFFFFu) * 0x10001u;
-                s16x2 counts = {0, 0};
-                auto take = [&](u32x4 x, uint32_t bound, uint32_t turn) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) counts -= __builtin_elementwise_sub_sat(s16x2_of(bound), s16x2_of(x[i] ^ turn)) >> 15;
-                };
-                if (all_before || none_before) {
-                    const uint32_t bound = all_before ? least : above, turn = all_before ? turn_least : turn_above;
-#pragma unroll
-                    for (int j = 0; j < kTokenRoundVecs; ++j) take(now[j], bound, turn);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < kTokenRoundVecs; ++j) {
-                        const bool before = base + j * THREADS + (int)threadIdx.x < first;
-                        take(now[j], before ? least : above, before ? turn_least : turn_above);
-                    }
-                }
-                n = __builtin_bit_cast(uint32_t, counts);
-                n = (n & 0xFFFFu) + (n >> 16);
-            } else {
-                const float above = v + 0.f, least = lane_value(below(value), c);   // (0 - 0 has no sign, -0 - 0 has)
-                auto take = [&](u32x4 x, float bound) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) n = __builtin_amdgcn_alignbit(n, __float_as_uint(bound - __uint_as_float(x[i])), 31);
-                };
-                static_assert(V::kLen * kTokenRoundVecs <= 32, "a bit each");
-                if (all_before || none_before) {
-                    const float bound = all_before ? least : above;
-#pragma unroll
-                    for (int j = 0; j < kTokenRoundVecs; ++j) take(now[j], bound);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < kTokenRoundVecs; ++j) take(now[j], base + j * THREADS + (int)threadIdx.x < first ? least : above);
-                }
-                n = __popc(n);
-            }
-            __hip_atomic_fetch_add(&before_token<THREADS>(c), n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+            __hip_atomic_fetch_add(&before_token<THREADS>(c), entries_before<KIND, THREADS>(now, base, first, v), __ATOMIC_RELAXED,
+                                   __HIP_MEMORY_SCOPE_WAVEFRONT);
         }
     }
 

@@ -127,6 +127,8 @@ def some_tokens(B, N, C, gen):
 
 
 def check_forward(x, tokens, kind, T=1.0, k=0, kernel=None, places=None):
+    if k:                                                               # without top entries, too: other kernels
+        check_forward(x, tokens, kind, T, 0, kernel, places)
     from paper_2506_03206_amd import rdk
     B, N = x.shape
     o = rdk.LogprobsOutputs(B, tokens.shape[1], k, "cuda")
@@ -199,7 +201,7 @@ def test_gradients(kind, B, N):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "prob"])
-@pytest.mark.parametrize("N", [5, 700, 20000, 90001])
+@pytest.mark.parametrize("N", [5, 700, 5000, 20000, 60000, 90001])
 def test_masks(kind, N):
     """Half of the ids masked, all, all but one, the type's lowest value as a mask, tokens that are masked, unknown, or padding."""
     B = 8
@@ -226,7 +228,7 @@ def test_masks(kind, N):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "prob"])
-@pytest.mark.parametrize("N", [9, 3001, 40000])
+@pytest.mark.parametrize("N", [9, 3001, 10000, 20000, 40000, 90001])
 def test_nan_and_infinity(kind, N):
     """A NaN or an infinity shows in its row and in no other; masked tokens of such a row stay -inf."""
     B = 6
@@ -261,7 +263,7 @@ def test_nan_and_infinity(kind, N):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "prob"])
-@pytest.mark.parametrize("N", [2, 300, 6000, 130000])
+@pytest.mark.parametrize("N", [2, 300, 6000, 15000, 30000, 60000, 130000])
 def test_sure_rows(kind, N):
     """Rows that are sure of one entry: the others together come to 1e-3 down to 1e-30 of it; the entropy, that entry's log probability and its gradient keep
     their own last bits, wherever in the row the entry stands."""
@@ -318,11 +320,11 @@ def test_weights_of_any_scale(scale):
 def test_ranks_of_ties():
     """Equal entries in order of their places, across vectors, rounds and parts, and zeros of both signs."""
     for kind in ("bf16", "f32"):
-        for N in (13, 2050, 70001):
-            x = torch.randint(-2, 3, (3, N), device="cuda").to(dtype_of(kind))
+        for B, N in ((3, 13), (3, 2050), (3, 7001), (3, 16001), (3, 30001), (33, 31001), (3, 70001)):
+            x = torch.randint(-2, 3, (B, N), device="cuda").to(dtype_of(kind))
             x[1] = torch.where(x[1] == 0, torch.tensor(-0.0, device="cuda", dtype=x.dtype), x[1])
             x[2, ::3] = -0.0
-            tokens = torch.stack([torch.randperm(N, device="cuda")[:13].to(torch.int32) for _ in range(3)])
+            tokens = torch.stack([torch.randperm(N, device="cuda")[:13].to(torch.int32) for _ in range(B)])
             tokens[0, 0], tokens[0, 1] = 0, N - 1
             check_forward(x, tokens, kind, k=5)
 
@@ -513,6 +515,19 @@ def test_rows_of_ties(kind):
         g[::4] = 0
         check_forward(x, tokens, kind, 0.3)
         check_gradients(x, tokens, kind, 0.3, g, h)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_ranks_of_the_lowest_value(kind):
+    """Tokens of the type's lowest finite value among others like it and masked ones, of rows that take every kernel."""
+    for B, N in ((3, 301), (3, 5003), (40, 20000), (8, 20000), (8, 45001), (8, 90001)):
+        x, gen = rows(kind, B, N, N)
+        u = torch.rand(x.shape, generator=gen, device="cuda")
+        x.masked_fill_(u < 0.4, torch.finfo(x.dtype).min)
+        x.masked_fill_(u > 0.8, -INF)
+        tokens = u.argsort(1)[:, :8].to(torch.int32)
+        tokens[:, 5:] = some_tokens(B, N, 3, gen)
+        check_forward(x, tokens, kind, 1.0, 7)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32", "prob"])

@@ -12,22 +12,36 @@ PART, FINISH, GRAD, ROW, TOP, MERGE = ("logprob_part_kernel", "logprob_finish_ke
 
 
 @pytest.mark.parametrize("kind,B,N,k,kernels", [
-    ("bf16", 8, 128256, 0, [PART, FINISH]), ("bf16", 127, 40000, 0, [PART, FINISH]), ("bf16", 128, 40000, 0, [PART]), ("bf16", 511, 4097, 0, [PART]),
-    ("bf16", 128, 4096, 0, [PART]), ("f32", 512, 8193, 0, [PART, FINISH]), ("prob", 600, 9000, 0, [PART]), ("bf16", 3, 16384, 0, [PART]),
-    ("bf16", 3, 16385, 0, [PART, FINISH]), ("bf16", 8, 128256, 5, [TOP, MERGE]), ("bf16", 200, 5000, 5, [TOP]), ("prob", 4, 30000, 128, [TOP, MERGE]),
+    ("bf16", 8, 128256, 0, [PART, FINISH]), ("bf16", 127, 70000, 0, [PART, FINISH]), ("bf16", 600, 40000, 0, [PART]), ("bf16", 1024, 40000, 0, [PART]),
+    ("bf16", 3, 4096, 0, [ROW]), ("bf16", 3, 4097, 0, [ROW]), ("bf16", 3, 8193, 0, [ROW]), ("bf16", 3, 16385, 0, [ROW]), ("bf16", 3, 32769, 0, [ROW]),
+    ("bf16", 256, 65536, 0, [ROW]), ("bf16", 257, 65536, 0, [PART, FINISH]), ("bf16", 3, 65537, 0, [PART, FINISH]),
+    ("f32", 300, 2049, 0, [ROW]), ("f32", 600, 4097, 0, [ROW]), ("f32", 512, 16384, 0, [ROW]), ("f32", 257, 16385, 0, [PART, FINISH]), ("f32", 33, 32768, 0, [ROW]),
+    ("prob", 512, 9000, 0, [ROW]), ("prob", 513, 9000, 0, [PART]), ("prob", 600, 8192, 0, [ROW]), ("prob", 256, 32768, 0, [ROW]), ("prob", 9, 32769, 0, [PART, FINISH]),
+    ("bf16", 8, 128256, 5, [TOP, MERGE]), ("bf16", 200, 5000, 5, [TOP]), ("prob", 4, 30000, 128, [TOP, MERGE]),
 ])
 def test_forward(kind, B, N, k, kernels):
     from paper_2506_03206_amd import rdk
     x, gen = rows(kind, B, N, B + N)
     tokens = some_tokens(B, N, 2, gen)
     o = rdk.LogprobsOutputs(B, 2, k, "cuda")
-    assert launched([PART, FINISH, TOP, MERGE], lambda: rdk.rdk_logprobs(x, tokens, "prob" if kind == "prob" else "logit", k=k, outputs=o)) == kernels
+    assert launched([PART, FINISH, ROW, TOP, MERGE], lambda: rdk.rdk_logprobs(x, tokens, "prob" if kind == "prob" else "logit", k=k, outputs=o)) == kernels
     check_forward(x, tokens, kind, k=k)
 
 
+def test_few_rows_of_many_tokens():
+    """Rows for one workgroup of 1024 threads each, or spread over several where they are few and have more than two tokens."""
+    from paper_2506_03206_amd import rdk
+    for kind, B, C, kernels in (("bf16", 31, 3, [PART, FINISH]), ("bf16", 32, 3, [ROW]), ("bf16", 31, 2, [ROW]), ("prob", 32, 16, [ROW]), ("prob", 5, 3, [PART, FINISH])):
+        x, gen = rows(kind, B, 32768 if kind == "prob" else 65536, B)
+        tokens = some_tokens(B, x.shape[1], C, gen)
+        assert launched([PART, FINISH, ROW], lambda: rdk.rdk_logprobs(x, tokens, "prob" if kind == "prob" else "logit")) == kernels
+        check_forward(x, tokens, kind)
+
+
 @pytest.mark.parametrize("kind,B,N,kernels", [
-    ("bf16", 4, 4096, [ROW]), ("bf16", 300, 16385, [ROW]), ("f32", 4, 16384, [ROW]), ("f32", 4, 16385, [PART, FINISH, GRAD]), ("f32", 129, 16385, [ROW]),
-    ("bf16", 127, 32769, [PART, FINISH, GRAD]), ("bf16", 128, 32769, [ROW]), ("bf16", 129, 131072, [ROW]), ("bf16", 129, 131073, [PART, GRAD]), ("f32", 600, 65537, [PART, GRAD]),
+    ("bf16", 4, 4096, [ROW]), ("bf16", 300, 16385, [ROW]), ("f32", 4, 16384, [ROW]), ("f32", 4, 16385, [GRAD, ROW]), ("f32", 129, 16385, [ROW]),
+    ("bf16", 127, 32769, [GRAD, ROW]), ("bf16", 128, 32769, [ROW]), ("bf16", 129, 131072, [ROW]), ("bf16", 129, 131073, [PART, FINISH, GRAD]),
+    ("f32", 600, 65537, [PART, GRAD]), ("bf16", 100, 65537, [PART, FINISH, GRAD]),
 ])
 def test_step(kind, B, N, kernels):
     from paper_2506_03206_amd import rdk
