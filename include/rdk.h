@@ -2,7 +2,8 @@
  * rdk.h -- C ABI of the MI355X (gfx950) library for Redistributing Drafter Kernels (RDK).
  *
  * The library covers the data-parallel hot path of the method, and beside it what its drafter is trained on and what decodes the same
- * rows without drawing: the teacher's top logits, distillation from them, beam search.  For a batch of B positions it
+ * rows without drawing: the teacher's top logits, distillation from them, beam search; and what stands at a model's ends: log
+ * probabilities of given tokens and embedding rows, with their gradients.  For a batch of B positions it
  * redistributes a vocabulary-pruned drafter's distribution q (n kept ids) onto the target
  * vocabulary (N ids) through a row-stochastic token-affinity kernel M (Alg. 1 of the paper), and
  * runs the accept / residual / sample step of speculative decoding against the target
