@@ -442,9 +442,10 @@ rdk_status_t rdk_beam_reorder(int32_t G, int32_t W, int32_t K, const int32_t *pa
  *     logits hold (they are not read), and so has a row that is masked altogether.  No workspace.
  *   rdk_logprobs_step  forward and backward at once, for d_logprob and d_entropy known beforehand; x is read once where a row fits the registers.
  *     No ranks and no alternatives (k = 0).
- * Gradients are of rows of logits only, B < 2^22 and B ceil(N / 16384) < 2^24 (fp32: N / 8192).  dx may be x itself (same stride), else they must not overlap.  Sums are held in fp32, a bf16 gradient is rounded once.
+ * Gradients are of rows of logits only, at temperatures from 2^-40 on, B < 2^22 and B ceil(N / 16384) < 2^24 (fp32: N / 8192).  dx may be x itself (same
+ * stride), else they must not overlap.  Sums are held in fp32, a bf16 gradient is rounded once.
  * Errors: RDK_ERR_NULL, RDK_ERR_SHAPE (B, N, C, k, strides, temperature, N other than the kernel's n, an overlap), RDK_ERR_DTYPE, RDK_ERR_ALIGN (x, dx, stats,
- * workspace), RDK_ERR_UNSUPPORTED (limits; weights with a temperature other than 1; gradients of weights; rdk_logprobs_step with k > 0), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
+ * workspace), RDK_ERR_UNSUPPORTED (limits; weights with a temperature other than 1; gradients of weights or at lower temperatures; rdk_logprobs_step with k > 0), RDK_ERR_WORKSPACE, RDK_ERR_HIP.
  */
 typedef struct {
     int32_t B, N, C, k;         /* rows, entries of a row, given tokens per row, alternatives per row */

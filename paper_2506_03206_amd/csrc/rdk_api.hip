@@ -863,7 +863,7 @@ static rdk_status_t check_logprobs_call(const rdk_logprobs_desc_t *d, const rdk_
 // Gradients: of logits, of a number of rows that a launch takes with all of their parts.
 static rdk_status_t check_logprobs_gradient(const rdk_logprobs_desc_t *d, rdk_input_kind_t kind, const void *x, int64_t ldx, const void *dx, int64_t ldd)
 {
-    if (kind == RDK_PROB_F32) return RDK_ERR_UNSUPPORTED;
+    if (kind == RDK_PROB_F32 || d->temperature < 0x1p-40f) return RDK_ERR_UNSUPPORTED;   // (the square of 1 / T stands in a gradient of the entropy)
     const rdk_distill_desc_t as{d->B, d->N, 1, d->temperature};
     const rdk_status_t rc = check_gradient(&as, kind, x, ldx, dx, ldd);
     if (rc != RDK_OK) return rc;

@@ -480,7 +480,7 @@ rdk_status_t launch_row(const LogprobArgs &a, const GradArgs &b, int32_t B, hipS
 // token's rank, in rounds or parts -> this way: 8192 bf16 rows of 4096 42.8 -> 21.0 us, 2048 of 1000 13.4 -> 7.1, 1024 of 16384 13.5 -> 12.7, 2048 of 32064 32.3 -> 30.9, 64 of
 // 32064 12.5 -> 6.5, 8192 fp32 rows of 2048 33.6 -> 16.2).  Weights take more registers: 512 rows of 16384 14.2 -> 10.2, 1024 16.2 -> 17.3 and so not.  1024 threads where a
 // row has a compute unit for itself (256 bf16 rows of 65536 16.0 -> 12.9, 512 21.2 -> 23.3; 256 rows of 32000 weights, 8 tokens 19.6 -> 14.8); a few rows of many tokens
-// are spread over more units instead, whose wavefronts have fewer ranks to count (one row of 65536, 8 tokens 11.8 us, 17.5 this way).
+// are spread over more units instead, whose wavefronts have fewer ranks to count (one row of 65536, 8 tokens 11.8 us, 17.5 this way).  A launch counts its threads in 32 bits.
 template <int KIND>
 rdk_status_t launch_forward(const LogprobArgs &a, int32_t B, hipStream_t st)
 {
@@ -489,7 +489,7 @@ rdk_status_t launch_forward(const LogprobArgs &a, int32_t B, hipStream_t st)
     if (a.n <= 256 * 2 * kLen) return launch_row<KIND, 256, 2, false>(a, none, B, st);
     if (a.n <= 256 * 4 * kLen) return launch_row<KIND, 256, 4, false>(a, none, B, st);
     if (a.n <= 256 * 8 * kLen) return launch_row<KIND, 256, 8, false>(a, none, B, st);
-    if (a.n <= 512 * 8 * kLen && (KIND != RDK_PROB_F32 || B <= 512)) return launch_row<KIND, 512, 8, false>(a, none, B, st);
+    if (a.n <= 512 * 8 * kLen && (KIND != RDK_PROB_F32 ? B < (1 << 23) : B <= 512)) return launch_row<KIND, 512, 8, false>(a, none, B, st);
     if (a.n <= 1024 * 8 * kLen && B <= 256 && (B >= 32 || a.t.C <= 2)) return launch_row<KIND, 1024, 8, false>(a, none, B, st);
     return launch_rows<KIND>(a, B, st);
 }

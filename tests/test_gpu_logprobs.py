@@ -57,6 +57,7 @@ def reference(x, tokens, kind, T=1.0, slots=None, g=None, h=None):
     dt = torch.gather(d, 1, at)
     lp = torch.where(masked[:, None], torch.full_like(dt, -INF), dt - torch.log1p(rest)[:, None])
     lp = torch.where(tokens == -2, torch.zeros_like(lp), torch.where(tokens == -1, torch.full_like(lp, -INF), lp))
+    lp = torch.where(lp < -torch.finfo(torch.float32).max, -INF, lp)     # no number of 32 bits: 4 / T at T = 2^-126 is 3.4e38 already
     dfin = lambda a: torch.where(torch.isfinite(a), a, torch.zeros_like(a)).abs()  # noqa: E731
     tol_lp = 2.0 ** -22 * dfin(dt) + (D * share)[:, None] + 2.0 ** -23 * dfin(lp) + n * 2.0 ** -126
     tol_h = D * (7 * share + 2 * u.abs()) + 2.0 ** -23 * entropy.abs() + 105 * n * 2.0 ** -126
@@ -542,3 +543,19 @@ def test_many_tokens_of_many_rows(kind):
         tokens[::3, 5] = -1
         tokens[1::3, 6] = N
         check_forward(x, tokens, kind)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_temperatures(kind):
+    """Temperatures at both ends of their range, powers of two (1 / T is exact): every kernel's forward call, and gradients from 2^-40 on."""
+    for B, N in ((6, 300), (6, 9001), (40, 20000), (6, 90001)):
+        x, gen = rows(kind, B, N, N)
+        x[1] = 1.0                                                          # all of them tie
+        x[2, ::2] = -INF
+        tokens = some_tokens(B, N, 2, gen)
+        tokens[:, 1] = x.float().argmax(1).to(torch.int32)
+        g, h = torch.randn((B, 2), generator=gen, device="cuda"), torch.randn(B, generator=gen, device="cuda")
+        for e in (-126, -70, -40, -20, 20, 100, 127):
+            check_forward(x, tokens, kind, 2.0 ** e, 3)
+            if e >= -40:
+                check_gradients(x, tokens, kind, 2.0 ** e, g, h)

@@ -55,6 +55,7 @@ def test_logprobs_refusals(rdk, which):
         assert call(k=1) == UNSUPPORTED
     if which != "forward":
         assert call(kind=0) == UNSUPPORTED
+        assert call(t=2.0 ** -41) == UNSUPPORTED
         assert call(dx=0) == NULL and call(ldd=999) == SHAPE and call(dx=0x900004) == ALIGN
         assert call(dx=0x100000, ldd=1008) == SHAPE                     # x itself, but other strides
         assert call(dx=0x100010) == SHAPE                               # overlaps x
