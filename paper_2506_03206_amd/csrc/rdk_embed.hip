@@ -783,7 +783,10 @@ GradPlan plan_of(const rdk_embed_desc_t &d, int columns)
     GradPlan p{};
     p.units = (d.d - 1) / columns + 1;
     p.few = d.B <= kFewTokens;
-    p.shift = std::max(threads_across(p.units, kWave), kLeastShift);
+    // Few tokens of wide rows: more columns to a workgroup where there are many more of these than the chip holds, each of which looks for its token (1000 tokens into
+    // 32000 x 8192 bf16 117.6 -> 109.2 us, added 24.1 -> 15.2; 844 into 3143 x 2048 8.6 -> 10.1 and so not).
+    const bool wide = p.few && (int64_t)d.B * ((p.units - 1) / kWave + 1) > 8192;
+    p.shift = std::max(threads_across(p.units, wide ? 2 * kWave : kWave), kLeastShift);
     p.blocks = (p.units - 1) / (1 << p.shift) + 1;
     if (p.few) return p;
     // Pieces as long as leaves enough of them to fill the chip.

@@ -240,3 +240,14 @@ def test_far_rows():
     assert (o.grad[5] == 7.0).all() and (o.grad[3:5] == 0).all()
     count = torch.bincount(ids.long(), minlength=6)[:3].float()
     assert torch.equal(o.grad[:3], count[:, None].expand(3, 1024))       # whole numbers below 2^24 are exact
+
+
+@pytest.mark.parametrize("types", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32)])
+def test_few_tokens_of_wide_rows(types):
+    """More columns to a workgroup, from more than 8192 workgroups of 64 threads across on."""
+    for B, d in ((513, 8195), (900, 5000)):
+        gen = generator(B)
+        ids = tokens("zipf", B, 700, gen)
+        x = strided(torch.randn((B, d), generator=gen, device="cuda"), d, types[1])
+        check_gradient(ids, x, 700, types[0], 0.5, False, d)
+        check_gradient(ids, x, 700, types[0], 0.5, True, d + 3)
