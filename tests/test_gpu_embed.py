@@ -58,6 +58,12 @@ def test_lookup(table, rows, d):
             check_lookup(tokens(how, B, V, gen), t, scale, out)
 
 
+def added(at, rows, V):
+    """Sums of the rows of equal places in 64 bits, small ones on the CPU (atomics on one address take half a minute)."""
+    where = "cpu" if rows.numel() <= 1 << 23 else rows.device
+    return torch.zeros((V, rows.shape[1]), dtype=torch.float64, device=where).index_add_(0, at.to(where), rows.to(where)).to(rows.device)
+
+
 def check_gradient(ids, d_out, V, dtype, scale, accumulate, ld=0, kernel=None, slots=None):
     from paper_2506_03206_amd import rdk
     d = d_out.shape[1]
@@ -70,9 +76,7 @@ def check_gradient(ids, d_out, V, dtype, scale, accumulate, ld=0, kernel=None, s
     rdk.rdk_embed_grad(ids, d_out, o, scale, kernel, accumulate)
     rows = torch.where(held[:, None], d_out.double(), 0.0)
     at = torch.where(held, at, 0)
-    total = torch.zeros((V, d), dtype=torch.float64, device="cuda").index_add_(0, at, rows)
-    absolute = torch.zeros((V, d), dtype=torch.float64, device="cuda").index_add_(0, at, rows.abs())
-    m = torch.zeros(V, dtype=torch.float64, device="cuda").index_add_(0, at, held.double())[:, None]
+    total, absolute, m = added(at, rows, V), added(at, rows.abs(), V), added(at, held.double()[:, None], V)
     base = old.double() if accumulate else torch.zeros_like(total)
     scale = float(torch.tensor(scale, dtype=F32))
     want = base + total * scale
