@@ -213,10 +213,11 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a)
     }
 }
 
-// Forward and backward of a row that lies in the registers of one workgroup, or forward alone (GRAD, RANKS: which): read once.  The largest value is known before the first exponential, so sums need no
-// second reference and what the largest leaves out is left out at once.  With two vectors a thread the exponentials are kept for the gradient; with more they are formed
-// again, because registers decide how many rows lie beside each other (2048 bf16 rows of 32064, 512 threads of eight vectors: 55 us with 5 wavefronts a SIMD unit, 60 with
-// 6, which spill, 67 with exponentials kept).  HBM: 2048 rows of 32064 52.5 us = 5.0 TB/s read and written, fp32 97 us = 5.4 TB/s.
+// Forward and backward of a row that lies in the registers of one workgroup, or forward alone (GRAD, RANKS: which): read once.  The largest value is known before
+// the first exponential, so sums need no second reference and what the largest leaves out is left out at once.  With two vectors a thread the exponentials are kept
+// for the gradient; with more they are formed again, because registers decide how many rows lie beside each other (2048 bf16 rows of 32064, 512 threads of eight
+// vectors: 55 us with 5 wavefronts a SIMD unit, 60 with 6, which spill, 67 with exponentials kept).  HBM: 2048 rows of 32064 52.5 us = 5.0 TB/s read and written,
+// fp32 97 us = 5.4 TB/s.
 template <int KIND, int THREADS, int VECS, bool GRAD, bool RANKS>
 __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel(LogprobArgs a, GradArgs b)
 {
