@@ -103,26 +103,28 @@ struct GradArgs {
 };
 
 // The gradient of a row: dx_j = 1/T (sum of g over the tokens at j - s_j (G + h (log s_j + entropy))), G = sum of g over the tokens that the row holds.
-// log s_j + entropy = (x_j - M) / T - pull / (1 + rest): one exponential and two products an element.  At a token of the largest value g - s G is
-// (g - G) + G rest / (1 + rest), so that a row that is sure of its token has the gradient that remains.
+// log s_j + entropy = (x_j - M) / T - pull / (1 + rest): one exponential and two products an element.  At tokens of the largest value, where s = 1 / (1 + rest), g - s G is
+// g rest / (1 + rest) - s (sum of g over the row's other tokens): no difference of g and G, of which nothing is left where the row is sure of its only token (rest far below
+// 2^-24), and beside whose rounding s is nothing where the row is flat.
 struct RowGrad {
     float m, c, least, inv_t;
-    float a0, a1, G, at_most;
+    float a0, a1, s_most, q_most, h_most;   // of the largest value: s, rest / (1 + rest), and what the entropy adds before 1 / T
 
     // stats as LogprobArgs has them
-    __device__ __forceinline__ RowGrad(const GradArgs &a, float4 stats, float sum_g, float h) : m(stats.x), c(a.c), least(a.least), inv_t(a.inv_t), G(sum_g)
+    __device__ __forceinline__ RowGrad(const GradArgs &a, float4 stats, float G, float h) : m(lane_value(stats.x, 0)), c(a.c), least(a.least), inv_t(a.inv_t)
     {
-        const float inv = 1.f / (1.f + stats.y);
-        a0 = -inv * inv_t * (G - h * stats.z);
-        a1 = -inv * inv_t * (h * inv_t);
-        at_most = inv_t * (G * (stats.y * inv) + h * stats.z * inv);   // what remains at the largest value where g = G
+        const float inv = 1.f / (1.f + stats.y);   // (all of it is alike for the wavefront: scalar registers)
+        a0 = lane_value(-inv * inv_t * (G - h * stats.z), 0);
+        a1 = lane_value(-inv * inv_t * (h * inv_t), 0);
+        s_most = lane_value(inv, 0);
+        q_most = lane_value(stats.y * inv, 0);
+        h_most = lane_value(h * stats.z * inv, 0);
     }
 
-    __device__ __forceinline__ float token(float x, float y, float g) const { return x == m ? fmaf(g - G, inv_t, at_most) : fmaf(g, inv_t, y); }
-
-    // A lane's vector of the gradient; first: the place of its first entry; place, g: the row's tokens, a lane each; terms: exp((x - M) / T) of its entries.
+    // A lane's vector of the gradient; first: the place of its first entry; place, g, elsewhere: the row's tokens, a lane each, and the sum of g over tokens at other
+    // places; terms: exp((x - M) / T) of its entries.
     template <int KIND>
-    __device__ __forceinline__ u32x4 vector(const u32x4 raw, const float (&terms)[Vec<KIND>::kLen], int first, int C, int place, float g) const
+    __device__ __forceinline__ u32x4 vector(const u32x4 raw, const float (&terms)[Vec<KIND>::kLen], int first, int C, int place, float g, float elsewhere) const
     {
         typedef Vec<KIND> V;
         float v[V::kLen], y[V::kLen];
@@ -137,36 +139,49 @@ struct RowGrad {
         uint64_t any = 0;
         for (int k = 0; k < C; ++k) any |= __ballot((uint32_t)(lane_value(place, k) - first) < (uint32_t)V::kLen);
         if (any) {
-            float add[V::kLen];
-            unsigned met = 0;
-#pragma unroll
-            for (int e = 0; e < V::kLen; ++e) add[e] = 0.f;
+            unsigned most = 0;   // entries of the largest value that tokens have met: before 1 / T
             for (int k = 0; k < C; ++k) {
                 const int at = lane_value(place, k) - first;
-                const float gk = lane_value(g, k);
+                const float gk = lane_value(g, k), others = lane_value(elsewhere, k);
 #pragma unroll
                 for (int e = 0; e < V::kLen; ++e)
                     if (at == e) {
-                        add[e] += gk;
-                        met |= 1u << e;
+                        if (v[e] == m) {
+                            if (!(most >> e & 1)) y[e] = fmaf(-others, s_most, h_most);
+                            y[e] = fmaf(gk, q_most, y[e]);
+                            most |= 1u << e;
+                        } else {
+                            y[e] = fmaf(gk, inv_t, y[e]);
+                        }
                     }
             }
 #pragma unroll
             for (int e = 0; e < V::kLen; ++e)
-                if (met >> e & 1) y[e] = token(v[e], y[e], add[e]);
+                if (most >> e & 1) y[e] *= inv_t;
         }
         return V::from(y);
     }
     template <int KIND>
-    __device__ __forceinline__ u32x4 vector(const u32x4 raw, int first, int C, int place, float g) const
+    __device__ __forceinline__ u32x4 vector(const u32x4 raw, int first, int C, int place, float g, float elsewhere) const
     {
         float v[Vec<KIND>::kLen];
         Vec<KIND>::to(raw, v);
 #pragma unroll
         for (int e = 0; e < Vec<KIND>::kLen; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * c);
-        return vector<KIND>(raw, v, first, C, place, g);
+        return vector<KIND>(raw, v, first, C, place, g, elsewhere);
     }
 };
+
+// In lane c: the sum of g over the tokens that lie at other places than token c.  (g is 0 of those that the row does not hold.)
+__device__ __forceinline__ float tokens_elsewhere(int place, float g, int C)
+{
+    float sum = 0.f;
+    for (int k = 0; k < C; ++k) {
+        const float gk = lane_value(g, k);
+        sum += lane_value(place, k) != place ? gk : 0.f;
+    }
+    return sum;
+}
 
 // The gradient of a part of a row, from the statistics that the forward call left.  One exponential and two or three products an entry, nothing to meet for: HBM
 // (2048 fp32 rows of 32064 95 us = 5.5 TB/s read and written), or the last-level cache where the logits still lie there (1024 bf16 rows of 16384 9.6-11.7 us = 5.7 TB/s
@@ -205,10 +220,11 @@ __global__ __launch_bounds__(kThreads) void logprob_grad_kernel(GradArgs a)
         raw[j] = left > 0 ? V::load_at(from, (j * kThreads + tid) * 16, left) : V::fill();
     }
     const RowGrad grad(a, st, wave_sum(g), h);
+    const float elsewhere = tokens_elsewhere(place, g, a.C);
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
         const int first = (j * kThreads + tid) * V::kLen, left = here - first;
-        const u32x4 y = grad.template vector<KIND>(raw[j], begin + first, a.C, place, g);
+        const u32x4 y = grad.template vector<KIND>(raw[j], begin + first, a.C, place, g, elsewhere);
         if (left > 0) V::store_at(to, first * V::kSize, left, y);
     }
 }
@@ -224,6 +240,8 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
     typedef Vec<KIND> V;
     constexpr int kW = THREADS / kWave;
     constexpr bool kKeep = GRAD && VECS <= 2;
+    // g asked for behind the sums, where registers are short while they run (16 vectors: 8 registers spilled become 1, 1024 rows of 60000 54.5 -> 49.3 us; eight 48 -> 51 and so not)
+    constexpr bool kLate = VECS > 8;
     __shared__ float wave_m[kW], wave_rest[kW], wave_pull[kW];
     __shared__ int wave_ties[kW], wave_rank[RANKS ? kW : 1][kMaxTokens];
     const int64_t row = blockIdx.x;
@@ -244,7 +262,7 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         place = place_of(a.t.tokens[row * a.t.C + lane_id()], a.t.slot_of, a.t.ids);
         if (place >= 0) {
             value = load1<KIND>(from, place);
-            if (GRAD && b.above) g = b.above[row * a.t.C + lane_id()];
+            if (GRAD && !kLate && b.above) g = b.above[row * a.t.C + lane_id()];
             if (RANKS && wid == 0) {   // entries of its own vector that equal it and lie before it
                 const int own = place & ~(V::kLen - 1);
                 float v[V::kLen];
@@ -338,6 +356,7 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         wave_pull[wid] = pull;
         wave_ties[wid] = ties;
     }
+    if (GRAD && kLate && b.above && place >= 0) g = b.above[row * a.t.C + lane_id()];
     if constexpr (RANKS) {
 #pragma unroll 1
         for (int c = 0; c < a.t.C; ++c) {
@@ -380,17 +399,18 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
     }
     const RowGrad grad(b, st, wave_sum(g), h);
     const int C = b.above ? b.C : 0;
+    const float elsewhere = tokens_elsewhere(place, g, C);
 #pragma unroll
     for (int j = 0; j < VECS; ++j) {
         const int at = j * THREADS + tid;
         u32x4 y;
-        if constexpr (kKeep) y = grad.template vector<KIND>(raw[j], terms[j], at * V::kLen, C, place, g);
-        else y = grad.template vector<KIND>(raw[j], at * V::kLen, C, place, g);
+        if constexpr (kKeep) y = grad.template vector<KIND>(raw[j], terms[j], at * V::kLen, C, place, g, elsewhere);
+        else y = grad.template vector<KIND>(raw[j], at * V::kLen, C, place, g, elsewhere);
         if (at < whole) V::store_at(to, (uint32_t)at * 16u, V::kLen, y);
         __builtin_amdgcn_sched_barrier(0);
     }
     if (behind > 0 && wid == last_tid / kWave) {
-        const u32x4 y = grad.template vector<KIND>(last, whole * V::kLen - (last_tid - tid) * V::kLen, C, place, g);
+        const u32x4 y = grad.template vector<KIND>(last, whole * V::kLen - (last_tid - tid) * V::kLen, C, place, g, elsewhere);
         if (tid == last_tid) V::store_at(to, (uint32_t)whole * 16u, behind, y);
     }
     }
