@@ -8,8 +8,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxParts = kWave;     // of a row: a lane each in the finish
-constexpr float kLog2e = 1.44269504088896341f;
-
 struct LogprobArgs {
     const void *x;
     int64_t ldx;
@@ -94,7 +92,9 @@ struct GradArgs {
     int64_t ldx;
     const int32_t *slot_of;
     int ids, n, C, parts;
-    float inv_t, c, least;    // least: what exponents of base 2 need not go below, over c
+    float inv_t;
+    Distance from_most;
+    float least;              // what distances need not go below: 200 in units of log 2
     const int32_t *tokens;
     const float4 *stats;
     const float *above, *above_entropy;   // d / d logprob [B, C], d / d entropy [B]; either may be NULL
@@ -103,19 +103,21 @@ struct GradArgs {
 };
 
 // The gradient of a row: dx_j = 1/T (sum of g over the tokens at j - s_j (G + h (log s_j + entropy))), G = sum of g over the tokens that the row holds.
-// log s_j + entropy = (x_j - M) / T - pull / (1 + rest): one exponential and two products an element.  At tokens of the largest value, where s = 1 / (1 + rest), g - s G is
+// log s_j + entropy = (x_j - M) / T - pull / (1 + rest): one exponential and two products an element, with distances in units of about T (the square of 1 / T in the
+// entropy's term would be 0 at high temperatures).  At tokens of the largest value, where s = 1 / (1 + rest), g - s G is
 // g rest / (1 + rest) - s (sum of g over the row's other tokens): no difference of g and G, of which nothing is left where the row is sure of its only token (rest far below
 // 2^-24), and beside whose rounding s is nothing where the row is flat.
 struct RowGrad {
-    float m, c, least, inv_t;
+    float m, least, inv_t;
+    Distance from_most;
     float a0, a1, s_most, q_most, h_most;   // of the largest value: s, rest / (1 + rest), and what the entropy adds before 1 / T
 
     // stats as LogprobArgs has them
-    __device__ __forceinline__ RowGrad(const GradArgs &a, float4 stats, float G, float h) : m(lane_value(stats.x, 0)), c(a.c), least(a.least), inv_t(a.inv_t)
+    __device__ __forceinline__ RowGrad(const GradArgs &a, float4 stats, float G, float h) : m(lane_value(stats.x, 0)), least(a.least), inv_t(a.inv_t), from_most(a.from_most)
     {
         const float inv = 1.f / (1.f + stats.y);   // (all of it is alike for the wavefront: scalar registers)
-        a0 = lane_value(-inv * inv_t * (G - h * stats.z), 0);
-        a1 = lane_value(-inv * inv_t * (h * inv_t), 0);
+        a0 = lane_value(-(inv * (G - h * stats.z)) * inv_t, 0);
+        a1 = lane_value(-(inv * (h * from_most.inv)) * inv_t, 0);
         s_most = lane_value(inv, 0);
         q_most = lane_value(stats.y * inv, 0);
         h_most = lane_value(h * stats.z * inv, 0);
@@ -134,7 +136,7 @@ struct RowGrad {
             for (int e = 0; e < V::kLen; ++e) y[e] = terms[e] * a0;
         } else {   // (The distance of a masked entry is held finite: s = 0, whatever its factor.  NaN is in the row's sum.)
 #pragma unroll
-            for (int e = 0; e < V::kLen; ++e) y[e] = terms[e] * fmaf(a1, fmaxf(v[e] - m, least), a0);
+            for (int e = 0; e < V::kLen; ++e) y[e] = terms[e] * fmaf(a1, fmaxf(from_most.of(v[e], m), least), a0);
         }
         uint64_t any = 0;
         for (int k = 0; k < C; ++k) any |= __ballot((uint32_t)(lane_value(place, k) - first) < (uint32_t)V::kLen);
@@ -167,7 +169,7 @@ struct RowGrad {
         float v[Vec<KIND>::kLen];
         Vec<KIND>::to(raw, v);
 #pragma unroll
-        for (int e = 0; e < Vec<KIND>::kLen; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - m) * c);
+        for (int e = 0; e < Vec<KIND>::kLen; ++e) v[e] = __builtin_amdgcn_exp2f(from_most.of(v[e], m) * from_most.c);
         return vector<KIND>(raw, v, first, C, place, g, elsewhere);
     }
 };
@@ -451,8 +453,8 @@ GradArgs grad_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, Row
     a.ids = h ? h->N : d.N;
     a.n = d.N; a.C = d.C;
     a.inv_t = 1.f / d.temperature;
-    a.c = a.inv_t * kLog2e;
-    const float least = -200.f / a.c;
+    a.from_most = Distance::over(d.temperature);
+    const float least = -200.f / a.from_most.c;
     a.least = least > -0x1p126f ? least : -0x1p126f;
     a.tokens = tokens; a.stats = stats; a.above = above; a.above_entropy = above_entropy;
     a.dx = dx; a.ldd = ldd;

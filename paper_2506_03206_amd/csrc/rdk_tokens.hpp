@@ -5,6 +5,9 @@
 // every term of which has one sign: a row that is sure of its best entry has an entropy and a log probability of that entry far below
 // the rounding of a sum that begins with 1, and they keep their own 24 bits this way.
 #pragma once
+#include <algorithm>
+#include <cmath>
+
 #include "rdk_select.hpp"
 #include "rdk_vec.hpp"
 
@@ -12,7 +15,23 @@ namespace rdk {
 
 constexpr int kMaxTokens = 16;        // given tokens of a row: a lane each
 constexpr int kTokenRoundVecs = 4;    // 16-byte vectors of a thread in a round
-constexpr float kLn2 = 0.693147180559945309f;
+constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
+
+// (x - M) / T by way of (x - M) unit, with a power of two that makes it a number of about its final size: nothing overflows that the result does not, at whatever T,
+// and the bits are those of x - M.
+struct Distance {
+    float unit;   // 2^-floor(log2 T); 1/2 at temperatures below 2
+    float inv;    // to units of log e
+    float c;      // to units of log 2
+
+    static Distance over(float T)
+    {
+        const float unit = std::ldexp(1.f, -std::min(std::max(std::ilogb(T), 1), 126));
+        const float inv = T < 2.f ? 1.f / T * 2.f : 1.f / (T * unit);
+        return Distance{unit, inv, inv * kLog2e};
+    }
+    __device__ __forceinline__ float of(float x, float m) const { return fmaf(x, unit, -m * unit); }
+};
 
 // What a part of a row, or a row, comes to.  m: the largest value; rest: the others' sum relative to it (the largest itself counts 1 beside it);
 // pull: the sum of their terms times their distance to it, in units of log e (<= 0).  Of a part without unmasked entries m is none.

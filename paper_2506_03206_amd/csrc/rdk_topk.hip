@@ -8,7 +8,6 @@ namespace rdk {
 namespace {
 
 constexpr int kTopThreads = 256;
-constexpr float kLog2e = 1.44269504088896341f;
 
 constexpr int kRoundVecs = 4;          // 16-byte vectors of a lane in a round
 constexpr int kNoted = 512, kFound = 1024;   // vectors noted by a wavefront, entries sorted: what exceeds these takes a slower way
