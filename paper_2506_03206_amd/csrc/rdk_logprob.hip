@@ -144,6 +144,7 @@ struct RowGrad {
             unsigned most = 0;   // entries of the largest value that tokens have met: before 1 / T
             for (int k = 0; k < C; ++k) {
                 const int at = lane_value(place, k) - first;
+                if (__ballot((uint32_t)at < (uint32_t)V::kLen) == 0) continue;
                 const float gk = lane_value(g, k), others = lane_value(elsewhere, k);
 #pragma unroll
                 for (int e = 0; e < V::kLen; ++e)
