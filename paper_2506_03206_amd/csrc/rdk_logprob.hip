@@ -297,15 +297,15 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
     const float ref = weight_reference(m);
     // of weights: a power of two that keeps them from overflowing and from having few bits, and the largest's reciprocal beside it
     const float scale = KIND == RDK_PROB_F32 ? power_of_two(-weight_exponent(m)) : 1.f, inv = KIND == RDK_PROB_F32 ? m > 0.f ? 1.f / (m * scale) : 0.f : 1.f;
-    // an entry relative to the largest value, and its distance from it: over T, in units of log 2 for weights
+    // an entry relative to the largest value, and its distance from it: in the units of from_most, of log 2 for weights
     auto term = [&](float v, float &d) __attribute__((always_inline)) {
         if constexpr (KIND == RDK_PROB_F32) {
             const float x = v * scale * inv;
             d = __builtin_amdgcn_logf(fmaxf(x, 0x1p-126f));
             return x;
         } else {
-            d = v - ref;
-            return __builtin_amdgcn_exp2f(d * a.t.c);
+            d = a.t.from_most.of(v, ref);
+            return __builtin_amdgcn_exp2f(d * a.t.from_most.c);
         }
     };
     float rest = 0.f, pull = 0.f, terms[kKeep ? VECS : 1][V::kLen];
@@ -381,7 +381,7 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
     }
     const bool some = m > no_value<KIND>() && m < INFINITY;
     rest = some ? rest + (float)(ties - 1) : m > 0.f ? NAN : rest - rest;   // (an infinity; NaN where there is one, 0 where all is masked)
-    pull = some ? pull * (KIND == RDK_PROB_F32 ? kLn2 : a.t.inv_t) : 0.f;
+    pull = some ? pull * (KIND == RDK_PROB_F32 ? kLn2 : a.t.from_most.inv) : 0.f;
     const float4 st = make_float4(m, rest, pull / (1.f + rest), 0.f);
     if (wid == 0) {
         if (RANKS && lane_id() < a.t.C)
@@ -453,8 +453,8 @@ GradArgs grad_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, Row
     a.slot_of = h ? h->slot_of : nullptr;
     a.ids = h ? h->N : d.N;
     a.n = d.N; a.C = d.C;
-    a.inv_t = 1.f / d.temperature;
     a.from_most = Distance::over(d.temperature);
+    a.inv_t = a.from_most.inv * a.from_most.unit;
     const float least = -200.f / a.from_most.c;
     a.least = least > -0x1p126f ? least : -0x1p126f;
     a.tokens = tokens; a.stats = stats; a.above = above; a.above_entropy = above_entropy;
@@ -554,8 +554,8 @@ TokenArgs token_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, c
     t.kept_ids = h ? h->kept_ids : nullptr;
     t.ids = h ? h->N : d.N;
     t.C = d.C;
-    t.inv_t = 1.f / d.temperature;
-    t.c = t.inv_t * kLog2e;
+    t.from_most = Distance::over(d.temperature);
+    t.c = t.from_most.c * t.from_most.unit;
     t.margin = 8.f / t.c;
     t.tokens = tokens; t.logprob = logprob; t.entropy = entropy; t.rank = rank; t.stats = stats;
     return t;

@@ -44,7 +44,8 @@ struct TokenArgs {
     const int32_t *kept_ids;  // slot -> target id, with slot_of
     int ids;                  // ids below this are known there
     int C;
-    float inv_t, c, margin;   // c = log2(e) / T; margin: what references are exceeded by before they are replaced, 8 / c
+    Distance from_most;
+    float c, margin;          // c = log2(e) / T; margin: what references are exceeded by before they are replaced, 8 / c
     const int32_t *tokens;
     float *logprob, *entropy;
     int32_t *rank;
@@ -172,14 +173,14 @@ inline uint32_t before_tokens_bytes(const TokenArgs &a, int threads) { return a.
 
 // log probability of an entry x of a row with the largest value m, log_all = log(1 + rest)
 template <int KIND>
-__device__ __forceinline__ float log_share(float x, float m, float log_all, float inv_t)
+__device__ __forceinline__ float log_share(float x, float m, float log_all, const Distance &by)
 {
     if (KIND == RDK_PROB_F32) {
         if (!(x > 0.f)) return x == 0.f ? -INFINITY : x;
         // (the ratio of weights that far apart may be no normal number, which has fewer bits)
         return (x < m * 0x1p-100f ? logf(x * 0x1p64f) - (logf(m) + 64.f * kLn2) : logf(x / m)) - log_all;
     }
-    return x == -INFINITY ? -INFINITY : (x - m) * inv_t - log_all;
+    return x == -INFINITY ? -INFINITY : by.of(x, m) * by.inv - log_all;
 }
 
 // The outputs of a row, by one wavefront; count: of lane c, entries before token c.
@@ -191,7 +192,7 @@ __device__ __forceinline__ void write_tokens(const TokenArgs &a, int64_t row, Ro
     if (lane_id() < a.C) {
         const int64_t o = row * a.C + lane_id();
         float lp = place == kNoToken ? 0.f : -INFINITY;
-        if (place >= 0 && !none) lp = log_share<KIND>(value, s.m, log_all, a.inv_t);
+        if (place >= 0 && !none) lp = log_share<KIND>(value, s.m, log_all, a.from_most);
         a.logprob[o] = lp;
         if (a.rank) a.rank[o] = place >= 0 && lp > -INFINITY ? count : -1;
     }
@@ -433,7 +434,7 @@ struct TokenPass {
                     e = x * scale * inv;
                     d = __builtin_amdgcn_logf(fmaxf(e, 0x1p-126f));
                 } else {
-                    d = fmaxf((x - m) * a.c, -0x1p126f);
+                    d = fmaxf(a.from_most.of(x, m) * a.from_most.c, -0x1p126f);
                     e = __builtin_amdgcn_exp2f(d);
                     if (x != x) e = x;
                 }
@@ -523,7 +524,7 @@ __device__ __forceinline__ RowSum merge_tokens(const TokenArgs &a, int64_t row, 
     r.m = wave_max(p.m);
     const uint64_t who = __ballot(p.m == r.m && p.m > no_value<KIND>());
     const bool holder = who && lane == __ffsll((unsigned long long)who) - 1, none = !(p.m > no_value<KIND>());
-    const float far = none ? 0.f : KIND == RDK_PROB_F32 ? logf(p.m / r.m) : (p.m - r.m) * a.inv_t;
+    const float far = none ? 0.f : KIND == RDK_PROB_F32 ? logf(p.m / r.m) : a.from_most.of(p.m, r.m) * a.from_most.inv;
     const float f = none ? 0.f : KIND == RDK_PROB_F32 ? p.m / r.m : expf(far), all = f * ((holder ? 0.f : 1.f) + p.rest);
     // (a part without unmasked entries has no terms, but NaN shows in its sum)
     r.rest = wave_sum(none ? p.rest : all);

@@ -170,7 +170,7 @@ __device__ __forceinline__ void write_top(const TokenArgs &t, int32_t *ids, floa
         const uint64_t e = in ? sorted[threadIdx.x] : 0;
         const int32_t at = in ? (int32_t)entry_id(e) : -1;
         ids[row * k + threadIdx.x] = in && t.kept_ids ? t.kept_ids[at] : at;
-        values[row * k + threadIdx.x] = in ? log_share<KIND>(key_value(entry_key(e)), r.m, log1pf(r.rest), t.inv_t) : -INFINITY;
+        values[row * k + threadIdx.x] = in ? log_share<KIND>(key_value(entry_key(e)), r.m, log1pf(r.rest), t.from_most) : -INFINITY;
     }
 }
 

@@ -1,4 +1,5 @@
-"""Logits and temperatures of any size together: distances from the largest value that are ordinary numbers only over T.  Tolerances: those of test_gpu_logprobs.py."""
+"""Logits and temperatures of any size together: distances from the largest value that are ordinary numbers only over T, differences of logits that are no number of 32
+bits, the lowest finite value as a mask at temperatures that see it.  Tolerances: those of test_gpu_logprobs.py."""
 import pytest
 import torch
 
@@ -23,3 +24,40 @@ def test_logits_of_the_temperatures_size(kind, B, N):
         check_forward(x, tokens, kind, 2.0 ** e, 3)
         check_gradients(x, tokens, kind, 2.0 ** e, None, h)
         check_gradients(x, tokens, kind, 2.0 ** e, g, h)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N", SIZES)
+def test_the_lowest_and_the_largest_value(kind, B, N):
+    """Half of the ids at the lowest finite value beside ordinary ones, beside the largest finite value, and beside one of it: at 2^127 these are 2 or 4 apart."""
+    low, high = torch.finfo(dtype_of(kind)).min, torch.finfo(dtype_of(kind)).max
+    for e, size in ((0, 1.0), (1, 1.0), (60, 1.0), (120, 2.0 ** 30), (126, 2.0 ** 40), (127, 2.0 ** 40)):
+        x, gen = rows(kind, B, N, N + e)
+        half = torch.rand(x.shape, generator=gen, device="cuda") < 0.5
+        x[0].masked_fill_(half[0], low)
+        x[1] = torch.where(half[1], torch.tensor(low, device="cuda"), torch.tensor(high, device="cuda")).to(x.dtype)
+        x[2] = low
+        x[2, N // 3] = high
+        x[3].masked_fill_(half[3], low)
+        x[3, ::3] = -INF
+        x[4] = low
+        tokens = some_tokens(B, N, 3, gen)
+        tokens[:, 1] = half.float().argmax(1).to(torch.int32)
+        tokens[2, 2] = N // 3
+        g, h = torch.randn((B, 3), generator=gen, device="cuda") * size, torch.randn(B, generator=gen, device="cuda") * size
+        check_forward(x, tokens, kind, 2.0 ** e, 3)
+        check_gradients(x, tokens, kind, 2.0 ** e, g, h)
+        check_gradients(x, tokens, kind, 2.0 ** e, None, h)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N", SIZES)
+def test_large_logits_at_high_temperatures(kind, B, N):
+    """Logits of a few T = 2^120, whose distances' sums over a row are no number of 32 bits before they are taken over T."""
+    x, gen = rows("f32", B, N, N + 3, sigma=1.5)
+    x = (x * 2.0 ** 120).to(dtype_of(kind))
+    tokens = some_tokens(B, N, 2, gen)
+    g, h = torch.randn((B, 2), generator=gen, device="cuda") * 2.0 ** 30, torch.randn(B, generator=gen, device="cuda") * 2.0 ** 30
+    check_forward(x, tokens, kind, 2.0 ** 120, 3)
+    check_gradients(x, tokens, kind, 2.0 ** 120, None, h)
+    check_gradients(x, tokens, kind, 2.0 ** 120, g, h)
