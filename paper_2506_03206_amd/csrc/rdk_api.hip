@@ -938,7 +938,8 @@ static rdk_status_t check_embed_rows(const rdk_embed_desc_t &d, const int32_t *i
 {
     if (!float_ok(table_type) || !float_ok(rows_type)) return RDK_ERR_DTYPE;
     if (!ids || !table || !rows) return RDK_ERR_NULL;
-    if (ldt < d.d || ldo < d.d || ldt > (int64_t)1 << 34 || ldo > (int64_t)1 << 34) return RDK_ERR_SHAPE;   // (extents stay inside 64 bits)
+    if (ldt < d.d || ldo < d.d || ldt > (int64_t)1 << 34 || ldo > (int64_t)1 << 34) return RDK_ERR_SHAPE;
+    if ((d.V - 1) * ldt > (int64_t)1 << 60) return RDK_ERR_SHAPE;   // (extents stay inside 64 bits; of B < 2^24 rows they do)
     if (!aligned16(table) || !aligned16(rows)) return RDK_ERR_ALIGN;
     const size_t table_bytes = ((size_t)(d.V - 1) * ldt + d.d) * (table_type == RDK_BF16 ? 2 : 4);
     const size_t rows_bytes = ((size_t)(d.B - 1) * ldo + d.d) * (rows_type == RDK_BF16 ? 2 : 4);
