@@ -295,17 +295,19 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
 #pragma unroll
     for (int w = 1; w < kW; ++w) m = fmaxf(m, wave_m[w]);
     const float ref = weight_reference(m);
+    // (Values from `far` on lie 2^103 T apart: all but the largest, which the sums leave out, are then held to be infinitely far.)
+    const float minus_ref = fabsf(ref) < a.t.far ? -ref * a.t.in_sums.unit : -INFINITY;
     // of weights: a power of two that keeps them from overflowing and from having few bits, and the largest's reciprocal beside it
     const float scale = KIND == RDK_PROB_F32 ? power_of_two(-weight_exponent(m)) : 1.f, inv = KIND == RDK_PROB_F32 ? m > 0.f ? 1.f / (m * scale) : 0.f : 1.f;
-    // an entry relative to the largest value, and its distance from it: in the units of from_most, of log 2 for weights
+    // an entry relative to the largest value, and its distance from it: in the units of in_sums, of log 2 for weights
     auto term = [&](float v, float &d) __attribute__((always_inline)) {
         if constexpr (KIND == RDK_PROB_F32) {
             const float x = v * scale * inv;
             d = __builtin_amdgcn_logf(fmaxf(x, 0x1p-126f));
             return x;
         } else {
-            d = a.t.from_most.of(v, ref);
-            return __builtin_amdgcn_exp2f(d * a.t.from_most.c);
+            d = fmaf(v, a.t.in_sums.unit, minus_ref);
+            return __builtin_amdgcn_exp2f(d * a.t.in_sums.c);
         }
     };
     float rest = 0.f, pull = 0.f, terms[kKeep ? VECS : 1][V::kLen];
@@ -344,6 +346,7 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
                     const float x = term(v[e], d);
                     ties += __popcll(__ballot(v[e] == m));
                     s += v[e] == m ? 0.f : x;
+                    if constexpr (kKeep) terms[j][e] = v[e] == m ? 1.f : x;
                     if (KIND == RDK_PROB_F32) p = v[e] == m ? p : fmaf(x, d, p);
                 }
             }
@@ -381,7 +384,7 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
     }
     const bool some = m > no_value<KIND>() && m < INFINITY;
     rest = some ? rest + (float)(ties - 1) : m > 0.f ? NAN : rest - rest;   // (an infinity; NaN where there is one, 0 where all is masked)
-    pull = some ? pull * (KIND == RDK_PROB_F32 ? kLn2 : a.t.from_most.inv) : 0.f;
+    pull = some ? pull * (KIND == RDK_PROB_F32 ? kLn2 : a.t.in_sums.inv) : 0.f;
     const float4 st = make_float4(m, rest, pull / (1.f + rest), 0.f);
     if (wid == 0) {
         if (RANKS && lane_id() < a.t.C)
@@ -555,6 +558,8 @@ TokenArgs token_arguments(const rdk_logprobs_desc_t &d, const KernelHandle *h, c
     t.ids = h ? h->N : d.N;
     t.C = d.C;
     t.from_most = Distance::over(d.temperature);
+    t.in_sums = Distance::in_sums(d.temperature);
+    t.far = t.in_sums.unit > 1.f ? 0x1p126f / t.in_sums.unit : INFINITY;
     t.c = t.from_most.c * t.from_most.unit;
     t.margin = 8.f / t.c;
     t.tokens = tokens; t.logprob = logprob; t.entropy = entropy; t.rank = rank; t.stats = stats;

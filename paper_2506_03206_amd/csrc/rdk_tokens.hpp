@@ -20,7 +20,7 @@ constexpr float kLn2 = 0.693147180559945309f, kLog2e = 1.44269504088896341f;
 // (x - M) / T by way of (x - M) unit, with a power of two that makes it a number of about its final size: nothing overflows that the result does not, at whatever T,
 // and the bits are those of x - M.
 struct Distance {
-    float unit;   // 2^-floor(log2 T); 1/2 at temperatures below 2
+    float unit;   // 1 / T to a power of two; 1/2 at temperatures below 2
     float inv;    // to units of log e
     float c;      // to units of log 2
 
@@ -28,6 +28,15 @@ struct Distance {
     {
         const float unit = std::ldexp(1.f, -std::min(std::max(std::ilogb(T), 1), 126));
         const float inv = T < 2.f ? 1.f / T * 2.f : 1.f / (T * unit);
+        return Distance{unit, inv, inv * kLog2e};
+    }
+    // Of sums of exponentials times distances: at temperatures below 2^-10, too, a number of about the size over T, so that products with exponentials that are next to
+    // nothing keep their bits.  (Above, half of x - M is near enough, and finite for any two numbers: masks of the lowest value cost nothing.)
+    static Distance in_sums(float T)
+    {
+        const int e = std::ilogb(T) + 1;
+        if (e > -10) return over(T);
+        const float unit = std::ldexp(1.f, -e), inv = 1.f / (T * unit);
         return Distance{unit, inv, inv * kLog2e};
     }
     __device__ __forceinline__ float of(float x, float m) const { return fmaf(x, unit, -m * unit); }
@@ -45,6 +54,8 @@ struct TokenArgs {
     int ids;                  // ids below this are known there
     int C;
     Distance from_most;
+    Distance in_sums;         // those in the sums of rows in registers
+    float far;                // a largest value whose product with its unit may be no number
     float c, margin;          // c = log2(e) / T; margin: what references are exceeded by before they are replaced, 8 / c
     const int32_t *tokens;
     float *logprob, *entropy;
