@@ -112,7 +112,7 @@ struct RowGrad {
     Distance from_most;
     float a0, a1, s_most, q_most, h_most;   // of the largest value: s, rest / (1 + rest), and what the entropy adds before 1 / T
 
-    // stats as LogprobArgs has them
+    // stats as TokenArgs has them
     __device__ __forceinline__ RowGrad(const GradArgs &a, float4 stats, float G, float h) : m(lane_value(stats.x, 0)), least(a.least), inv_t(a.inv_t), from_most(a.from_most)
     {
         const float inv = 1.f / (1.f + stats.y);   // (all of it is alike for the wavefront: scalar registers)
@@ -393,32 +393,32 @@ __global__ __launch_bounds__(THREADS, VECS <= 8 ? 5 : 4) void logprob_row_kernel
         write_tokens<KIND>(a.t, row, RowSum{m, rest, pull}, place, value, count);
     }
     if constexpr (GRAD) {
-    char *to = (char *)const_cast<void *>(row_ptr<KIND>(b.dx, b.ldd, row));
-    const bool masked = m == -INFINITY && rest == 0.f;
-    if (masked || (h == 0.f && __ballot(g != 0.f) == 0)) {
-        const u32x4 zero{0, 0, 0, 0};
+        char *to = (char *)const_cast<void *>(row_ptr<KIND>(b.dx, b.ldd, row));
+        const bool masked = m == -INFINITY && rest == 0.f;
+        if (masked || (h == 0.f && __ballot(g != 0.f) == 0)) {
+            const u32x4 zero{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < VECS; ++j)
-            if (j * THREADS + tid < whole) V::store_at(to, (uint32_t)(j * THREADS + tid) * 16u, V::kLen, zero);
-        if (behind > 0 && tid == last_tid) V::store_at(to, (uint32_t)whole * 16u, behind, zero);
-        return;
-    }
-    const RowGrad grad(b, st, wave_sum(g), h);
-    const int C = b.above ? b.C : 0;
-    const float elsewhere = tokens_elsewhere(place, g, C);
+            for (int j = 0; j < VECS; ++j)
+                if (j * THREADS + tid < whole) V::store_at(to, (uint32_t)(j * THREADS + tid) * 16u, V::kLen, zero);
+            if (behind > 0 && tid == last_tid) V::store_at(to, (uint32_t)whole * 16u, behind, zero);
+            return;
+        }
+        const RowGrad grad(b, st, wave_sum(g), h);
+        const int C = b.above ? b.C : 0;
+        const float elsewhere = tokens_elsewhere(place, g, C);
 #pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        const int at = j * THREADS + tid;
-        u32x4 y;
-        if constexpr (kKeep) y = grad.template vector<KIND>(raw[j], terms[j], at * V::kLen, C, place, g, elsewhere);
-        else y = grad.template vector<KIND>(raw[j], at * V::kLen, C, place, g, elsewhere);
-        if (at < whole) V::store_at(to, (uint32_t)at * 16u, V::kLen, y);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    if (behind > 0 && wid == last_tid / kWave) {
-        const u32x4 y = grad.template vector<KIND>(last, whole * V::kLen - (last_tid - tid) * V::kLen, C, place, g, elsewhere);
-        if (tid == last_tid) V::store_at(to, (uint32_t)whole * 16u, behind, y);
-    }
+        for (int j = 0; j < VECS; ++j) {
+            const int at = j * THREADS + tid;
+            u32x4 y;
+            if constexpr (kKeep) y = grad.template vector<KIND>(raw[j], terms[j], at * V::kLen, C, place, g, elsewhere);
+            else y = grad.template vector<KIND>(raw[j], at * V::kLen, C, place, g, elsewhere);
+            if (at < whole) V::store_at(to, (uint32_t)at * 16u, V::kLen, y);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (behind > 0 && wid == last_tid / kWave) {
+            const u32x4 y = grad.template vector<KIND>(last, whole * V::kLen - (last_tid - tid) * V::kLen, C, place, g, elsewhere);
+            if (tid == last_tid) V::store_at(to, (uint32_t)whole * 16u, behind, y);
+        }
     }
 }
 
@@ -507,7 +507,10 @@ rdk_status_t launch_row(const LogprobArgs &a, const GradArgs &b, int32_t B, hipS
 // token's rank, in rounds or parts -> this way: 8192 bf16 rows of 4096 42.8 -> 21.0 us, 2048 of 1000 13.4 -> 7.1, 1024 of 16384 13.5 -> 12.7, 2048 of 32064 32.3 -> 30.9, 64 of
 // 32064 12.5 -> 6.5, 8192 fp32 rows of 2048 33.6 -> 16.2).  Weights take more registers: 512 rows of 16384 14.2 -> 10.2, 1024 16.2 -> 17.3 and so not.  1024 threads where a
 // row has a compute unit for itself (256 bf16 rows of 65536 16.0 -> 12.9, 512 21.2 -> 23.3; 256 rows of 32000 weights, 8 tokens 19.6 -> 14.8); a few rows of many tokens
-// are spread over more units instead, whose wavefronts have fewer ranks to count (one row of 65536, 8 tokens 11.8 us, 17.5 this way).  A launch counts its threads in 32 bits.
+// are spread over more units instead, whose wavefronts have fewer ranks to count (bf16 rows of 65536, this way / in parts: 31 rows with one token 9.3 / 12.5, with two 10.6 / 13.1,
+// three 11.8 / 13.7, eight 18.3 / 17.7, 32 rows the same; 8 rows with two 10.4 / 10.6, three 11.7 / 10.5, eight 18.1 / 12.2; so the line at 32 rows gives up to 2 us of three or four
+// tokens away, and of fp32 rows, which come out ahead this way up to eight tokens from 24 rows on, up to 3: 31 of 32768, three tokens 8.2 / 11.2).  A launch counts its threads in 32
+// bits.
 template <int KIND>
 rdk_status_t launch_forward(const LogprobArgs &a, int32_t B, hipStream_t st)
 {

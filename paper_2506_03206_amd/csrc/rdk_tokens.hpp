@@ -84,7 +84,7 @@ __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((u
 
 constexpr float kWide = 0x1p22f;
 
-// The sums that a lane, and later a workgroup, holds.  With y = x log2(e) / T (weights: log2 x) and a whole number ref that the largest y exceeds by 2^8 at most:
+// The sums that a lane, and later a workgroup, holds.  With y = x log2(e) / T (weights: log2 x) and a whole number ref that the largest y exceeds by about 8.5 at most (terms up to 2^8.5):
 //   sum = sum 2^(y - ref),   pull = sum 2^(y - ref) (y - ref)
 // A whole reference is exact in a product and sum of one rounding, so an entry costs an addition less than with a difference first, and a change of it is
 // a power of two.  (Rows with y beyond +-2^22, where a product is rounded by more than a fraction, are read again: kWide.)
